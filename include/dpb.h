@@ -377,6 +377,128 @@ dpb_status dpb_variance_loss(const dpb_plan* plan, const int32_t* idx, const flo
 dpb_status dpb_variance_grad(const dpb_plan* plan, int64_t T, const void* workspace, size_t ws_bytes,
                              float* grad_coef, const float* grad_scale, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * TRAINING OPERATORS beside the bottleneck: the attention sublayer of its
+ * block with its gradient, and the optimizer's step.  They need no plan and run
+ * on the current device. */
+
+/* One [sequences, tokens, heads, head_dim] tensor of an attention call: device
+ * pointer, 16-byte aligned, and strides in ELEMENTS, each a multiple of 16
+ * bytes; the elements of a head are contiguous.  Any order of the dimensions and
+ * views into larger tensors are fine, and so are inputs whose strides are 0; a
+ * stride along which there is one entry is ignored.  With packed sequences the
+ * tensor is [tokens, heads, head_dim] and batch_stride is ignored. */
+typedef struct {
+    void* data;
+    int64_t batch_stride, token_stride, head_stride;
+} dpb_heads;
+
+/* Sizes and masks of an attention call.
+ *  - Padded sequences (q_starts and k_starts NULL): `batch` sequences of q_len
+ *    query and k_len key rows; q_lens / k_lens (device int32 [batch], or NULL for
+ *    all rows) give the rows that take part, clamped to [0, q_len] / [0, k_len].
+ *    Rows behind them may hold anything, NaN included.
+ *  - Packed sequences (q_starts and k_starts: device int32 [batch + 1], rising,
+ *    from 0 to q_rows / k_rows): sequence b has the rows from starts[b] up to
+ *    starts[b + 1], at most q_len / k_len of them (the longest sequence, or more).
+ *    q_rows, k_rows: rows of the tensors.  q_lens and k_lens must be NULL.  Starts
+ *    outside the tensor are clamped to it; output rows that belong to no sequence
+ *    are not written.
+ *  - Query heads share key heads: head h reads key head h / (heads / kv_heads).
+ *  - With `causal`, query i of a sequence of q queries and k keys sees the keys
+ *    j <= i + k - q (the last query sees them all); without it, all k.
+ *  - scale > 0 multiplies the scores. */
+typedef struct {
+    int64_t batch, q_len, k_len;
+    int64_t q_rows, k_rows;   /* packed sequences only */
+    int heads, kv_heads, head_dim;
+    int causal;
+    float scale;
+    const int32_t *q_lens, *k_lens;
+    const int32_t *q_starts, *k_starts;
+} dpb_attn;
+
+/* Bytes of device workspace that dpb_attention / dpb_attention_bwd need (0 for
+ * a NULL or empty description).  The forward needs some where it splits the keys
+ * of few query rows over many workgroups; the backward two floats per query row and
+ * head. */
+size_t dpb_attention_workspace_bytes(const dpb_attn* a);
+size_t dpb_attention_bwd_workspace_bytes(const dpb_attn* a);
+
+/* ATTENTION: out = softmax(scale Q K^T) V over each query's visible keys, and
+ *   lse = log sum_j exp(scale <q, k_j>).
+ * A query that sees no key, and a padded row that takes no part, gets out = 0 and
+ * lse = -inf.
+ *   dtype   : of q, k, v and out (DPB_F32 or DPB_BF16)
+ *   q, out  : heads heads;  k, v: kv_heads heads
+ *   lse     : device fp32 [rows of q, heads] (padded: [batch, q_len, heads])
+ * Scores, softmax and sums are fp32; with bf16 the probabilities are rounded to
+ * bf16 as operands of the product with V.  The forms: tiles of query rows against
+ * the keys; for few rows (one new token over a cache) the keys are split and the
+ * parts joined.  Either is deterministic.
+ * DPB_EINVAL: a bad size, pointer, stride, scale or workspace; DPB_EUNSUPPORTED:
+ * head_dim over 128 or not a multiple of 8, a token stride of 16 MiB or more,
+ * more than 2^31 rows or workgroups. */
+dpb_status dpb_attention(const dpb_attn* a, dpb_dtype dtype, const dpb_heads* q, const dpb_heads* k,
+                         const dpb_heads* v, const dpb_heads* out, float* lse, void* workspace, size_t ws_bytes,
+                         void* stream);
+
+/* ATTENTION BACKWARD for upstream gradient grad_out, from the forward's out and
+ * lse; the probabilities are recomputed:
+ *   P = exp(scale Q K^T - lse),  dP = dO V^T,  dS = P (dP - sum_d dO O)
+ *   dV = P^T dO,  dQ = scale dS K,  dK = scale dS^T Q
+ * dk and dv of a shared key head are the sums over the query heads that read it.
+ * Rows that take no part get gradients of 0 (padded).  No atomics: the same
+ * inputs give the same bits.
+ *   dq like q, dk and dv like k and v (written; their own strides; must not
+ *   overlap each other or the inputs) */
+dpb_status dpb_attention_bwd(const dpb_attn* a, dpb_dtype dtype, const dpb_heads* grad_out, const dpb_heads* q,
+                             const dpb_heads* k, const dpb_heads* v, const dpb_heads* out, const float* lse,
+                             const dpb_heads* dq, const dpb_heads* dk, const dpb_heads* dv, void* workspace,
+                             size_t ws_bytes, void* stream);
+
+/* Elements that share the scales of 8-bit optimizer states. */
+#define DPB_ADAMW_BLOCK 256
+
+/* Blocks of DPB_ADAMW_BLOCK elements in the states of `count` tensors of sizes[i]
+ * elements: each tensor's states start a new block. */
+int64_t dpb_adamw_blocks(const int64_t* sizes, int count);
+
+/* Settings of one step. */
+typedef struct {
+    double lr, beta1, beta2, eps;
+    int64_t step;             /* 1 for the first step */
+    uint32_t seed;            /* of the rounding of 8-bit states; another one each step */
+} dpb_adamw;
+
+/* ADAMW: one step over many tensors in one launch (per 96 tensors), in place:
+ *   g = grad_scale * grad
+ *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2
+ *   w <- (1 - lr decay) w - lr / (1 - beta1^step) m / (sqrt(v / (1 - beta2^step)) + eps)
+ *   params, grads : host arrays of `count` device pointers to contiguous tensors
+ *                   (aligned to their element; 16 bytes are fastest)
+ *   sizes         : host array, elements of each (0 is skipped)
+ *   weight_decay  : host array, one per tensor, or NULL for 0
+ *   state_bits 32 : m, v are device fp32 [blocks * 256] (first states: zeros)
+ *   state_bits 8  : m and v hold m and sqrt(v) as 8-bit floats (e4m3, no
+ *                   infinities) [blocks * 256] times the block's scales, device
+ *                   fp32 [blocks][2] (m's, sqrt(v)'s); first states: zeros.
+ *                   They are rounded up or down at random, unbiased, by a hash of
+ *                   (seed, place in the states); a positive v never to zero.  A
+ *                   gradient that is not finite makes its block's states so.
+ *   master        : device fp32 [blocks * 256], the weights that the step updates
+ *                   (params then receive them rounded), or NULL: params are
+ *                   updated themselves (in bf16 an update under half a
+ *                   neighbour's distance is lost)
+ *   grad_scale    : device fp32 scalar (loss scaling, clipping), or NULL for 1
+ * m, v, scales and master are 16-byte aligned; tensor i's part starts at block
+ * dpb_adamw_blocks(sizes, i).  Arithmetic is fp32.  DPB_EINVAL for a bad pointer,
+ * size or setting (0 <= beta < 1, eps > 0, step >= 1, finite values). */
+dpb_status dpb_adamw_step(const dpb_adamw* settings, int count, void* const* params, const void* const* grads,
+                          const int64_t* sizes, const float* weight_decay, dpb_dtype param_dtype,
+                          dpb_dtype grad_dtype, int state_bits, void* m, void* v, float* scales, float* master,
+                          const float* grad_scale, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -65,6 +65,12 @@ def load():
         "dpb_variance_workspace_bytes": (ctypes.c_size_t, [P, i64]),
         "dpb_variance_loss": (i32, [P, P, P, i64, i32, P, ctypes.c_size_t, P, P, P, P]),
         "dpb_variance_grad": (i32, [P, i64, P, ctypes.c_size_t, P, P, P]),
+        "dpb_attention_workspace_bytes": (ctypes.c_size_t, [P]),
+        "dpb_attention_bwd_workspace_bytes": (ctypes.c_size_t, [P]),
+        "dpb_attention": (i32, [P, i32] + [P] * 6 + [ctypes.c_size_t, P]),
+        "dpb_attention_bwd": (i32, [P, i32] + [P] * 10 + [ctypes.c_size_t, P]),
+        "dpb_adamw_blocks": (i64, [P, i32]),
+        "dpb_adamw_step": (i32, [P, i32, P, P, P, P, i32, i32, i32, P, P, P, P, P, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -438,3 +444,183 @@ def std_update(plan: Plan, x: torch.Tensor, idx: torch.Tensor, stats: torch.Tens
         _dev(stats, "stats"), _dev(m2, "m2"), _dev(workspace, "workspace"),
         workspace.numel() * workspace.element_size(), _stream(x)))
     return stats, m2
+
+
+# ---- training operators beside the bottleneck: attention and AdamW
+
+class _Attn(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("q_len", ctypes.c_int64), ("k_len", ctypes.c_int64),
+                ("q_rows", ctypes.c_int64), ("k_rows", ctypes.c_int64),
+                ("heads", ctypes.c_int), ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
+                ("causal", ctypes.c_int), ("scale", ctypes.c_float),
+                ("q_lens", ctypes.c_void_p), ("k_lens", ctypes.c_void_p),
+                ("q_starts", ctypes.c_void_p), ("k_starts", ctypes.c_void_p)]
+
+
+class _Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64)]
+
+
+def _heads(t: torch.Tensor, name: str):
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    st = t.stride()
+    if st[-1] != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{name} must be contiguous along head_dim")
+    return ctypes.byref(_Heads(t.data_ptr(), 0 if t.dim() == 3 else st[0], st[-3], st[-2]))
+
+
+def _attn(q, k, v, causal, scale, q_lens, k_lens, q_starts, k_starts, max_q, max_k):
+    """The description of an attention call, its arguments checked."""
+    packed = q_starts is not None
+    assert packed == (k_starts is not None), "packed sequences need q_starts and k_starts"
+    assert q.dim() == k.dim() == (3 if packed else 4) and v.shape == k.shape and k.shape[-1] == q.shape[-1]
+    assert q.dtype == k.dtype == v.dtype
+    if packed:
+        assert q_lens is None and k_lens is None and max_q is not None and max_k is not None
+        batch, q_len, k_len = q_starts.shape[0] - 1, int(max_q), int(max_k)
+        assert batch >= 0 and k_starts.shape == q_starts.shape
+    else:
+        batch, q_len, k_len = q.shape[0], q.shape[1], k.shape[1]
+        assert k.shape[0] == batch
+    for n in (q_lens, k_lens):
+        assert n is None or n.shape == (batch,)
+    for n in (q_lens, k_lens, q_starts, k_starts):
+        assert n is None or n.dtype == torch.int32
+    dim = q.shape[-1]
+    return _Attn(batch, q_len, k_len, q.shape[0] if packed else 0, k.shape[0] if packed else 0, q.shape[-2],
+                 k.shape[-2], dim, int(bool(causal)), dim ** -0.5 if scale is None else scale,
+                 _opt(q_lens, "q_lens"), _opt(k_lens, "k_lens"), _opt(q_starts, "q_starts"),
+                 _opt(k_starts, "k_starts"))
+
+
+def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = False, scale: float | None = None,
+              q_lens: torch.Tensor | None = None, k_lens: torch.Tensor | None = None,
+              q_starts: torch.Tensor | None = None, k_starts: torch.Tensor | None = None,
+              max_q: int | None = None, max_k: int | None = None, out: torch.Tensor | None = None,
+              lse: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """softmax(scale q k^T) v -> (out like q, lse fp32 [..., heads]).
+
+    Padded: q [B, Sq, H, D], k and v [B, Sk, Hkv, D] (any order in memory), with
+    lengths q_lens / k_lens int32 [B] or none; packed: q [rows, H, D], k and v
+    [rows, Hkv, D] with q_starts / k_starts int32 [B + 1] and the longest sequences
+    max_q / max_k.  scale defaults to 1 / sqrt(D); causal: query i sees the keys
+    j <= i + k_len - q_len.  A query that sees none gets 0 and lse -inf."""
+    a = _attn(q, k, v, causal, scale, q_lens, k_lens, q_starts, k_starts, max_q, max_k)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.empty(q.shape[:-1], dtype=torch.float32, device=q.device)
+    assert out.shape == q.shape and out.dtype == q.dtype
+    assert lse.shape == q.shape[:-1] and lse.dtype == torch.float32
+    ref = ctypes.byref(a)
+    lib = load()
+    need = lib.dpb_attention_workspace_bytes(ref)
+    if need and workspace is None:
+        workspace = torch.empty((need + 3) // 4, dtype=torch.float32, device=q.device)
+    _check("dpb_attention", lib.dpb_attention(
+        ref, _dtype_code(q), _heads(q, "q"), _heads(k, "k"), _heads(v, "v"), _heads(out, "out"), _dev(lse, "lse"),
+        _opt(workspace, "workspace"), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+        _stream(q)))
+    return out, lse
+
+
+def attention_bwd(grad_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                  lse: torch.Tensor, causal: bool = False, scale: float | None = None,
+                  q_lens: torch.Tensor | None = None, k_lens: torch.Tensor | None = None,
+                  q_starts: torch.Tensor | None = None, k_starts: torch.Tensor | None = None,
+                  max_q: int | None = None, max_k: int | None = None, dq: torch.Tensor | None = None,
+                  dk: torch.Tensor | None = None, dv: torch.Tensor | None = None,
+                  workspace: torch.Tensor | None = None):
+    """Gradients (dq, dk, dv) of attention for grad_out, from its out and lse; the
+    other arguments as in the forward call."""
+    a = _attn(q, k, v, causal, scale, q_lens, k_lens, q_starts, k_starts, max_q, max_k)
+    assert grad_out.shape == out.shape == q.shape and grad_out.dtype == out.dtype == q.dtype
+    assert lse.shape == q.shape[:-1] and lse.dtype == torch.float32
+    grads = []
+    for x, g in ((q, dq), (k, dk), (v, dv)):
+        grads.append(torch.empty(x.shape, dtype=x.dtype, device=x.device) if g is None else g)
+        assert grads[-1].shape == x.shape and grads[-1].dtype == x.dtype
+    ref = ctypes.byref(a)
+    lib = load()
+    if workspace is None:
+        need = lib.dpb_attention_bwd_workspace_bytes(ref)
+        workspace = torch.empty((need + 3) // 4, dtype=torch.float32, device=q.device)
+    dq, dk, dv = grads
+    _check("dpb_attention_bwd", lib.dpb_attention_bwd(
+        ref, _dtype_code(q), _heads(grad_out, "grad_out"), _heads(q, "q"), _heads(k, "k"), _heads(v, "v"),
+        _heads(out, "out"), _dev(lse, "lse"), _heads(dq, "dq"), _heads(dk, "dk"), _heads(dv, "dv"),
+        _dev(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream(q)))
+    return dq, dk, dv
+
+
+ADAMW_BLOCK = 256
+
+
+class _AdamW(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("step", ctypes.c_int64), ("seed", ctypes.c_uint32)]
+
+
+def adamw_blocks(sizes: Sequence[int]) -> int:
+    """Blocks of ADAMW_BLOCK elements in the states of tensors of these sizes."""
+    n = len(sizes)
+    return int(load().dpb_adamw_blocks((ctypes.c_int64 * n)(*sizes), n))
+
+
+def adamw_state(params: Sequence[torch.Tensor], bits: int = 32, master: bool = False):
+    """First states (m, v, scales, master) of adamw_step for these tensors: m and v
+    fp32, or 8-bit floats with scales [blocks, 2]; master: fp32 copies of the
+    tensors (or None)."""
+    sizes = [p.numel() for p in params]
+    blocks, dev = adamw_blocks(sizes), params[0].device
+    m, v = (torch.zeros(blocks * ADAMW_BLOCK, dtype=torch.float32 if bits == 32 else torch.float8_e4m3fn, device=dev)
+            for _ in range(2))
+    scales = None if bits == 32 else torch.zeros((blocks, 2), dtype=torch.float32, device=dev)
+    weights = None
+    if master:
+        weights, at = torch.zeros(blocks * ADAMW_BLOCK, dtype=torch.float32, device=dev), 0
+        for p, n in zip(params, sizes):
+            weights[at:at + n] = p.detach().reshape(-1)
+            at += -(-n // ADAMW_BLOCK) * ADAMW_BLOCK
+    return m, v, scales, weights
+
+
+def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m: torch.Tensor, v: torch.Tensor,
+               scales: torch.Tensor | None = None, master: torch.Tensor | None = None, *, step: int, lr: float,
+               betas: tuple[float, float] = (0.9, 0.999), eps: float = 1e-8,
+               weight_decay: float | Sequence[float] = 0.0, grad_scale: torch.Tensor | None = None, seed: int = 0):
+    """One AdamW step over all params in place, with the states of adamw_state (8
+    bits when scales are given).  weight_decay: one for all, or one per tensor; seed:
+    of the rounding of 8-bit states, another one each step; grad_scale: a device
+    scalar that multiplies the gradients.  All params have one type, all grads one."""
+    n = len(params)
+    assert len(grads) == n
+    if n == 0:
+        return
+    sizes = [p.numel() for p in params]
+    pt, gt = params[0].dtype, grads[0].dtype
+    for p, g, k in zip(params, grads, sizes):
+        assert g.numel() == k and p.dtype == pt and g.dtype == gt
+        if not (p.is_cuda and g.is_cuda):
+            raise ValueError("params and grads must be device tensors")
+        if not (p.is_contiguous() and g.is_contiguous()):
+            raise ValueError("params and grads must be contiguous")
+    size_arr = (ctypes.c_int64 * n)(*sizes)
+    lib = load()
+    elems = lib.dpb_adamw_blocks(size_arr, n) * ADAMW_BLOCK
+    state = torch.float32 if scales is None else torch.float8_e4m3fn
+    assert m.dtype == v.dtype == state and m.numel() >= elems and v.numel() >= elems
+    assert scales is None or (scales.dtype == torch.float32 and scales.numel() >= elems // (ADAMW_BLOCK // 2))
+    assert master is None or (master.dtype == torch.float32 and master.numel() >= elems)
+    assert grad_scale is None or (grad_scale.dtype == torch.float32 and grad_scale.numel() == 1)
+    decay = [weight_decay] * n if isinstance(weight_decay, (int, float)) else weight_decay
+    assert len(decay) == n
+    pointers = ctypes.c_void_p * n
+    o = _AdamW(lr, betas[0], betas[1], eps, step, seed & 0xFFFFFFFF)
+    _check("dpb_adamw_step", lib.dpb_adamw_step(
+        ctypes.byref(o), n, pointers(*[p.data_ptr() for p in params]), pointers(*[g.data_ptr() for g in grads]),
+        size_arr, (ctypes.c_float * n)(*decay), _dtype_code(params[0]), _dtype_code(grads[0]),
+        32 if scales is None else 8, _dev(m, "m"), _dev(v, "v"), _opt(scales, "scales"), _opt(master, "master"),
+        _opt(grad_scale, "grad_scale"), _stream(m)))

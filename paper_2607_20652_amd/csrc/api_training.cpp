@@ -1,0 +1,241 @@
+// C ABI of the training operators: argument validation and launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "../../include/dpb.h"
+#include "adamw.hpp"
+#include "attention.hpp"
+
+static_assert(dpb::kAdamwBlock == DPB_ADAMW_BLOCK, "optimizer state blocks");
+
+namespace {
+
+using dpb::AttnArgs;
+using dpb::AttnRows;
+
+constexpr int64_t kMaxRows = ((int64_t)1 << 31) - 256;   // rows and workgroups are counted in 32 bits
+constexpr int64_t kMaxTokenBytes = (int64_t)1 << 24;     // the rows of a tile stay within a 32-bit offset
+constexpr int kMaxDim = 128;
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+bool dtype_ok(dpb_dtype t) { return t == DPB_F32 || t == DPB_BF16; }
+int64_t bytes_of(dpb_dtype t) { return t == DPB_BF16 ? 2 : 4; }
+
+dpb_status launched(hipError_t e)
+{
+    if (e == hipSuccess) return DPB_OK;
+    (void)hipGetLastError();
+    return DPB_EHIP;
+}
+
+// The sizes of a call, without its tensors.
+dpb_status check_sizes(const dpb_attn* a)
+{
+    if (!a || a->batch < 0 || a->q_len < 0 || a->k_len < 0 || a->heads < 1 || a->kv_heads < 1 ||
+        a->heads % a->kv_heads || a->head_dim < 1)
+        return DPB_EINVAL;
+    if (!(a->scale > 0.f) || !std::isfinite(a->scale)) return DPB_EINVAL;
+    if (!a->q_starts != !a->k_starts) return DPB_EINVAL;
+    if (a->q_starts && (a->q_lens || a->k_lens || a->q_rows < 0 || a->k_rows < 0)) return DPB_EINVAL;
+    if (a->head_dim > kMaxDim || a->head_dim % 8) return DPB_EUNSUPPORTED;
+    const int64_t group = a->heads / a->kv_heads;
+    if (a->batch > kMaxRows || a->q_len > kMaxRows / group || a->k_len > kMaxRows) return DPB_EUNSUPPORTED;
+    if (a->q_starts && (a->q_rows > kMaxRows || a->k_rows > kMaxRows)) return DPB_EUNSUPPORTED;
+    // workgroups: at most one per 32 rows and head, and per 128 keys and head
+    const int64_t tiles = std::max((a->q_len * group + 31) / 32, (a->k_len + 127) / 128);
+    if (a->batch > 0 && tiles > 0 && (a->kv_heads > kMaxRows / a->batch || a->kv_heads * a->batch > kMaxRows / tiles))
+        return DPB_EUNSUPPORTED;
+    return DPB_OK;
+}
+
+bool packed(const dpb_attn* a) { return a->q_starts != nullptr; }
+int64_t rows_of(const dpb_attn* a, bool q)
+{
+    return packed(a) ? (q ? a->q_rows : a->k_rows) : a->batch * (q ? a->q_len : a->k_len);
+}
+
+// One tensor: its pointer and strides in bytes.  `q`: it has the query's rows and heads.
+dpb_status take(const dpb_attn* a, dpb_dtype t, const dpb_heads* x, bool q, AttnRows* out)
+{
+    if (!x) return DPB_EINVAL;
+    const int64_t tokens = packed(a) ? (q ? a->q_rows : a->k_rows) : (q ? a->q_len : a->k_len);
+    const int64_t heads = q ? a->heads : a->kv_heads;
+    out->p = (char*)x->data;
+    out->bs = packed(a) || a->batch <= 1 ? 0 : x->batch_stride;
+    out->ts = tokens <= 1 ? 0 : x->token_stride;
+    out->hs = heads <= 1 ? 0 : x->head_stride;
+    if (rows_of(a, q) > 0 && (!x->data || !aligned16(x->data))) return DPB_EINVAL;
+    int64_t* strides[3] = {&out->bs, &out->ts, &out->hs};
+    for (int64_t* s : strides) {
+        if (*s < 0 || *s > ((int64_t)1 << 56) || (*s * bytes_of(t)) % 16) return DPB_EINVAL;
+        *s *= bytes_of(t);
+    }
+    return out->ts >= kMaxTokenBytes ? DPB_EUNSUPPORTED : DPB_OK;
+}
+
+void fill_args(const dpb_attn* a, AttnArgs* g)
+{
+    std::memset((void*)g, 0, sizeof *g);
+    g->q_lens = a->q_lens;
+    g->k_lens = a->k_lens;
+    g->q_starts = a->q_starts;
+    g->k_starts = a->k_starts;
+    g->q_rows = rows_of(a, true);
+    g->k_rows = rows_of(a, false);
+    g->batch = (int)a->batch;
+    g->q_len = (int)a->q_len;
+    g->k_len = (int)a->k_len;
+    g->heads = a->heads;
+    g->kv_heads = a->kv_heads;
+    g->group = a->heads / a->kv_heads;
+    g->dim = a->head_dim;
+    g->causal = a->causal != 0;
+    g->scale = a->scale;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t dpb_attention_workspace_bytes(const dpb_attn* a)
+{
+    return 0;
+}
+
+size_t dpb_attention_bwd_workspace_bytes(const dpb_attn* a)
+{
+    if (check_sizes(a)) return 0;
+    return (size_t)rows_of(a, true) * a->heads * 8;
+}
+
+dpb_status dpb_attention(const dpb_attn* a, dpb_dtype dtype, const dpb_heads* q, const dpb_heads* k,
+                         const dpb_heads* v, const dpb_heads* out, float* lse, void* workspace, size_t ws_bytes,
+                         void* stream)
+{
+    dpb_status s = check_sizes(a);
+    if (s) return s;
+    if (!dtype_ok(dtype)) return DPB_EINVAL;
+    AttnArgs g;
+    fill_args(a, &g);
+    const struct { const dpb_heads* x; bool q; AttnRows* to; } all[4] = {
+        {q, true, &g.q}, {k, false, &g.k}, {v, false, &g.v}, {out, true, &g.o}};
+    for (const auto& t : all)
+        if ((s = take(a, dtype, t.x, t.q, t.to))) return s;
+    if (a->batch == 0 || a->q_len == 0 || g.q_rows == 0) return DPB_OK;
+    if (!lse || !aligned16(lse)) return DPB_EINVAL;
+    g.lse = lse;
+    return launched(dpb::launch_attention(g, dtype == DPB_BF16, (hipStream_t)stream));
+}
+
+dpb_status dpb_attention_bwd(const dpb_attn* a, dpb_dtype dtype, const dpb_heads* grad_out, const dpb_heads* q,
+                             const dpb_heads* k, const dpb_heads* v, const dpb_heads* out, const float* lse,
+                             const dpb_heads* dq, const dpb_heads* dk, const dpb_heads* dv, void* workspace,
+                             size_t ws_bytes, void* stream)
+{
+    dpb_status s = check_sizes(a);
+    if (s) return s;
+    if (!dtype_ok(dtype)) return DPB_EINVAL;
+    AttnArgs g;
+    fill_args(a, &g);
+    const struct { const dpb_heads* x; bool q; AttnRows* to; } all[8] = {
+        {grad_out, true, &g.go}, {q, true, &g.q}, {k, false, &g.k}, {v, false, &g.v}, {out, true, &g.o},
+        {dq, true, &g.gq}, {dk, false, &g.gk}, {dv, false, &g.gv}};
+    for (const auto& t : all)
+        if ((s = take(a, dtype, t.x, t.q, t.to))) return s;
+    if (a->batch == 0 || (g.q_rows == 0 && g.k_rows == 0)) return DPB_OK;
+    const size_t need = dpb_attention_bwd_workspace_bytes(a);
+    if (g.q_rows > 0 && (!lse || !aligned16(lse) || !workspace || !aligned16(workspace) || ws_bytes < need))
+        return DPB_EINVAL;
+    // an output that is an input (or another output) would be read after it is written
+    const void* outs[3] = {g.gq.p, g.gk.p, g.gv.p};
+    const void* ins[5] = {g.go.p, g.q.p, g.k.p, g.v.p, g.o.p};
+    for (int i = 0; i < 3; ++i) {
+        for (const void* p : ins)
+            if (outs[i] && outs[i] == p) return DPB_EINVAL;
+        for (int j = 0; j < i; ++j)
+            if (outs[i] && outs[i] == outs[j]) return DPB_EINVAL;
+    }
+    g.lse = const_cast<float*>(lse);
+    g.row_lse2 = (float*)workspace;
+    g.row_delta = g.row_lse2 + g.q_rows * a->heads;
+    return launched(dpb::launch_attention_bwd(g, dtype == DPB_BF16, (hipStream_t)stream));
+}
+
+int64_t dpb_adamw_blocks(const int64_t* sizes, int count)
+{
+    int64_t n = 0;
+    for (int i = 0; sizes && i < count; ++i) n += sizes[i] > 0 ? (sizes[i] - 1) / DPB_ADAMW_BLOCK + 1 : 0;
+    return n;
+}
+
+dpb_status dpb_adamw_step(const dpb_adamw* o, int count, void* const* params, const void* const* grads,
+                          const int64_t* sizes, const float* weight_decay, dpb_dtype param_dtype,
+                          dpb_dtype grad_dtype, int state_bits, void* m, void* v, float* scales, float* master,
+                          const float* grad_scale, void* stream)
+{
+    if (!o || count < 0 || !dtype_ok(param_dtype) || !dtype_ok(grad_dtype) || (state_bits != 8 && state_bits != 32))
+        return DPB_EINVAL;
+    if (!std::isfinite(o->lr) || !(o->beta1 >= 0. && o->beta1 < 1.) || !(o->beta2 >= 0. && o->beta2 < 1.) ||
+        !((float)o->eps > 0.f) || !std::isfinite(o->eps) || o->step < 1)
+        return DPB_EINVAL;
+    if (count == 0) return DPB_OK;
+    if (!params || !grads || !sizes) return DPB_EINVAL;
+    int64_t blocks = 0;
+    for (int i = 0; i < count; ++i) {
+        if (sizes[i] < 0 || (weight_decay && !std::isfinite(weight_decay[i]))) return DPB_EINVAL;
+        if (sizes[i] == 0) continue;
+        if (!params[i] || !grads[i] || (uintptr_t)params[i] % bytes_of(param_dtype) ||
+            (uintptr_t)grads[i] % bytes_of(grad_dtype))
+            return DPB_EINVAL;
+        blocks += (sizes[i] - 1) / DPB_ADAMW_BLOCK + 1;
+        if (blocks > kMaxRows) return DPB_EUNSUPPORTED;
+    }
+    if (blocks == 0) return DPB_OK;
+    if (!m || !v || !aligned16(m) || !aligned16(v) || !aligned16(scales) || !aligned16(master) ||
+        ((uintptr_t)grad_scale & 3u) || (state_bits == 8 && !scales))
+        return DPB_EINVAL;
+
+    dpb::AdamwArgs g;
+    std::memset((void*)&g, 0, sizeof g);
+    g.m = m;
+    g.v = v;
+    g.scales = scales;
+    g.master = master;
+    g.grad_scale = grad_scale;
+    g.beta1 = (float)o->beta1;
+    g.rest1 = (float)(1. - o->beta1);
+    g.beta2 = (float)o->beta2;
+    g.rest2 = (float)(1. - o->beta2);
+    g.eps = (float)o->eps;
+    g.rate = (float)(o->lr / (1. - std::pow(o->beta1, (double)o->step)));
+    g.unbias2 = (float)(1. / std::sqrt(1. - std::pow(o->beta2, (double)o->step)));
+    g.seed = o->seed;
+    int64_t block = 0;
+    int chunks = 0;
+    for (int i = 0; i < count; ++i) {
+        if (sizes[i] > 0) {
+            const int64_t n = (sizes[i] - 1) / DPB_ADAMW_BLOCK + 1;
+            dpb::AdamwTensor& t = g.tensor[g.count];
+            t.param = params[i];
+            t.grad = grads[i];
+            t.n = sizes[i];
+            t.block = (int32_t)block;
+            t.shrink = (float)(1. - o->lr * (weight_decay ? (double)weight_decay[i] : 0.));
+            g.first_chunk[g.count++] = chunks;
+            chunks += (int)((n + dpb::kAdamwChunk - 1) / dpb::kAdamwChunk);
+            block += n;
+        }
+        if (g.count == dpb::kAdamwTensors || (i == count - 1 && g.count > 0)) {
+            const dpb_status s = launched(dpb::launch_adamw(g, chunks, param_dtype == DPB_BF16, grad_dtype == DPB_BF16,
+                                                            state_bits == 8, (hipStream_t)stream));
+            if (s) return s;
+            g.count = chunks = 0;
+        }
+    }
+    return DPB_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,259 @@
+// Attention kernels: arguments, sequences, LDS tiles and matrix-core products
+// shared by the forward and the backward.
+//
+// Every product is a chain of 32 x 32 MFMAs.  An operand fragment holds, per
+// lane, one row (lane % 32) and eight values of the contraction; a result
+// fragment one column (lane % 32) and sixteen rows, in groups of four:
+//     row(r) = 8 * (r / 4) + 4 * (lane / 32) + r % 4.
+// The order of the values inside a contraction is free as long as both
+// operands agree, so a result (scores, probabilities) becomes the operand of
+// the next product where it lies, in registers: the eight values of its
+// registers 8s..8s+7 stand for rows 16s + 4h + {0..3} and 16s + 8 + 4h + {0..3}
+// (h = lane / 32), and the other operand is read from LDS in that order.
+#pragma once
+
+#include "device_common.hpp"
+
+namespace dpb {
+
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+
+// One [sequences, tokens, heads, head_dim] tensor; strides in bytes.
+struct AttnRows {
+    char* p;
+    int64_t bs, ts, hs;
+};
+
+struct AttnArgs {
+    AttnRows q, k, v, o;             // o: written by the forward, read by the backward
+    AttnRows go, gq, gk, gv;         // backward: gradient of o (read), of q, k, v (written)
+    float* lse;                      // [query rows, heads]
+    float* row_lse2;                 // backward scratch [heads][query rows]: lse * log2(e)
+    float* row_delta;                // and sum_d go * o
+    float* part;                     // forward scratch of a split call (see attention.hip)
+    const int32_t *q_lens, *k_lens;      // padded: lengths, or null
+    const int32_t *q_starts, *k_starts;  // packed: starts, or null
+    int64_t q_rows, k_rows;          // rows of q and k in all
+    int batch, q_len, k_len;         // sequences; padded lengths, or the longest packed ones
+    int heads, kv_heads, group, dim;
+    int causal;
+    int splits;
+    float scale;
+};
+
+hipError_t launch_attention(const AttnArgs& a, bool bf16, hipStream_t stream);
+hipError_t launch_attention_bwd(const AttnArgs& a, bool bf16, hipStream_t stream);
+// Parts that the keys of a call are split into, and the scratch floats that takes.
+int attention_splits(int batch, int q_len, int k_len, int heads, int kv_heads);
+size_t attention_part_floats(int batch, int q_len, int heads, int dim, int splits);
+
+// Where sequence b lies: rows before it, its lengths, and the query (key) rows
+// of the outputs that belong to it.  Packed starts are clamped to the tensor, so
+// that no value of theirs makes a kernel leave it.
+struct Sequence {
+    int64_t q0, k0;     // first row of the sequence in q (out, lse) and in k, v
+    int64_t qbs, kbs;   // 1 when that row is reached by the batch stride
+    int qn, kn;         // rows that take part
+    int qw, kw;         // rows to write
+};
+
+__device__ __forceinline__ void sequence_rows(const int32_t* starts, const int32_t* lens, int64_t rows, int len, int b,
+                                              int64_t& first, int& n, int& written)
+{
+    if (starts) {
+        const int64_t s = min(max((int64_t)starts[b], (int64_t)0), rows);
+        const int64_t e = min(max((int64_t)starts[b + 1], s), rows);
+        first = s;
+        n = written = (int)min(e - s, (int64_t)len);
+    } else {
+        first = (int64_t)b * len;
+        n = lens ? min(max(lens[b], 0), len) : len;
+        written = len;
+    }
+}
+
+__device__ __forceinline__ Sequence sequence_of(const AttnArgs& a, int b)
+{
+    Sequence s;
+    sequence_rows(a.q_starts, a.q_lens, a.q_rows, a.q_len, b, s.q0, s.qn, s.qw);
+    sequence_rows(a.k_starts, a.k_lens, a.k_rows, a.k_len, b, s.k0, s.kn, s.kw);
+    return s;
+}
+
+// First byte of (sequence b, head h).
+__device__ __forceinline__ char* head_base(const AttnRows& t, bool packed, int b, int64_t first, int h)
+{
+    return t.p + (packed ? first * t.ts : (int64_t)b * t.bs) + (int64_t)h * t.hs;
+}
+
+// Keys that query `token` of a sequence sees: the first `visible` ones.
+__device__ __forceinline__ int visible_keys(const AttnArgs& a, const Sequence& s, int token)
+{
+    if (token >= s.qn) return 0;
+    return a.causal ? min(max(token + 1 + s.kn - s.qn, 0), s.kn) : s.kn;
+}
+
+// Workgroup ids go round the eight XCDs in turn; this order gives every XCD a
+// contiguous run of the work, so that the workgroups that read one head's keys
+// share an L2.
+__device__ __forceinline__ int xcd_order(int id, int total)
+{
+    const int x = id & 7, q = total >> 3, r = total & 7;
+    return x * q + min(x, r) + (id >> 3);
+}
+
+// ---- elements
+
+template <typename T> struct Operand;   // eight values of one lane
+template <> struct Operand<__bf16> { typedef bf16x8 type; };
+template <> struct Operand<float> { typedef f32x8 type; };
+
+__device__ __forceinline__ f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma(f32x8 a, f32x8 b, f32x16 c)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+}
+
+// Registers 8s..8s+7 of a result as an operand (bf16: rounded to nearest even, the
+// precision of the products' inputs; sums stay in fp32).
+template <typename T>
+__device__ __forceinline__ typename Operand<T>::type as_operand(const f32x16& c, int s)
+{
+    typename Operand<T>::type v;
+    if constexpr (sizeof(T) == 2) {
+        u32x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(c[8 * s + 2 * i], c[8 * s + 2 * i + 1]);
+        v = __builtin_bit_cast(bf16x8, w);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = c[8 * s + i];
+    }
+    return v;
+}
+
+// Lanes l and l ^ 32 hold the two halves of a column.
+__device__ __forceinline__ float other_half(float v)
+{
+    return __shfl_xor(v, 32, 64);
+}
+
+// Eight values of a row in global memory, from element 16s + 8h; zero past dim.
+template <typename T>
+__device__ __forceinline__ typename Operand<T>::type global_operand(const char* row, int s, int dim, bool valid)
+{
+    typename Operand<T>::type v = {};
+    const int e = 16 * s + 8 * ((threadIdx.x & 63) >> 5);
+    if (valid && e < dim) v = *(const typename Operand<T>::type*)(row + e * sizeof(T));
+    return v;
+}
+
+// Four values of column `lane % 32` of a result, as values 8g + 4h.. of a row.
+template <typename T>
+__device__ __forceinline__ void store4(char* row, int e, float a, float b, float c, float d)
+{
+    if constexpr (sizeof(T) == 2) *(u32x2*)(row + e * 2) = (u32x2){pack_bf16x2(a, b), pack_bf16x2(c, d)};
+    else *(f32x4*)(row + e * 4) = (f32x4){a, b, c, d};
+}
+
+// ---- LDS tiles
+
+// A tile of R rows of one head in LDS, DP values wide (DP: dim rounded up to 64
+// or 128), rows behind each other in 16-byte chunks.  Chunk c of row r lies at
+// place c ^ turn(r): reading one chunk of sixteen rows, or two chunks of four
+// rows for a transposed read, then meets every bank once.  WAVES waves fill it
+// straight from global memory (no registers), 1 KB an instruction; the place a
+// lane writes is fixed, so the lane picks the chunk that belongs there.  Rows
+// past the sequence and chunks past dim are asked for out of the buffer's range
+// and arrive as zeros.
+template <typename T, int DP, int R, int WAVES = 4>
+struct Tile {
+    static constexpr int kRowBytes = DP * (int)sizeof(T);
+    static constexpr int kChunks = kRowBytes / 16;
+    static constexpr int kBytes = R * kRowBytes;
+    static constexpr int kLoads = kBytes / 1024 / WAVES;      // instructions a wave
+    static constexpr int kLoadRows = 1024 / kRowBytes;        // rows an instruction
+    static_assert(kLoads * WAVES * 1024 == kBytes, "a tile is a whole number of loads");
+    typedef typename Operand<T>::type Op;
+
+    __device__ static __forceinline__ int turn(int r)
+    {
+        if constexpr (kChunks == 8) return 2 * ((r >> 1) & 3) + ((r >> 3) & 1);
+        else return 2 * (r & 7) + ((r >> 3) & 1);
+    }
+
+    // Enqueues the tile's loads: rows [0, left) from `first`, `stride` bytes apart.
+    // (Whoever reads the tile waits for them: fill_wait, and a barrier if other
+    // waves filled parts of it.)
+    __device__ static __forceinline__ void fill(char* lds, const char* first, int64_t stride, int left, int dim, int wave)
+    {
+        const int lane = threadIdx.x & 63;
+        const int n = min(left, R);
+        const uint32_t bytes = n > 0 ? (uint32_t)((n - 1) * stride + dim * (int)sizeof(T)) : 0u;
+        const __amdgpu_buffer_rsrc_t buf =
+            __builtin_amdgcn_make_buffer_rsrc((void*)first, 0, (int)bytes, 0x00027000);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int at = (i * WAVES + wave) * kLoadRows;
+            const int r = at + lane / kChunks, c = (lane % kChunks) ^ turn(r);
+            const uint32_t off = r < n && c * 16 < dim * (int)sizeof(T) ? (uint32_t)r * (uint32_t)stride + c * 16 : 0xFFFFFFF0u;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lds_void*)(lds + at * kRowBytes), 16, (int)off, 0, 0, 0);
+        }
+    }
+
+    // Operand: row `row + lane % 32`, values 16s + 8h + {0..7}.
+    __device__ static __forceinline__ Op rows(const char* lds, int row, int s)
+    {
+        const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+        const char* p = lds + row * kRowBytes + r * kRowBytes;
+        if constexpr (sizeof(T) == 2) {
+            return *(const bf16x8*)(p + (((2 * s + h) ^ turn(r)) << 4));
+        } else {
+            const int c = 4 * s + 2 * h;
+            const f32x4 a = *(const f32x4*)(p + ((c ^ turn(r)) << 4)), b = *(const f32x4*)(p + (((c + 1) ^ turn(r)) << 4));
+            return (Op){a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+        }
+    }
+
+    // Operand of the transposed tile: value `32 * dt + lane % 32`, rows
+    // 16s + 4h + {0..3} and 16s + 8 + 4h + {0..3}.
+    __device__ static __forceinline__ Op columns(const char* lds, int s, int dt)
+    {
+        const int lane = threadIdx.x & 63, h = lane >> 5;
+        if constexpr (sizeof(T) == 2) {
+            // a group of sixteen lanes reads four rows of sixteen values and gets them transposed
+            const int i = lane & 15, r = 4 * h + (i >> 2), c = 4 * dt + 2 * ((lane >> 4) & 1) + ((i >> 1) & 1);
+            const char* p = lds + s * 16 * kRowBytes + r * kRowBytes + 8 * (i & 1);
+            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + ((c ^ turn(r)) << 4)));
+            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lds_s16x4*)(p + 8 * kRowBytes + ((c ^ turn(r + 8)) << 4)));
+            return __builtin_bit_cast(Op, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            const int c = 8 * dt + ((lane & 31) >> 2);
+            Op v;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int r = 4 * h + 8 * (j >> 2) + (j & 3);
+                v[j] = *(const float*)(lds + (s * 16 + r) * kRowBytes + ((c ^ turn(r)) << 4) + 4 * (lane & 3));
+            }
+            return v;
+        }
+    }
+};
+
+// Waits for this wave's loads into LDS.
+__device__ __forceinline__ void fill_wait() { __builtin_amdgcn_s_waitcnt(0x0F70); }
+
+}  // namespace dpb
