@@ -65,7 +65,7 @@ dpb_status take(const dpb_attn* a, dpb_dtype t, const dpb_heads* x, bool q, Attn
     const int64_t heads = q ? a->heads : a->kv_heads;
     out->p = (char*)x->data;
     out->bs = packed(a) || a->batch <= 1 ? 0 : x->batch_stride;
-    out->ts = tokens <= 1 ? 0 : x->token_stride;
+    out->ts = tokens <= 1 ? a->head_dim : x->token_stride;
     out->hs = heads <= 1 ? 0 : x->head_stride;
     if (rows_of(a, q) > 0 && (!x->data || !aligned16(x->data))) return DPB_EINVAL;
     int64_t* strides[3] = {&out->bs, &out->ts, &out->hs};
@@ -102,7 +102,9 @@ extern "C" {
 
 size_t dpb_attention_workspace_bytes(const dpb_attn* a)
 {
-    return 0;
+    if (check_sizes(a) || a->batch == 0 || a->q_len == 0) return 0;
+    const int splits = dpb::attention_splits((int)a->batch, (int)a->q_len, (int)a->k_len, a->heads, a->kv_heads);
+    return dpb::attention_part_floats(rows_of(a, true), a->heads, a->head_dim, splits) * 4;
 }
 
 size_t dpb_attention_bwd_workspace_bytes(const dpb_attn* a)
@@ -127,6 +129,10 @@ dpb_status dpb_attention(const dpb_attn* a, dpb_dtype dtype, const dpb_heads* q,
     if (a->batch == 0 || a->q_len == 0 || g.q_rows == 0) return DPB_OK;
     if (!lse || !aligned16(lse)) return DPB_EINVAL;
     g.lse = lse;
+    g.splits = dpb::attention_splits(g.batch, g.q_len, g.k_len, g.heads, g.kv_heads);
+    const size_t need = dpb::attention_part_floats(g.q_rows, g.heads, g.dim, g.splits) * 4;
+    if (need && (!workspace || !aligned16(workspace) || ws_bytes < need)) return DPB_EINVAL;
+    g.part = (float*)workspace;
     return launched(dpb::launch_attention(g, dtype == DPB_BF16, (hipStream_t)stream));
 }
 

@@ -1,5 +1,7 @@
 // Softmax attention: out = softmax(scale Q K^T) V over each query's visible keys,
 // and its log-sum-exp.
+#include <algorithm>
+
 #include "attention.hpp"
 
 namespace dpb {
@@ -8,23 +10,31 @@ namespace {
 constexpr int kWaves = 4;
 
 // The running state of 32 query rows (one a lane pair) over a pass of the keys:
-// the largest score so far, the sum of exp(scale (s - top)) on this lane's
-// keys, and the unscaled output, transposed (column = row of the query tile).
+// the largest score so far, the sum of 2^(c s - base) on this lane's keys (c =
+// scale log2 e, base = c top; a few thousand terms one behind the other, so what
+// each addition rounds off is kept in `lost`), and the unscaled output, transposed
+// (column = row of the query tile).
 template <typename T, int DP>
 struct Rows {
     static constexpr int kSteps = DP / 16, kParts = DP / 32;
     typename Operand<T>::type q[kSteps];
     f32x16 o[kParts];
-    float top, sum;
+    float top, base, sum, lost;
 
     __device__ __forceinline__ void clear()
     {
         top = -INFINITY;
-        sum = 0.f;
+        base = sum = lost = 0.f;
 #pragma unroll
         for (int i = 0; i < kParts; ++i)
 #pragma unroll
             for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
+    }
+
+    __device__ __forceinline__ float total() const
+    {
+        const float s = sum + lost;
+        return s + other_half(s);
     }
 
     // One tile of KT keys, the first of them key `first`; this lane's row sees the
@@ -55,10 +65,10 @@ struct Rows {
 #pragma unroll
             for (int r = 0; r < 16; ++r) big = fmaxf(big, s[m][r]);
         big = fmaxf(big, other_half(big));
-        const float now = fmaxf(top, big);
-        const float base = now == -INFINITY ? 0.f : now * c;   // nothing seen so far: every weight is 0
-        const float keep = __builtin_amdgcn_exp2f(top * c - base);
-        top = now;
+        const float was = top * c;
+        top = fmaxf(top, big);
+        base = top == -INFINITY ? 0.f : top * c;   // nothing seen so far: every weight is 0
+        const float keep = __builtin_amdgcn_exp2f(was - base);
         float add = 0.f;
 #pragma unroll
         for (int m = 0; m < KT / 32; ++m)
@@ -67,7 +77,9 @@ struct Rows {
                 s[m][r] = __builtin_amdgcn_exp2f(fmaf(s[m][r], c, -base));
                 add += s[m][r];
             }
-        sum = fmaf(sum, keep, add);
+        const float old = sum * keep, term = fmaf(lost, keep, add);
+        sum = old + term;
+        lost = term - (sum - old);
 #pragma unroll
         for (int i = 0; i < kParts; ++i)
 #pragma unroll
@@ -80,6 +92,15 @@ struct Rows {
         }
     }
 };
+
+// 1 / a row's sum of weights; 0 where no key was seen.
+__device__ __forceinline__ float inverse(float total) { return total > 0.f || total != total ? 1.f / total : 0.f; }
+
+// log sum exp from the sum of 2^(c s - base).
+__device__ __forceinline__ float log_sum(float base, float total)
+{
+    return total > 0.f || total != total ? (base + __builtin_amdgcn_logf(total)) * kLn2 : -INFINITY;
+}
 
 // One workgroup: 128 rows (tokens x the heads that share a key head) against the
 // keys they see.
@@ -117,9 +138,10 @@ __global__ __launch_bounds__(256, W) void attention_kernel(AttnArgs a)
     const char* vb = head_base(a.v, a.k_starts, b, sq.k0, hk);
     const float c = a.scale * kLog2e;
     const int n = (seen + KT - 1) / KT;
+    const typename Tl::Fill kfill(a.k.ts, a.dim, wave), vfill(a.v.ts, a.dim, wave);
     auto fill = [&](char* kt, char* vt, int t) {
-        Tl::fill(kt, kb + (int64_t)t * KT * a.k.ts, a.k.ts, sq.kn - t * KT, a.dim, wave);
-        Tl::fill(vt, vb + (int64_t)t * KT * a.v.ts, a.v.ts, sq.kn - t * KT, a.dim, wave);
+        kfill(kt, kb + (int64_t)t * KT * a.k.ts, sq.kn - t * KT, wave);
+        vfill(vt, vb + (int64_t)t * KT * a.v.ts, sq.kn - t * KT, wave);
     };
     auto step = [&](const char* kt, const char* vt, int t) {
         if (t * KT < most) st.template step<KT, kWaves>(kt, vt, t * KT, limit, (t + 1) * KT > least, c);
@@ -138,10 +160,9 @@ __global__ __launch_bounds__(256, W) void attention_kernel(AttnArgs a)
         step(k1, v1, t + 1);
     }
 
-    const float total = st.sum + other_half(st.sum);
+    const float total = st.total();
     if (token >= sq.qw) return;
-    const float inv = total > 0.f || total != total ? 1.f / total : 0.f;
-    const int64_t at = sq.q0 + token;
+    const float inv = inverse(total);
     char* out = head_base(a.o, a.q_starts, b, sq.q0, head) + (int64_t)token * a.o.ts;
     const int h = lane >> 5;
 #pragma unroll
@@ -153,7 +174,175 @@ __global__ __launch_bounds__(256, W) void attention_kernel(AttnArgs a)
                 store4<T>(out, e, st.o[i][4 * g] * inv, st.o[i][4 * g + 1] * inv, st.o[i][4 * g + 2] * inv,
                           st.o[i][4 * g + 3] * inv);
         }
-    if (h == 0) a.lse[at * a.heads + head] = inv == 0.f ? -INFINITY : fmaf(st.top, a.scale, __logf(total));
+    if (h == 0) a.lse[(sq.q0 + token) * a.heads + head] = log_sum(st.base, total);
+}
+
+// Few rows against many keys: one workgroup takes 32 rows and one of the call's
+// `splits` parts of the keys they see.  Its waves take tiles of 32 keys in turn,
+// each through buffers of its own, so that none waits for another before the
+// end; then the waves' states are joined, and, where there are several parts,
+// left for attention_join_kernel.
+template <typename T, int DP, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 1) void attention_split_kernel(AttnArgs a)
+{
+    typedef Tile<T, DP, 32, 1> Tl;
+    constexpr int kLoads = 2 * Tl::kLoads;   // loads of one tile's keys and values
+    __shared__ __align__(1024) char k0[WAVES][Tl::kBytes], v0[WAVES][Tl::kBytes], k1[WAVES][Tl::kBytes], v1[WAVES][Tl::kBytes];
+    __shared__ float bases[WAVES][32], totals[WAVES][32];
+    const int tiles = (a.q_len * a.group + 31) / 32;
+    int work = xcd_order(blockIdx.x, gridDim.x);
+    const int part = work % a.splits;
+    work /= a.splits;
+    const int bh = work / tiles, b = bh / a.kv_heads, hk = bh % a.kv_heads, tile = tiles - 1 - work % tiles;
+    const Sequence sq = sequence_of(a, b);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (tile * 32 >= sq.qw * a.group) return;
+
+    const int row = tile * 32 + (lane & 31);
+    const int token = row / a.group, head = hk * a.group + row % a.group;
+    const bool valid = token < sq.qn;
+    const int limit = visible_keys(a, sq, token);
+    const int last = min((tile * 32 + 31) / a.group, sq.qn - 1);
+    const int seen = last >= 0 ? visible_keys(a, sq, last) : 0;
+    const int least = __all(valid) ? __builtin_amdgcn_readfirstlane(limit) : 0;
+    const int all = (seen + 31) / 32;
+    const int begin = (int)((int64_t)all * part / a.splits), end = (int)((int64_t)all * (part + 1) / a.splits);
+
+    Rows<T, DP> st;
+    st.clear();
+    const char* qrow = head_base(a.q, a.q_starts, b, sq.q0, head) + (int64_t)token * a.q.ts;
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i) st.q[i] = global_operand<T>(qrow, i, a.dim, valid);
+    const char* kb = head_base(a.k, a.k_starts, b, sq.k0, hk);
+    const char* vb = head_base(a.v, a.k_starts, b, sq.k0, hk);
+    const float c = a.scale * kLog2e;
+    const typename Tl::Fill kfill(a.k.ts, a.dim, 0), vfill(a.v.ts, a.dim, 0);
+    auto fill = [&](char* kt, char* vt, int t) {
+        kfill(kt, kb + (int64_t)t * 32 * a.k.ts, sq.kn - t * 32, 0);
+        vfill(vt, vb + (int64_t)t * 32 * a.v.ts, sq.kn - t * 32, 0);
+    };
+    auto step = [&](const char* kt, const char* vt, int t) {
+        st.template step<32, 1>(kt, vt, t * 32, limit, (t + 1) * 32 > least, c);
+    };
+    int t = begin + wave;
+    if (t < end) fill(k0[wave], v0[wave], t);
+    while (t < end) {
+        // the buffer's last reads are done; the older of the two tiles in flight has landed
+        wait_lds();
+        if (t + WAVES < end) {
+            fill(k1[wave], v1[wave], t + WAVES);
+            wait_loads<kLoads>();
+        } else {
+            wait_loads<0>();
+        }
+        step(k0[wave], v0[wave], t);
+        t += WAVES;
+        if (t >= end) break;
+        wait_lds();
+        if (t + WAVES < end) {
+            fill(k0[wave], v0[wave], t + WAVES);
+            wait_loads<kLoads>();
+        } else {
+            wait_loads<0>();
+        }
+        step(k1[wave], v1[wave], t);
+        t += WAVES;
+    }
+
+    // the waves' states, a wave's output rows in its own key and value buffers
+    const float total = st.total();
+    const int h = lane >> 5;
+    static_assert(Tl::kBytes >= 32 * DP * 2, "an output row tile takes two buffers");
+    __syncthreads();
+    if (h == 0) {
+        bases[wave][lane] = total > 0.f || total != total ? st.base : -INFINITY;
+        totals[wave][lane] = total;
+    }
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int e = 32 * i + 8 * g + 4 * h;
+            char* to = e < DP / 2 ? k0[wave] : v0[wave];
+            *(f32x4*)(to + (((lane & 31) * (DP / 2) + e % (DP / 2)) << 2)) =
+                (f32x4){st.o[i][4 * g], st.o[i][4 * g + 1], st.o[i][4 * g + 2], st.o[i][4 * g + 3]};
+        }
+    __syncthreads();
+    const int rows = min(32, sq.qw * a.group - tile * 32);
+    for (int x = threadIdx.x; x < rows * (DP / 4); x += 64 * WAVES) {
+        const int r = x / (DP / 4), e = 4 * (x % (DP / 4));
+        float base = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) base = fmaxf(base, bases[w][r]);
+        const float zero_of = base == -INFINITY ? 0.f : base;
+        float sum = 0.f;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float f = __builtin_amdgcn_exp2f(bases[w][r] - zero_of);
+            sum = fmaf(totals[w][r], f, sum);
+            const f32x4 p = *(const f32x4*)((e < DP / 2 ? k0[w] : v0[w]) + ((r * (DP / 2) + e % (DP / 2)) << 2));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = fmaf(p[i], f, o[i]);
+        }
+        if (e >= a.dim) continue;
+        const int tok = (tile * 32 + r) / a.group, hd = hk * a.group + (tile * 32 + r) % a.group;
+        const int64_t at = (sq.q0 + tok) * a.heads + hd;
+        if (a.splits > 1) {
+            float* to = a.part + (at * a.splits + part) * (a.dim + 4);
+            *(f32x4*)(to + 4 + e) = o;
+            if (e == 0) {
+                to[0] = base;
+                to[1] = sum;
+            }
+        } else {
+            const float inv = inverse(sum);
+            store4<T>(head_base(a.o, a.q_starts, b, sq.q0, hd) + (int64_t)tok * a.o.ts, e, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+            if (e == 0) a.lse[at] = log_sum(zero_of, sum);
+        }
+    }
+}
+
+// Joins the parts of a split call, a wave per row: out = sum_p 2^(base_p - base)
+// o_p / sum_p 2^(base_p - base) sum_p, in the order of the parts.
+template <typename T>
+__global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t per = (int64_t)a.q_len * a.heads, id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int b = (int)(id / per), tok = (int)(id % per / a.heads), head = (int)(id % a.heads);
+    if (b >= a.batch) return;
+    const Sequence sq = sequence_of(a, b);
+    if (tok >= sq.qw) return;
+    const int64_t at = (sq.q0 + tok) * a.heads + head;
+    const float* from = a.part + at * a.splits * (a.dim + 4);
+    float base = -INFINITY;
+    for (int p = lane; p < a.splits; p += 64) base = fmaxf(base, from[(int64_t)p * (a.dim + 4)]);
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) base = fmaxf(base, __shfl_xor(base, x, 64));
+    const float zero_of = base == -INFINITY ? 0.f : base;
+    // half a wave takes the even parts, the other the odd ones; four elements a lane
+    const int half = lane >> 5, e = 4 * (lane & 31);
+    float sum = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    if (e < a.dim) {
+#pragma unroll 4
+        for (int p = half; p < a.splits; p += 2) {
+            const float* x = from + (int64_t)p * (a.dim + 4);
+            const float f = __builtin_amdgcn_exp2f(x[0] - zero_of);
+            const f32x4 v = *(const f32x4*)(x + 4 + e);
+            sum = fmaf(x[1], f, sum);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = fmaf(v[i], f, o[i]);
+        }
+    }
+    sum += other_half(sum);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] += other_half(o[i]);
+    if (half || e >= a.dim) return;
+    const float inv = inverse(sum);
+    store4<T>(head_base(a.o, a.q_starts, b, sq.q0, head) + (int64_t)tok * a.o.ts, e, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+    if (e == 0) a.lse[at] = log_sum(zero_of, sum);
 }
 
 template <typename T, int DP, int KT, int W>
@@ -164,10 +353,41 @@ hipError_t launch_tiles(const AttnArgs& a, hipStream_t stream)
     return hipGetLastError();
 }
 
+template <typename T, int DP, int WAVES>
+hipError_t launch_split(const AttnArgs& a, hipStream_t stream)
+{
+    const int64_t rows = (int64_t)a.q_len * a.group, tiles = (rows + 31) / 32;
+    attention_split_kernel<T, DP, WAVES><<<dim3((unsigned)(tiles * a.batch * a.kv_heads * a.splits)), 64 * WAVES, 0, stream>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.splits == 1) return e;
+    const int64_t all = (int64_t)a.batch * a.q_len * a.heads;
+    attention_join_kernel<T><<<dim3((unsigned)((all + 3) / 4)), 256, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
 }  // namespace
+
+int attention_splits(int batch, int q_len, int k_len, int heads, int kv_heads)
+{
+    const int64_t rows = (int64_t)q_len * (heads / kv_heads), cus = device_cus();
+    const int64_t pairs = (int64_t)batch * kv_heads;
+    if (rows > 32 && pairs * ((rows + 127) / 128) >= cus / 2) return 0;
+    // enough workgroups for every compute unit to be given several, of at least 256 keys each
+    const int64_t want = (8 * cus + pairs * ((rows + 31) / 32) - 1) / (pairs * ((rows + 31) / 32));
+    return (int)std::max<int64_t>(1, std::min<int64_t>(want, ((int64_t)k_len + 255) / 256));
+}
+
+size_t attention_part_floats(int64_t q_rows, int heads, int dim, int splits)
+{
+    return splits > 1 ? (size_t)q_rows * heads * splits * (dim + 4) : 0;
+}
 
 hipError_t launch_attention(const AttnArgs& a, bool bf16, hipStream_t stream)
 {
+    if (a.splits) {
+        if (bf16) return a.dim <= 64 ? launch_split<__bf16, 64, 4>(a, stream) : launch_split<__bf16, 128, 4>(a, stream);
+        return a.dim <= 64 ? launch_split<float, 64, 4>(a, stream) : launch_split<float, 128, 2>(a, stream);
+    }
     if (bf16) return a.dim <= 64 ? launch_tiles<__bf16, 64, 64, 2>(a, stream) : launch_tiles<__bf16, 128, 64, 2>(a, stream);
     return a.dim <= 64 ? launch_tiles<float, 64, 32, 2>(a, stream) : launch_tiles<float, 128, 32, 1>(a, stream);
 }

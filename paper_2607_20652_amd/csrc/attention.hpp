@@ -37,22 +37,24 @@ struct AttnArgs {
     float* lse;                      // [query rows, heads]
     float* row_lse2;                 // backward scratch [heads][query rows]: lse * log2(e)
     float* row_delta;                // and sum_d go * o
-    float* part;                     // forward scratch of a split call (see attention.hip)
+    float* part;                     // scratch of a split call: [query rows][heads][splits][4 + dim]
+                                     // (base, sum, -, -, output)
     const int32_t *q_lens, *k_lens;      // padded: lengths, or null
     const int32_t *q_starts, *k_starts;  // packed: starts, or null
     int64_t q_rows, k_rows;          // rows of q and k in all
     int batch, q_len, k_len;         // sequences; padded lengths, or the longest packed ones
     int heads, kv_heads, group, dim;
     int causal;
-    int splits;
+    int splits;                      // parts the keys are split into
     float scale;
 };
 
 hipError_t launch_attention(const AttnArgs& a, bool bf16, hipStream_t stream);
 hipError_t launch_attention_bwd(const AttnArgs& a, bool bf16, hipStream_t stream);
-// Parts that the keys of a call are split into, and the scratch floats that takes.
+// Parts that the keys of a forward call are split into (0: whole, by tiles of 128
+// rows), and the scratch floats that takes.
 int attention_splits(int batch, int q_len, int k_len, int heads, int kv_heads);
-size_t attention_part_floats(int batch, int q_len, int heads, int dim, int splits);
+size_t attention_part_floats(int64_t q_rows, int heads, int dim, int splits);
 
 // Where sequence b lies: rows before it, its lengths, and the query (key) rows
 // of the outputs that belong to it.  Packed starts are clamped to the tensor, so
@@ -176,8 +178,9 @@ __device__ __forceinline__ void store4(char* row, int e, float a, float b, float
 // rows for a transposed read, then meets every bank once.  WAVES waves fill it
 // straight from global memory (no registers), 1 KB an instruction; the place a
 // lane writes is fixed, so the lane picks the chunk that belongs there.  Rows
-// past the sequence and chunks past dim are asked for out of the buffer's range
-// and arrive as zeros.
+// past the sequence and chunks past dim lie out of the buffer's range and arrive
+// as zeros (of a tensor whose token stride is 0, rows past the sequence arrive as
+// its one row; either way no result depends on them).
 template <typename T, int DP, int R, int WAVES = 4>
 struct Tile {
     static constexpr int kRowBytes = DP * (int)sizeof(T);
@@ -194,24 +197,35 @@ struct Tile {
         else return 2 * (r & 7) + ((r >> 3) & 1);
     }
 
-    // Enqueues the tile's loads: rows [0, left) from `first`, `stride` bytes apart.
-    // (Whoever reads the tile waits for them: fill_wait, and a barrier if other
-    // waves filled parts of it.)
-    __device__ static __forceinline__ void fill(char* lds, const char* first, int64_t stride, int left, int dim, int wave)
-    {
-        const int lane = threadIdx.x & 63;
-        const int n = min(left, R);
-        const uint32_t bytes = n > 0 ? (uint32_t)((n - 1) * stride + dim * (int)sizeof(T)) : 0u;
-        const __amdgpu_buffer_rsrc_t buf =
-            __builtin_amdgcn_make_buffer_rsrc((void*)first, 0, (int)bytes, 0x00027000);
+    // A wave's loads of tiles from one tensor: where each lane's chunks lie from a
+    // tile's first row (the same for every tile).
+    struct Fill {
+        uint32_t off[kLoads];
+        int stride, row_bytes;
+
+        __device__ __forceinline__ Fill(int64_t ts, int dim, int wave) : stride((int)ts), row_bytes(dim * (int)sizeof(T))
+        {
+            const int lane = threadIdx.x & 63;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int at = (i * WAVES + wave) * kLoadRows;
-            const int r = at + lane / kChunks, c = (lane % kChunks) ^ turn(r);
-            const uint32_t off = r < n && c * 16 < dim * (int)sizeof(T) ? (uint32_t)r * (uint32_t)stride + c * 16 : 0xFFFFFFF0u;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lds_void*)(lds + at * kRowBytes), 16, (int)off, 0, 0, 0);
+            for (int i = 0; i < kLoads; ++i) {
+                const int r = (i * WAVES + wave) * kLoadRows + lane / kChunks, c = (lane % kChunks) ^ turn(r);
+                off[i] = c * 16 < row_bytes ? (uint32_t)r * (uint32_t)stride + c * 16 : 0xFFFFFFF0u;
+            }
         }
-    }
+
+        // Enqueues the loads of the tile whose first row is `first`, with `left` rows to the
+        // end.  (Whoever reads the tile waits for them: wait_loads, and a barrier if
+        // other waves filled parts of it.)
+        __device__ __forceinline__ void operator()(char* lds, const char* first, int left, int wave) const
+        {
+            const int bytes = left > 0 ? (min(left, R) - 1) * stride + row_bytes : 0;
+            const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc((void*)first, 0, bytes, 0x00027000);
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lds_void*)(lds + (i * WAVES + wave) * 1024), 16,
+                                                         (int)off[i], 0, 0, 0);
+        }
+    };
 
     // Operand: row `row + lane % 32`, values 16s + 8h + {0..7}.
     __device__ static __forceinline__ Op rows(const char* lds, int row, int s)
@@ -253,7 +267,16 @@ struct Tile {
     }
 };
 
-// Waits for this wave's loads into LDS.
-__device__ __forceinline__ void fill_wait() { __builtin_amdgcn_s_waitcnt(0x0F70); }
+// Waits for this wave's loads into LDS, all but the N issued last.
+template <int N>
+__device__ __forceinline__ void wait_loads()
+{
+    static_assert(N < 64, "six bits count the loads in flight");
+    __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void fill_wait() { wait_loads<0>(); }
+
+// Waits for this wave's reads of LDS (before a load is sent into what they read).
+__device__ __forceinline__ void wait_lds() { __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 }  // namespace dpb

@@ -83,9 +83,10 @@ __global__ __launch_bounds__(256, W) void attention_dq_kernel(AttnArgs a)
     const char* vb = head_base(a.v, a.k_starts, b, sq.k0, hk);
     const float c = a.scale * kLog2e;
     const int n = (seen + KT - 1) / KT;
+    const typename Tl::Fill kfill(a.k.ts, a.dim, wave), vfill(a.v.ts, a.dim, wave);
     auto fill = [&](char* kt, char* vt, int t) {
-        Tl::fill(kt, kb + (int64_t)t * KT * a.k.ts, a.k.ts, sq.kn - t * KT, a.dim, wave);
-        Tl::fill(vt, vb + (int64_t)t * KT * a.v.ts, a.v.ts, sq.kn - t * KT, a.dim, wave);
+        kfill(kt, kb + (int64_t)t * KT * a.k.ts, sq.kn - t * KT, wave);
+        vfill(vt, vb + (int64_t)t * KT * a.v.ts, sq.kn - t * KT, wave);
     };
     auto step = [&](const char* kt, const char* vt, int t) {
         if (t * KT >= most) return;
@@ -176,7 +177,8 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
         if constexpr (!kValuesInLds) v[i] = global_operand<T>(vrow, i, a.dim, valid);
     }
     if constexpr (kValuesInLds)
-        Vl::fill(vt, head_base(a.v, a.k_starts, b, sq.k0, hk) + (int64_t)tile * 128 * a.v.ts, a.v.ts, sq.kn - tile * 128, a.dim, wave);
+        typename Vl::Fill(a.v.ts, a.dim, wave)(vt, head_base(a.v, a.k_starts, b, sq.k0, hk) + (int64_t)tile * 128 * a.v.ts,
+                                               sq.kn - tile * 128, wave);
     f32x16 dk[kParts], dv[kParts];
 #pragma unroll
     for (int i = 0; i < kParts; ++i) {
@@ -192,10 +194,11 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
     const int per_head = from < sq.qn ? (sq.qn - from + QT - 1) / QT : 0;
     const int n = per_head * a.group;
     const float c = a.scale * kLog2e;
+    const typename Tl::Fill qfill(a.q.ts, a.dim, wave), gfill(a.go.ts, a.dim, wave);
     auto fill = [&](char* qt, char* gt, float* lt, float* dt, int t) {
         const int head = hk * a.group + t / per_head, tok = from + (t % per_head) * QT, left = sq.qn - tok;
-        Tl::fill(qt, head_base(a.q, a.q_starts, b, sq.q0, head) + (int64_t)tok * a.q.ts, a.q.ts, left, a.dim, wave);
-        Tl::fill(gt, head_base(a.go, a.q_starts, b, sq.q0, head) + (int64_t)tok * a.go.ts, a.go.ts, left, a.dim, wave);
+        qfill(qt, head_base(a.q, a.q_starts, b, sq.q0, head) + (int64_t)tok * a.q.ts, left, wave);
+        gfill(gt, head_base(a.go, a.q_starts, b, sq.q0, head) + (int64_t)tok * a.go.ts, left, wave);
         if (wave < 2) {
             const float* src = (wave ? a.row_delta : a.row_lse2) + head * a.q_rows + sq.q0 + tok;
             const __amdgpu_buffer_rsrc_t buf =
@@ -207,7 +210,7 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
         const int tok = from + (t % per_head) * QT;
         const int key_last = tile * 128 + wave * 32 + 31;
         if (a.causal && tok + QT - 1 + behind < key_last - 31) return;   // no query of the tile sees this wave's keys
-        const bool edge = a.causal && key_last > tok + behind;
+        const bool edge = (a.causal && key_last > tok + behind) || tok + QT > sq.qn;
 #pragma unroll
         for (int m = 0; m < QT / 32; ++m) {
             f32x16 s, dp;
@@ -221,7 +224,8 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
                 if constexpr (kValuesInLds) dp = mma(Tl::rows(gt, 32 * m, i), Vl::rows(vt, 32 * wave, i), dp);
                 else dp = mma(Tl::rows(gt, 32 * m, i), v[i], dp);
             }
-            const int need = first_token - tok - 32 * m - 4 * h;   // rows from here on see the key
+            // rows from `need` on see the key, and those before `left` are the sequence's
+            const int need = first_token - tok - 32 * m - 4 * h, left = sq.qn - tok - 32 * m - 4 * h;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const f32x4 l = *(const f32x4*)(lt + 32 * m + 8 * g + 4 * h), d = *(const f32x4*)(dt + 32 * m + 8 * g + 4 * h);
@@ -229,7 +233,7 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
                 for (int j = 0; j < 4; ++j) {
                     const int r = 4 * g + j;
                     float p = __builtin_amdgcn_exp2f(fmaf(s[r], c, -l[j]));
-                    if (edge) p = 8 * g + j >= need ? p : 0.f;
+                    if (edge) p = 8 * g + j >= need && 8 * g + j < left ? p : 0.f;
                     s[r] = p;
                     dp[r] = p * (dp[r] - d[j]);
                 }
