@@ -23,8 +23,8 @@ struct Rows {
 
     __device__ __forceinline__ void clear()
     {
-        top = -INFINITY;
-        base = sum = lost = 0.f;
+        top = base = -INFINITY;
+        sum = lost = 0.f;
 #pragma unroll
         for (int i = 0; i < kParts; ++i)
 #pragma unroll
@@ -65,16 +65,17 @@ struct Rows {
 #pragma unroll
             for (int r = 0; r < 16; ++r) big = fmaxf(big, s[m][r]);
         big = fmaxf(big, other_half(big));
-        const float was = top * c;
+        const float was = base;
         top = fmaxf(top, big);
-        base = top == -INFINITY ? 0.f : top * c;   // nothing seen so far: every weight is 0
-        const float keep = __builtin_amdgcn_exp2f(was - base);
+        base = __fmul_rn(top, c);   // rounded once: the same top gives the same base, and sums are kept exactly
+        const float from = base == -INFINITY ? 0.f : base;   // nothing seen so far: every weight is 0
+        const float keep = __builtin_amdgcn_exp2f(was - from);
         float add = 0.f;
 #pragma unroll
         for (int m = 0; m < KT / 32; ++m)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                s[m][r] = __builtin_amdgcn_exp2f(fmaf(s[m][r], c, -base));
+                s[m][r] = __builtin_amdgcn_exp2f(fmaf(s[m][r], c, -from));
                 add += s[m][r];
             }
         const float old = sum * keep, term = fmaf(lost, keep, add);
@@ -255,7 +256,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void attention_split_kernel(AttnArgs
     static_assert(Tl::kBytes >= 32 * DP * 2, "an output row tile takes two buffers");
     __syncthreads();
     if (h == 0) {
-        bases[wave][lane] = total > 0.f || total != total ? st.base : -INFINITY;
+        bases[wave][lane] = st.base;
         totals[wave][lane] = total;
     }
 #pragma unroll
