@@ -9,21 +9,25 @@ namespace {
 
 constexpr int kWaves = 4;
 
+// Weights are 2^(c s - base).  The base follows the largest score only where that
+// is this far above it: up to 2^8 a weight is as precise as one below 1, in bf16
+// and fp32, and the output need not be rescaled for every new maximum.
+constexpr float kHeadroom = 8.f;
+
 // The running state of 32 query rows (one a lane pair) over a pass of the keys:
-// the largest score so far, the sum of 2^(c s - base) on this lane's keys (c =
-// scale log2 e, base = c top; a few thousand terms one behind the other, so what
-// each addition rounds off is kept in `lost`), and the unscaled output, transposed
-// (column = row of the query tile).
+// the base, the sum of 2^(c s - base) on this lane's keys (c = scale log2 e; a few
+// thousand terms one behind the other, so what each addition rounds off is kept in
+// `lost`), and the unscaled output, transposed (column = row of the query tile).
 template <typename T, int DP>
 struct Rows {
     static constexpr int kSteps = DP / 16, kParts = DP / 32;
     typename Operand<T>::type q[kSteps];
     f32x16 o[kParts];
-    float top, base, sum, lost;
+    float base, sum, lost;
 
     __device__ __forceinline__ void clear()
     {
-        top = base = -INFINITY;
+        base = -INFINITY;
         sum = lost = 0.f;
 #pragma unroll
         for (int i = 0; i < kParts; ++i)
@@ -65,11 +69,19 @@ struct Rows {
 #pragma unroll
             for (int r = 0; r < 16; ++r) big = fmaxf(big, s[m][r]);
         big = fmaxf(big, other_half(big));
-        const float was = base;
-        top = fmaxf(top, big);
-        base = __fmul_rn(top, c);   // rounded once: the same top gives the same base, and sums are kept exactly
+        big *= c;
+        if (__any(big > base + kHeadroom)) {
+            const float was = base;
+            base = fmaxf(base, big);
+            const float keep = __builtin_amdgcn_exp2f(was - (base == -INFINITY ? 0.f : base));
+            sum *= keep;
+            lost *= keep;
+#pragma unroll
+            for (int i = 0; i < kParts; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[i][r] *= keep;
+        }
         const float from = base == -INFINITY ? 0.f : base;   // nothing seen so far: every weight is 0
-        const float keep = __builtin_amdgcn_exp2f(was - from);
         float add = 0.f;
 #pragma unroll
         for (int m = 0; m < KT / 32; ++m)
@@ -78,13 +90,9 @@ struct Rows {
                 s[m][r] = __builtin_amdgcn_exp2f(fmaf(s[m][r], c, -from));
                 add += s[m][r];
             }
-        const float old = sum * keep, term = fmaf(lost, keep, add);
+        const float old = sum, term = lost + add;
         sum = old + term;
         lost = term - (sum - old);
-#pragma unroll
-        for (int i = 0; i < kParts; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[i][r] *= keep;
 #pragma unroll
         for (int j = 0; j < KT / 16; ++j) {
             const typename Operand<T>::type p = as_operand<T>(s[j / 2], j & 1);
@@ -111,9 +119,8 @@ __global__ __launch_bounds__(256, W) void attention_kernel(AttnArgs a)
     typedef Tile<T, DP, KT, kWaves> Tl;
     __shared__ __align__(1024) char k0[Tl::kBytes], v0[Tl::kBytes], k1[Tl::kBytes], v1[Tl::kBytes];
     const int tiles = (a.q_len * a.group + 127) / 128;
-    const int work = xcd_order(blockIdx.x, gridDim.x);
-    const int bh = work / tiles, b = bh / a.kv_heads, hk = bh % a.kv_heads;
-    const int tile = tiles - 1 - work % tiles;   // of a causal sequence the longest first
+    const int pairs = a.batch * a.kv_heads, bh = (int)blockIdx.x % pairs, b = bh / a.kv_heads, hk = bh % a.kv_heads;
+    const int tile = tiles - 1 - (int)blockIdx.x / pairs;   // of causal sequences the longest rows first
     const Sequence sq = sequence_of(a, b);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (tile * 128 >= sq.qw * a.group) return;
@@ -191,10 +198,8 @@ __global__ __launch_bounds__(64 * WAVES, 1) void attention_split_kernel(AttnArgs
     __shared__ __align__(1024) char k0[WAVES][Tl::kBytes], v0[WAVES][Tl::kBytes], k1[WAVES][Tl::kBytes], v1[WAVES][Tl::kBytes];
     __shared__ float bases[WAVES][32], totals[WAVES][32];
     const int tiles = (a.q_len * a.group + 31) / 32;
-    int work = xcd_order(blockIdx.x, gridDim.x);
-    const int part = work % a.splits;
-    work /= a.splits;
-    const int bh = work / tiles, b = bh / a.kv_heads, hk = bh % a.kv_heads, tile = tiles - 1 - work % tiles;
+    const int pairs = a.batch * a.kv_heads, bh = (int)blockIdx.x % pairs, b = bh / a.kv_heads, hk = bh % a.kv_heads;
+    const int part = (int)blockIdx.x / pairs % a.splits, tile = tiles - 1 - (int)blockIdx.x / pairs / a.splits;
     const Sequence sq = sequence_of(a, b);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (tile * 32 >= sq.qw * a.group) return;

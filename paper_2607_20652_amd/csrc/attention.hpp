@@ -102,14 +102,10 @@ __device__ __forceinline__ int visible_keys(const AttnArgs& a, const Sequence& s
     return a.causal ? min(max(token + 1 + s.kn - s.qn, 0), s.kn) : s.kn;
 }
 
-// Workgroup ids go round the eight XCDs in turn; this order gives every XCD a
-// contiguous run of the work, so that the workgroups that read one head's keys
-// share an L2.
-__device__ __forceinline__ int xcd_order(int id, int total)
-{
-    const int x = id & 7, q = total >> 3, r = total & 7;
-    return x * q + min(x, r) + (id >> 3);
-}
+// Workgroups are numbered with the heads innermost and the longest work first: ids
+// go round the eight XCDs in turn, so the workgroups of one head meet in one L2
+// (for a power of two of heads), every compute unit gets long and short work
+// alike, and the short work fills the end.
 
 // ---- elements
 
@@ -174,7 +170,7 @@ __device__ __forceinline__ void store4(char* row, int e, float a, float b, float
 
 // A tile of R rows of one head in LDS, DP values wide (DP: dim rounded up to 64
 // or 128), rows behind each other in 16-byte chunks.  Chunk c of row r lies at
-// place c ^ turn(r): reading one chunk of sixteen rows, or two chunks of four
+// place c ^ turn(r): reading one chunk of sixteen rows, or four chunks of four
 // rows for a transposed read, then meets every bank once.  WAVES waves fill it
 // straight from global memory (no registers), 1 KB an instruction; the place a
 // lane writes is fixed, so the lane picks the chunk that belongs there.  Rows
@@ -193,8 +189,8 @@ struct Tile {
 
     __device__ static __forceinline__ int turn(int r)
     {
-        if constexpr (kChunks == 8) return 2 * ((r >> 1) & 3) + ((r >> 3) & 1);
-        else return 2 * (r & 7) + ((r >> 3) & 1);
+        if constexpr (kChunks == 8) return 4 * ((r >> 1) & 1) + ((r >> 2) & 3);   // two rows meet all banks
+        else return 4 * (r & 3) + ((r >> 2) & 3);
     }
 
     // A wave's loads of tiles from one tensor: where each lane's chunks lie from a

@@ -39,9 +39,8 @@ __global__ __launch_bounds__(256, W) void attention_dq_kernel(AttnArgs a)
     constexpr int kSteps = DP / 16, kParts = DP / 32;
     __shared__ __align__(1024) char k0[Tl::kBytes], v0[Tl::kBytes], k1[Tl::kBytes], v1[Tl::kBytes];
     const int tiles = (a.q_len * a.group + 127) / 128;
-    const int work = xcd_order(blockIdx.x, gridDim.x);
-    const int bh = work / tiles, b = bh / a.kv_heads, hk = bh % a.kv_heads;
-    const int tile = tiles - 1 - work % tiles;
+    const int pairs = a.batch * a.kv_heads, bh = (int)blockIdx.x % pairs, b = bh / a.kv_heads, hk = bh % a.kv_heads;
+    const int tile = tiles - 1 - (int)blockIdx.x / pairs;
     const Sequence sq = sequence_of(a, b);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     if (tile * 128 >= sq.qw * a.group) return;
@@ -158,10 +157,8 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
     constexpr bool kValuesInLds = DP * sizeof(T) == 512;
     typedef Tile<T, DP, 128, kWaves> Vl;
     __shared__ __align__(1024) char vt[kValuesInLds ? Vl::kBytes : 16];
-    const int tiles = (a.k_len + 127) / 128;
-    const int work = xcd_order(blockIdx.x, gridDim.x);
-    const int bh = work / tiles, b = bh / a.kv_heads, hk = bh % a.kv_heads;
-    const int tile = work % tiles;   // of a causal sequence the keys that most queries see first
+    const int pairs = a.batch * a.kv_heads, bh = (int)blockIdx.x % pairs, b = bh / a.kv_heads, hk = bh % a.kv_heads;
+    const int tile = (int)blockIdx.x / pairs;   // of a causal sequence the keys that most queries see first
     const Sequence sq = sequence_of(a, b);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     if (tile * 128 >= sq.kw) return;
