@@ -24,12 +24,10 @@ HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # keep the compiler from forming packed fp32 instructions
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+    # matrix-core results in ordinary VGPRs (no accumulator-register copies)
+    "-mllvm", "-amdgpu-mfma-vgpr-form",
     "-Wall", "-Wno-unused-result",
 ]
-# matrix-core results in ordinary VGPRs (no accumulator-register copies); not where
-# a kernel's sums outgrow the 256 of them
-VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
-ACCUMULATORS = {"attention_bwd.hip"}
 _NOISE = ("is not a recognized feature for this target", "argument unused during compilation")
 
 
@@ -43,7 +41,7 @@ def build(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     os.makedirs(OBJ_DIR, exist_ok=True)
     objs = [os.path.join(OBJ_DIR, os.path.splitext(s)[0] + ".o") for s in SOURCES]
-    cmds = [[hipcc, *HIPCC_FLAGS, *([] if s in ACCUMULATORS else VGPR_FORM), "-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(SOURCES, objs)]
+    cmds = [[hipcc, *HIPCC_FLAGS, "-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(SOURCES, objs)]
     jobs = max(1, min(len(cmds), int(os.environ.get("MAX_JOBS", os.cpu_count() or 1))))
     with ThreadPoolExecutor(jobs) as ex:
         results = list(ex.map(_run, cmds))

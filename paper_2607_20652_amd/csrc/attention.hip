@@ -44,17 +44,17 @@ struct Rows {
     // One tile of KT keys, the first of them key `first`; this lane's row sees the
     // keys below `limit`, and every row of the wave sees all of the tile unless `edge`.
     template <int KT, int W>
-    __device__ __forceinline__ void step(const char* kt, const char* vt, int first, int limit, bool edge, float c)
+    __device__ __forceinline__ void step(typename Tile<T, DP, KT, W>::Reader& rd, const char* kt, const char* vt, int first, int limit, bool edge, float c)
     {
-        typedef Tile<T, DP, KT, W> Tl;
         const int h = (threadIdx.x & 63) >> 5;
+        rd.fresh();
         f32x16 s[KT / 32];
 #pragma unroll
         for (int m = 0; m < KT / 32; ++m) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[m][r] = 0.f;
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) s[m] = mma(Tl::rows(kt, 32 * m, i), q[i], s[m]);
+            for (int i = 0; i < kSteps; ++i) s[m] = mma(rd.rows(kt, 32 * m, i), q[i], s[m]);
         }
         if (edge) {
             const int n = limit - first - 4 * h;
@@ -97,7 +97,7 @@ struct Rows {
         for (int j = 0; j < KT / 16; ++j) {
             const typename Operand<T>::type p = as_operand<T>(s[j / 2], j & 1);
 #pragma unroll
-            for (int i = 0; i < kParts; ++i) o[i] = mma(Tl::columns(vt, j, i), p, o[i]);
+            for (int i = 0; i < kParts; ++i) o[i] = mma(rd.columns(vt, j, i), p, o[i]);
         }
     }
 };
@@ -138,6 +138,7 @@ __global__ __launch_bounds__(256, W) void attention_kernel(AttnArgs a)
 
     Rows<T, DP> st;
     st.clear();
+    typename Tl::Reader rd;
     const char* qrow = head_base(a.q, a.q_starts, b, sq.q0, head) + (int64_t)token * a.q.ts;
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i) st.q[i] = global_operand<T>(qrow, i, a.dim, valid);
@@ -152,7 +153,7 @@ __global__ __launch_bounds__(256, W) void attention_kernel(AttnArgs a)
         vfill(vt, vb + (int64_t)t * KT * a.v.ts, sq.kn - t * KT, wave);
     };
     auto step = [&](const char* kt, const char* vt, int t) {
-        if (t * KT < most) st.template step<KT, kWaves>(kt, vt, t * KT, limit, (t + 1) * KT > least, c);
+        if (t * KT < most) st.template step<KT, kWaves>(rd, kt, vt, t * KT, limit, (t + 1) * KT > least, c);
     };
     if (n > 0) fill(k0, v0, 0);
     for (int t = 0; t < n; t += 2) {
@@ -216,6 +217,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void attention_split_kernel(AttnArgs
 
     Rows<T, DP> st;
     st.clear();
+    typename Tl::Reader rd;
     const char* qrow = head_base(a.q, a.q_starts, b, sq.q0, head) + (int64_t)token * a.q.ts;
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i) st.q[i] = global_operand<T>(qrow, i, a.dim, valid);
@@ -228,7 +230,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void attention_split_kernel(AttnArgs
         vfill(vt, vb + (int64_t)t * 32 * a.v.ts, sq.kn - t * 32, 0);
     };
     auto step = [&](const char* kt, const char* vt, int t) {
-        st.template step<32, 1>(kt, vt, t * 32, limit, (t + 1) * 32 > least, c);
+        st.template step<32, 1>(rd, kt, vt, t * 32, limit, (t + 1) * 32 > least, c);
     };
     int t = begin + wave;
     if (t < end) fill(k0[wave], v0[wave], t);

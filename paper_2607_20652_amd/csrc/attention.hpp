@@ -187,7 +187,8 @@ struct Tile {
     static_assert(kLoads * WAVES * 1024 == kBytes, "a tile is a whole number of loads");
     typedef typename Operand<T>::type Op;
 
-    __device__ static __forceinline__ int turn(int r)
+    // (turn(a + b) = turn(a) ^ turn(b) for a and b that share no bit, as above)
+    __device__ static constexpr int turn(int r)
     {
         if constexpr (kChunks == 8) return 4 * ((r >> 1) & 1) + ((r >> 2) & 3);   // two rows meet all banks
         else return 4 * (r & 3) + ((r >> 2) & 3);
@@ -223,44 +224,61 @@ struct Tile {
         }
     };
 
-    // Operand: row `row + lane % 32`, values 16s + 8h + {0..7}.
-    __device__ static __forceinline__ Op rows(const char* lds, int row, int s)
-    {
-        const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
-        const char* p = lds + row * kRowBytes + r * kRowBytes;
-        if constexpr (sizeof(T) == 2) {
-            return *(const bf16x8*)(p + (((2 * s + h) ^ turn(r)) << 4));
-        } else {
-            const int c = 4 * s + 2 * h;
-            const f32x4 a = *(const f32x4*)(p + ((c ^ turn(r)) << 4)), b = *(const f32x4*)(p + (((c + 1) ^ turn(r)) << 4));
-            return (Op){a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-        }
-    }
+    // Where this lane reads: the places of its first row operand and of its first
+    // transposed one; every other place differs by an exclusive or with a constant and
+    // a constant offset.  fresh() has the compiler form those anew, one instruction each,
+    // where it would keep all of them in registers through a kernel's loop.
+    struct Reader {
+        uint32_t row, col;
 
-    // Operand of the transposed tile: value `32 * dt + lane % 32`, rows
-    // 16s + 4h + {0..3} and 16s + 8 + 4h + {0..3}.
-    __device__ static __forceinline__ Op columns(const char* lds, int s, int dt)
-    {
-        const int lane = threadIdx.x & 63, h = lane >> 5;
-        if constexpr (sizeof(T) == 2) {
-            // a group of sixteen lanes reads four rows of sixteen values and gets them transposed
-            const int i = lane & 15, r = 4 * h + (i >> 2), c = 4 * dt + 2 * ((lane >> 4) & 1) + ((i >> 1) & 1);
-            const char* p = lds + s * 16 * kRowBytes + r * kRowBytes + 8 * (i & 1);
-            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + ((c ^ turn(r)) << 4)));
-            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (lds_s16x4*)(p + 8 * kRowBytes + ((c ^ turn(r + 8)) << 4)));
-            return __builtin_bit_cast(Op, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
-        } else {
-            const int c = 8 * dt + ((lane & 31) >> 2);
-            Op v;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int r = 4 * h + 8 * (j >> 2) + (j & 3);
-                v[j] = *(const float*)(lds + (s * 16 + r) * kRowBytes + ((c ^ turn(r)) << 4) + 4 * (lane & 3));
+        __device__ __forceinline__ Reader()
+        {
+            const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5, i = lane & 15;
+            if constexpr (sizeof(T) == 2) {
+                row = r * kRowBytes + ((h ^ turn(r)) << 4);
+                // a group of sixteen lanes reads four rows of sixteen values and gets them transposed
+                const int q = 4 * h + (i >> 2), c = 2 * ((lane >> 4) & 1) + ((i >> 1) & 1);
+                col = q * kRowBytes + ((c ^ turn(q)) << 4) + 8 * (i & 1);
+            } else {
+                row = r * kRowBytes + (((2 * h) ^ turn(r)) << 4);
+                col = 4 * h * kRowBytes + (((r >> 2) ^ turn(4 * h)) << 4) + 4 * (r & 3);
             }
-            return v;
         }
-    }
+        __device__ __forceinline__ void fresh() { __asm__ volatile("" : "+v"(row), "+v"(col)); }
+
+        // Operand: row `first + lane % 32`, values 16s + 8h + {0..7}.
+        __device__ __forceinline__ Op rows(const char* lds, int first, int s) const
+        {
+            const char* p = lds + first * kRowBytes;
+            if constexpr (sizeof(T) == 2) {
+                return *(const bf16x8*)(p + (row ^ (s << 5)));
+            } else {
+                const f32x4 a = *(const f32x4*)(p + (row ^ (s << 6))), b = *(const f32x4*)(p + (row ^ (s << 6 | 16)));
+                return (Op){a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+            }
+        }
+
+        // Operand of the transposed tile: value `32 * dt + lane % 32`, rows
+        // 16s + 4h + {0..3} and 16s + 8 + 4h + {0..3}.
+        __device__ __forceinline__ Op columns(const char* lds, int s, int dt) const
+        {
+            const char* p = lds + s * 16 * kRowBytes;
+            if constexpr (sizeof(T) == 2) {
+                const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (col ^ (dt << 6))));
+                const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (lds_s16x4*)(p + 8 * kRowBytes + (col ^ (dt << 6 | turn(8) << 4))));
+                return __builtin_bit_cast(Op, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+            } else {
+                Op v;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int r = 8 * (j >> 2) + (j & 3);
+                    v[j] = *(const float*)(p + r * kRowBytes + (col ^ (dt << 7) ^ (turn(r) << 4)));
+                }
+                return v;
+            }
+        }
+    };
 };
 
 // Waits for this wave's loads into LDS, all but the N issued last.

@@ -23,10 +23,10 @@ __device__ __forceinline__ void zero(f32x16& c)
 
 // fp32 operands take twice the registers: there the products' LDS reads stay in
 // their own phase, or the compiler, which issues them early, runs out of registers.
-template <typename T>
+template <bool ON>
 __device__ __forceinline__ void phase()
 {
-    if constexpr (sizeof(T) == 4) __builtin_amdgcn_sched_barrier(0);
+    if constexpr (ON) __builtin_amdgcn_sched_barrier(0);
 }
 
 // dQ of 128 rows (tokens x the heads that share a key head); also leaves each
@@ -81,6 +81,7 @@ __global__ __launch_bounds__(256, W) void attention_dq_kernel(AttnArgs a)
     const char* kb = head_base(a.k, a.k_starts, b, sq.k0, hk);
     const char* vb = head_base(a.v, a.k_starts, b, sq.k0, hk);
     const float c = a.scale * kLog2e;
+    typename Tl::Reader rd;
     const int n = (seen + KT - 1) / KT;
     const typename Tl::Fill kfill(a.k.ts, a.dim, wave), vfill(a.v.ts, a.dim, wave);
     auto fill = [&](char* kt, char* vt, int t) {
@@ -93,12 +94,13 @@ __global__ __launch_bounds__(256, W) void attention_dq_kernel(AttnArgs a)
 #pragma unroll
         for (int m = 0; m < KT / 32; ++m) {
             f32x16 s, dp;
+            rd.fresh();
             zero(s);
             zero(dp);
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) s = mma(Tl::rows(kt, 32 * m, i), q[i], s);
+            for (int i = 0; i < kSteps; ++i) s = mma(rd.rows(kt, 32 * m, i), q[i], s);
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) dp = mma(Tl::rows(vt, 32 * m, i), go[i], dp);
+            for (int i = 0; i < kSteps; ++i) dp = mma(rd.rows(vt, 32 * m, i), go[i], dp);
             const int left = limit - t * KT - 32 * m - 4 * h;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
@@ -110,7 +112,7 @@ __global__ __launch_bounds__(256, W) void attention_dq_kernel(AttnArgs a)
             for (int j = 0; j < 2; ++j) {
                 const Op p = as_operand<T>(s, j);
 #pragma unroll
-                for (int i = 0; i < kParts; ++i) dq[i] = mma(Tl::columns(kt, 2 * m + j, i), p, dq[i]);
+                for (int i = 0; i < kParts; ++i) dq[i] = mma(rd.columns(kt, 2 * m + j, i), p, dq[i]);
             }
         }
     };
@@ -150,11 +152,12 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
     typedef Tile<T, DP, QT, kWaves> Tl;
     typedef typename Operand<T>::type Op;
     constexpr int kSteps = DP / 16, kParts = DP / 32;
+    constexpr bool kPhases = sizeof(T) == 4 || DP == 128;
     __shared__ __align__(1024) char q0[Tl::kBytes], g0[Tl::kBytes], q1[Tl::kBytes], g1[Tl::kBytes];
     __shared__ __align__(256) float l0[64], d0[64], l1[64], d1[64];
     static_assert(QT <= 64, "one load brings a tile's row values");
     // The widest fp32 rows leave no registers for V: its operands come from LDS each time.
-    constexpr bool kValuesInLds = DP * sizeof(T) == 512;
+    constexpr bool kValuesInLds = DP == 128;
     typedef Tile<T, DP, 128, kWaves> Vl;
     __shared__ __align__(1024) char vt[kValuesInLds ? Vl::kBytes : 16];
     const int pairs = a.batch * a.kv_heads, bh = (int)blockIdx.x % pairs, b = bh / a.kv_heads, hk = bh % a.kv_heads;
@@ -191,6 +194,7 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
     const int per_head = from < sq.qn ? (sq.qn - from + QT - 1) / QT : 0;
     const int n = per_head * a.group;
     const float c = a.scale * kLog2e;
+    typename Tl::Reader rd;
     const typename Tl::Fill qfill(a.q.ts, a.dim, wave), gfill(a.go.ts, a.dim, wave);
     auto fill = [&](char* qt, char* gt, float* lt, float* dt, int t) {
         const int head = hk * a.group + t / per_head, tok = from + (t % per_head) * QT, left = sq.qn - tok;
@@ -211,15 +215,16 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
 #pragma unroll
         for (int m = 0; m < QT / 32; ++m) {
             f32x16 s, dp;
+            rd.fresh();
             zero(s);
             zero(dp);
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) s = mma(Tl::rows(qt, 32 * m, i), k[i], s);
-            phase<T>();
+            for (int i = 0; i < kSteps; ++i) s = mma(rd.rows(qt, 32 * m, i), k[i], s);
+            phase<kPhases>();
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
-                if constexpr (kValuesInLds) dp = mma(Tl::rows(gt, 32 * m, i), Vl::rows(vt, 32 * wave, i), dp);
-                else dp = mma(Tl::rows(gt, 32 * m, i), v[i], dp);
+                if constexpr (kValuesInLds) dp = mma(rd.rows(gt, 32 * m, i), rd.rows(vt, 32 * wave, i), dp);
+                else dp = mma(rd.rows(gt, 32 * m, i), v[i], dp);
             }
             // rows from `need` on see the key, and those before `left` are the sequence's
             const int need = first_token - tok - 32 * m - 4 * h, left = sq.qn - tok - 32 * m - 4 * h;
@@ -240,9 +245,9 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
                 const Op p = as_operand<T>(s, j), ds = as_operand<T>(dp, j);
 #pragma unroll
                 for (int i = 0; i < kParts; ++i) {
-                    phase<T>();
-                    dv[i] = mma(Tl::columns(gt, 2 * m + j, i), p, dv[i]);
-                    dk[i] = mma(Tl::columns(qt, 2 * m + j, i), ds, dk[i]);
+                    if (i % 2 == 0) phase<kPhases>();
+                    dv[i] = mma(rd.columns(gt, 2 * m + j, i), p, dv[i]);
+                    dk[i] = mma(rd.columns(qt, 2 * m + j, i), ds, dk[i]);
                 }
             }
         }
@@ -279,15 +284,15 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
         }
 }
 
-template <typename T, int DP, int KT, int QT>
+template <typename T, int DP, int KT, int QT, int WQ, int WK>
 hipError_t launch_bwd(const AttnArgs& a, hipStream_t stream)
 {
     const int64_t rows = (int64_t)a.q_len * a.group, qt = (rows + 127) / 128, kt = ((int64_t)a.k_len + 127) / 128;
     const unsigned heads = (unsigned)(a.batch * a.kv_heads);
-    if (qt > 0) attention_dq_kernel<T, DP, KT, 1><<<dim3((unsigned)qt * heads), 256, 0, stream>>>(a);
+    if (qt > 0) attention_dq_kernel<T, DP, KT, WQ><<<dim3((unsigned)qt * heads), 256, 0, stream>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (kt > 0) attention_dkv_kernel<T, DP, QT, 1><<<dim3((unsigned)kt * heads), 256, 0, stream>>>(a);
+    if (kt > 0) attention_dkv_kernel<T, DP, QT, WK><<<dim3((unsigned)kt * heads), 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -295,8 +300,8 @@ hipError_t launch_bwd(const AttnArgs& a, hipStream_t stream)
 
 hipError_t launch_attention_bwd(const AttnArgs& a, bool bf16, hipStream_t stream)
 {
-    if (bf16) return a.dim <= 64 ? launch_bwd<__bf16, 64, 64, 64>(a, stream) : launch_bwd<__bf16, 128, 64, 64>(a, stream);
-    return a.dim <= 64 ? launch_bwd<float, 64, 32, 32>(a, stream) : launch_bwd<float, 128, 32, 32>(a, stream);
+    if (bf16) return a.dim <= 64 ? launch_bwd<__bf16, 64, 64, 64, 3, 2>(a, stream) : launch_bwd<__bf16, 128, 32, 32, 2, 2>(a, stream);
+    return a.dim <= 64 ? launch_bwd<float, 64, 32, 32, 2, 1>(a, stream) : launch_bwd<float, 128, 32, 32, 1, 1>(a, stream);
 }
 
 }  // namespace dpb
