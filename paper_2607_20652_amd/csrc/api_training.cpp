@@ -165,8 +165,7 @@ dpb_status dpb_attention_bwd(const dpb_attn* a, dpb_dtype dtype, const dpb_heads
             if (outs[i] && outs[i] == outs[j]) return DPB_EINVAL;
     }
     g.lse = const_cast<float*>(lse);
-    g.row_lse2 = (float*)workspace;
-    g.row_delta = g.row_lse2 + g.q_rows * a->heads;
+    g.row_stats = (float*)workspace;
     return launched(dpb::launch_attention_bwd(g, dtype == DPB_BF16, (hipStream_t)stream));
 }
 

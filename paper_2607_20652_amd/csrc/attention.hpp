@@ -35,8 +35,7 @@ struct AttnArgs {
     AttnRows q, k, v, o;             // o: written by the forward, read by the backward
     AttnRows go, gq, gk, gv;         // backward: gradient of o (read), of q, k, v (written)
     float* lse;                      // [query rows, heads]
-    float* row_lse2;                 // backward scratch [heads][query rows]: lse * log2(e)
-    float* row_delta;                // and sum_d go * o
+    float* row_stats;                // backward scratch [heads][query rows][2]: lse * log2(e), sum_d go * o
     float* part;                     // scratch of a split call: [query rows][heads][splits][4 + dim]
                                      // (base, sum, -, -, output)
     const int32_t *q_lens, *k_lens;      // padded: lengths, or null
@@ -292,5 +291,43 @@ __device__ __forceinline__ void fill_wait() { wait_loads<0>(); }
 
 // Waits for this wave's reads of LDS (before a load is sent into what they read).
 __device__ __forceinline__ void wait_lds() { __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// LDS of a ring's stage: an object each, so that the compiler sees that reads of
+// one and loads into another are independent.
+template <int BYTES, int STAGE>
+__device__ __forceinline__ char* stage_lds()
+{
+    __shared__ __align__(1024) char lds[BYTES];
+    return lds;
+}
+
+// Steps 0..n-1 of a workgroup, the loads of each sent N - 1 steps ahead.
+// fill(lds, t) enqueues exactly L loads a wave (of nothing, where t >= n); step(lds,
+// t) uses them.  Before a step every wave has waited for its part of the stage and is
+// done with the step before, whose stage the loads sent next go into.
+template <int N, int L, int BYTES, typename F, typename S>
+__device__ __forceinline__ void ring(int n, F&& fill, S&& step)
+{
+    static_assert(N >= 2 && N <= 5, "stages");
+    char* const lds[5] = {stage_lds<BYTES, 0>(), stage_lds<BYTES, 1>(), stage_lds<BYTES, (N > 2 ? 2 : 0)>(),
+                          stage_lds<BYTES, (N > 3 ? 3 : 0)>(), stage_lds<BYTES, (N > 4 ? 4 : 0)>()};
+    if (n <= 0) return;
+#pragma unroll
+    for (int s = 0; s < N - 1; ++s) fill(lds[s], s);
+    for (int t = 0; t < n; t += N) {
+#pragma unroll
+        for (int s = 0; s < N; ++s) {
+            if (t + s < n) {
+                wait_lds();
+                wait_loads<L * (N - 2)>();
+                __builtin_amdgcn_s_barrier();
+                __asm__ volatile("" ::: "memory");
+                fill(lds[(s + N - 1) % N], t + s + N - 1);
+                step(lds[s], t + s);
+            }
+        }
+    }
+    wait_loads<0>();   // none is under way when the workgroup ends or its LDS is used again
+}
 
 }  // namespace dpb

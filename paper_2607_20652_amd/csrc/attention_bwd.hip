@@ -15,10 +15,10 @@ namespace {
 
 constexpr int kWaves = 4;
 
-__device__ __forceinline__ void zero(f32x16& c)
+__device__ __forceinline__ void fill16(f32x16& c, float v)
 {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) c[r] = 0.f;
+    for (int r = 0; r < 16; ++r) c[r] = v;
 }
 
 // fp32 operands take twice the registers: there the products' LDS reads stay in
@@ -31,13 +31,12 @@ __device__ __forceinline__ void phase()
 
 // dQ of 128 rows (tokens x the heads that share a key head); also leaves each
 // row's lse * log2(e) and delta for the other kernel.
-template <typename T, int DP, int KT, int W>
+template <typename T, int DP, int KT, int W, int NS>
 __global__ __launch_bounds__(256, W) void attention_dq_kernel(AttnArgs a)
 {
     typedef Tile<T, DP, KT, kWaves> Tl;
     typedef typename Operand<T>::type Op;
     constexpr int kSteps = DP / 16, kParts = DP / 32;
-    __shared__ __align__(1024) char k0[Tl::kBytes], v0[Tl::kBytes], k1[Tl::kBytes], v1[Tl::kBytes];
     const int tiles = (a.q_len * a.group + 127) / 128;
     const int pairs = a.batch * a.kv_heads, bh = (int)blockIdx.x % pairs, b = bh / a.kv_heads, hk = bh % a.kv_heads;
     const int tile = tiles - 1 - (int)blockIdx.x / pairs;
@@ -69,45 +68,45 @@ __global__ __launch_bounds__(256, W) void attention_dq_kernel(AttnArgs a)
         for (int j = 0; j < 8; ++j) delta = fmaf((float)go[i][j], (float)o[j], delta);
     }
     delta += other_half(delta);
-    const float lse2 = valid ? a.lse[(sq.q0 + token) * a.heads + head] * kLog2e : 0.f;
+    // a row that sees nothing: no score comes near its sum
+    const float lse2 = limit > 0 ? a.lse[(sq.q0 + token) * a.heads + head] * kLog2e : INFINITY;
     if (valid && h == 0) {
-        a.row_lse2[head * a.q_rows + sq.q0 + token] = lse2;
-        a.row_delta[head * a.q_rows + sq.q0 + token] = delta;
+        dpb_f32x2 stats = {lse2, delta};
+        *(dpb_f32x2*)(a.row_stats + 2 * (head * a.q_rows + sq.q0 + token)) = stats;
     }
 
     f32x16 dq[kParts];
 #pragma unroll
-    for (int i = 0; i < kParts; ++i) zero(dq[i]);
+    for (int i = 0; i < kParts; ++i) fill16(dq[i], 0.f);
     const char* kb = head_base(a.k, a.k_starts, b, sq.k0, hk);
     const char* vb = head_base(a.v, a.k_starts, b, sq.k0, hk);
     const float c = a.scale * kLog2e;
     typename Tl::Reader rd;
     const int n = (seen + KT - 1) / KT;
     const typename Tl::Fill kfill(a.k.ts, a.dim, wave), vfill(a.v.ts, a.dim, wave);
-    auto fill = [&](char* kt, char* vt, int t) {
-        kfill(kt, kb + (int64_t)t * KT * a.k.ts, sq.kn - t * KT, wave);
-        vfill(vt, vb + (int64_t)t * KT * a.v.ts, sq.kn - t * KT, wave);
+    auto fill = [&](char* lds, int t) {
+        const int left = t < n ? sq.kn - t * KT : 0;
+        kfill(lds, kb + (int64_t)t * KT * a.k.ts, left, wave);
+        vfill(lds + Tl::kBytes, vb + (int64_t)t * KT * a.v.ts, left, wave);
     };
-    auto step = [&](const char* kt, const char* vt, int t) {
-        if (t * KT >= most) return;
-        const bool edge = (t + 1) * KT > least;
+    auto products = [&](const char* kt, const char* vt, int t, bool edge) {
 #pragma unroll
         for (int m = 0; m < KT / 32; ++m) {
             f32x16 s, dp;
             rd.fresh();
-            zero(s);
-            zero(dp);
+            fill16(s, 0.f);
+            fill16(dp, -delta);
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) s = mma(rd.rows(kt, 32 * m, i), q[i], s);
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) dp = mma(rd.rows(vt, 32 * m, i), go[i], dp);
-            const int left = limit - t * KT - 32 * m - 4 * h;
+            if (edge) {
+                const int left = limit - t * KT - 32 * m - 4 * h;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                float p = __builtin_amdgcn_exp2f(fmaf(s[r], c, -lse2)) * (dp[r] - delta);
-                if (edge) p = 8 * (r >> 2) + (r & 3) < left ? p : 0.f;
-                s[r] = p;
+                for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) < left ? s[r] : -INFINITY;
             }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -lse2)) * dp[r];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const Op p = as_operand<T>(s, j);
@@ -116,18 +115,12 @@ __global__ __launch_bounds__(256, W) void attention_dq_kernel(AttnArgs a)
             }
         }
     };
-    if (n > 0) fill(k0, v0, 0);
-    for (int t = 0; t < n; t += 2) {
-        fill_wait();
-        __syncthreads();
-        if (t + 1 < n) fill(k1, v1, t + 1);
-        step(k0, v0, t);
-        if (t + 1 >= n) break;
-        fill_wait();
-        __syncthreads();
-        if (t + 2 < n) fill(k0, v0, t + 2);
-        step(k1, v1, t + 1);
-    }
+    auto step = [&](const char* kt, int t) {
+        const char* vt = kt + Tl::kBytes;
+        if (t * KT >= most) return;
+        products(kt, vt, t, (t + 1) * KT > least);
+    };
+    ring<NS, 2 * Tl::kLoads, 2 * Tl::kBytes>(n, fill, step);
 
     if (token >= sq.qw) return;
     const float f = limit > 0 ? a.scale : 0.f;
@@ -146,16 +139,14 @@ __global__ __launch_bounds__(256, W) void attention_dq_kernel(AttnArgs a)
 
 // dK and dV of 128 keys of one key head: the queries of every head that shares it
 // pass by, QT rows at a time.
-template <typename T, int DP, int QT, int W>
+template <typename T, int DP, int QT, int W, int NS>
 __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
 {
     typedef Tile<T, DP, QT, kWaves> Tl;
     typedef typename Operand<T>::type Op;
     constexpr int kSteps = DP / 16, kParts = DP / 32;
-    constexpr bool kPhases = sizeof(T) == 4 || DP == 128;
-    __shared__ __align__(1024) char q0[Tl::kBytes], g0[Tl::kBytes], q1[Tl::kBytes], g1[Tl::kBytes];
-    __shared__ __align__(256) float l0[64], d0[64], l1[64], d1[64];
-    static_assert(QT <= 64, "one load brings a tile's row values");
+    constexpr bool kPhases = sizeof(T) == 4;
+    constexpr int kStatBytes = QT * 8;
     // The widest fp32 rows leave no registers for V: its operands come from LDS each time.
     constexpr bool kValuesInLds = DP == 128;
     typedef Tile<T, DP, 128, kWaves> Vl;
@@ -182,8 +173,8 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
     f32x16 dk[kParts], dv[kParts];
 #pragma unroll
     for (int i = 0; i < kParts; ++i) {
-        zero(dk[i]);
-        zero(dv[i]);
+        fill16(dk[i], 0.f);
+        fill16(dv[i], 0.f);
     }
 
     // Query `token` sees this lane's key if token >= first_token; the tiles from the
@@ -196,74 +187,77 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
     const float c = a.scale * kLog2e;
     typename Tl::Reader rd;
     const typename Tl::Fill qfill(a.q.ts, a.dim, wave), gfill(a.go.ts, a.dim, wave);
-    auto fill = [&](char* qt, char* gt, float* lt, float* dt, int t) {
-        const int head = hk * a.group + t / per_head, tok = from + (t % per_head) * QT, left = sq.qn - tok;
-        qfill(qt, head_base(a.q, a.q_starts, b, sq.q0, head) + (int64_t)tok * a.q.ts, left, wave);
-        gfill(gt, head_base(a.go, a.q_starts, b, sq.q0, head) + (int64_t)tok * a.go.ts, left, wave);
-        if (wave < 2) {
-            const float* src = (wave ? a.row_delta : a.row_lse2) + head * a.q_rows + sq.q0 + tok;
-            const __amdgpu_buffer_rsrc_t buf =
-                __builtin_amdgcn_make_buffer_rsrc((void*)src, 0, min(left, QT) * 4, 0x00027000);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lds_void*)(wave ? dt : lt), 4, lane * 4, 0, 0, 0);
-        }
+    auto fill = [&](char* lds, int t) {
+        const int u = min(t, n - 1), head = hk * a.group + u / per_head, tok = from + (u % per_head) * QT;
+        const int left = t < n ? sq.qn - tok : 0;
+        qfill(lds, head_base(a.q, a.q_starts, b, sq.q0, head) + (int64_t)tok * a.q.ts, left, wave);
+        gfill(lds + Tl::kBytes, head_base(a.go, a.q_starts, b, sq.q0, head) + (int64_t)tok * a.go.ts, left, wave);
+        // the rows' two values each, by every wave alike
+        const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(
+            (void*)(a.row_stats + 2 * (head * a.q_rows + sq.q0 + tok)), 0, min(left, QT) * 8, 0x00027000);
+#pragma unroll
+        for (int i = 0; i < kStatBytes; i += 256)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lds_void*)(lds + 2 * Tl::kBytes + i), 4, lane * 4 + i, 0, 0, 0);
     };
-    auto step = [&](const char* qt, const char* gt, const float* lt, const float* dt, int t) {
-        const int tok = from + (t % per_head) * QT;
-        const int key_last = tile * 128 + wave * 32 + 31;
-        if (a.causal && tok + QT - 1 + behind < key_last - 31) return;   // no query of the tile sees this wave's keys
-        const bool edge = (a.causal && key_last > tok + behind) || tok + QT > sq.qn;
+    // rows at..at+31 of a tile, the first of them `tok` of the sequence
+    auto products = [&](const char* qt, const char* gt, const char* stats, int at, int tok, bool edge) {
+        f32x16 s, dp;
+        rd.fresh();
+        fill16(s, 0.f);
+        float l[16];
 #pragma unroll
-        for (int m = 0; m < QT / 32; ++m) {
-            f32x16 s, dp;
-            rd.fresh();
-            zero(s);
-            zero(dp);
+        for (int r = 0; r < 16; r += 2) {
+            const f32x4 x = *(const f32x4*)(stats + (at + 8 * (r >> 2) + (r & 3) + 4 * h) * 8);
+            l[r] = x[0];
+            dp[r] = -x[1];
+            l[r + 1] = x[2];
+            dp[r + 1] = -x[3];
+        }
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) s = mma(rd.rows(qt, 32 * m, i), k[i], s);
-            phase<kPhases>();
+        for (int i = 0; i < kSteps; ++i) s = mma(rd.rows(qt, at, i), k[i], s);
+        phase<kPhases>();
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) {
-                if constexpr (kValuesInLds) dp = mma(rd.rows(gt, 32 * m, i), rd.rows(vt, 32 * wave, i), dp);
-                else dp = mma(rd.rows(gt, 32 * m, i), v[i], dp);
-            }
+        for (int i = 0; i < kSteps; ++i) {
+            if constexpr (kValuesInLds) dp = mma(rd.rows(gt, at, i), rd.rows(vt, 32 * wave, i), dp);
+            else dp = mma(rd.rows(gt, at, i), v[i], dp);
+        }
+        if (edge) {
             // rows from `need` on see the key, and those before `left` are the sequence's
-            const int need = first_token - tok - 32 * m - 4 * h, left = sq.qn - tok - 32 * m - 4 * h;
+            const int need = first_token - tok - 4 * h, left = sq.qn - tok - 4 * h;
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const f32x4 l = *(const f32x4*)(lt + 32 * m + 8 * g + 4 * h), d = *(const f32x4*)(dt + 32 * m + 8 * g + 4 * h);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int r = 4 * g + j;
-                    float p = __builtin_amdgcn_exp2f(fmaf(s[r], c, -l[j]));
-                    if (edge) p = 8 * g + j >= need && 8 * g + j < left ? p : 0.f;
-                    s[r] = p;
-                    dp[r] = p * (dp[r] - d[j]);
-                }
+            for (int r = 0; r < 16; ++r) {
+                const int i = 8 * (r >> 2) + (r & 3);
+                s[r] = i >= need && i < left ? s[r] : -INFINITY;
             }
+        }
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const Op p = as_operand<T>(s, j), ds = as_operand<T>(dp, j);
+        for (int r = 0; r < 16; ++r) {
+            s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -l[r]));
+            dp[r] *= s[r];
+        }
 #pragma unroll
-                for (int i = 0; i < kParts; ++i) {
-                    if (i % 2 == 0) phase<kPhases>();
-                    dv[i] = mma(rd.columns(gt, 2 * m + j, i), p, dv[i]);
-                    dk[i] = mma(rd.columns(qt, 2 * m + j, i), ds, dk[i]);
-                }
+        for (int j = 0; j < 2; ++j) {
+            const Op p = as_operand<T>(s, j), ds = as_operand<T>(dp, j);
+#pragma unroll
+            for (int i = 0; i < kParts; ++i) {
+                if (i % 2 == 0) phase<kPhases>();
+                dv[i] = mma(rd.columns(gt, at / 16 + j, i), p, dv[i]);
+                dk[i] = mma(rd.columns(qt, at / 16 + j, i), ds, dk[i]);
             }
         }
     };
-    if (n > 0) fill(q0, g0, l0, d0, 0);
-    for (int t = 0; t < n; t += 2) {
-        fill_wait();
-        __syncthreads();
-        if (t + 1 < n) fill(q1, g1, l1, d1, t + 1);
-        step(q0, g0, l0, d0, t);
-        if (t + 1 >= n) break;
-        fill_wait();
-        __syncthreads();
-        if (t + 2 < n) fill(q0, g0, l0, d0, t + 2);
-        step(q1, g1, l1, d1, t + 1);
-    }
+    auto step = [&](const char* qt, int t) {
+        const char *gt = qt + Tl::kBytes, *stats = gt + Tl::kBytes;
+        const int tok = from + (t % per_head) * QT;
+        const int key_first = tile * 128 + wave * 32;
+#pragma unroll
+        for (int at = 0; at < QT; at += 32) {
+            const int first = tok + at;
+            if ((a.causal && first + 31 + behind < key_first) || first >= sq.qn) continue;   // nothing to see
+            products(qt, gt, stats, at, first, (a.causal && key_first + 31 > first + behind) || first + 32 > sq.qn);
+        }
+    };
+    ring<NS, 2 * Tl::kLoads + kStatBytes / 256, 2 * Tl::kBytes + kStatBytes>(n, fill, step);
 
     if (key >= sq.kw) return;
     char* okr = head_base(a.gk, a.k_starts, b, sq.k0, hk) + (int64_t)key * a.gk.ts;
@@ -284,15 +278,15 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
         }
 }
 
-template <typename T, int DP, int KT, int QT, int WQ, int WK>
+template <typename T, int DP, int KT, int WQ, int NQ, int QT, int WK, int NK>
 hipError_t launch_bwd(const AttnArgs& a, hipStream_t stream)
 {
     const int64_t rows = (int64_t)a.q_len * a.group, qt = (rows + 127) / 128, kt = ((int64_t)a.k_len + 127) / 128;
     const unsigned heads = (unsigned)(a.batch * a.kv_heads);
-    if (qt > 0) attention_dq_kernel<T, DP, KT, WQ><<<dim3((unsigned)qt * heads), 256, 0, stream>>>(a);
+    if (qt > 0) attention_dq_kernel<T, DP, KT, WQ, NQ><<<dim3((unsigned)qt * heads), 256, 0, stream>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (kt > 0) attention_dkv_kernel<T, DP, QT, WK><<<dim3((unsigned)kt * heads), 256, 0, stream>>>(a);
+    if (kt > 0) attention_dkv_kernel<T, DP, QT, WK, NK><<<dim3((unsigned)kt * heads), 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -300,8 +294,8 @@ hipError_t launch_bwd(const AttnArgs& a, hipStream_t stream)
 
 hipError_t launch_attention_bwd(const AttnArgs& a, bool bf16, hipStream_t stream)
 {
-    if (bf16) return a.dim <= 64 ? launch_bwd<__bf16, 64, 64, 64, 3, 2>(a, stream) : launch_bwd<__bf16, 128, 32, 32, 2, 2>(a, stream);
-    return a.dim <= 64 ? launch_bwd<float, 64, 32, 32, 2, 1>(a, stream) : launch_bwd<float, 128, 32, 32, 1, 1>(a, stream);
+    if (bf16) return a.dim <= 64 ? launch_bwd<__bf16, 64, 64, 3, 2, 64, 2, 2>(a, stream) : launch_bwd<__bf16, 128, 32, 2, 2, 32, 2, 2>(a, stream);
+    return a.dim <= 64 ? launch_bwd<float, 64, 32, 2, 2, 32, 2, 2>(a, stream) : launch_bwd<float, 128, 32, 1, 2, 32, 1, 2>(a, stream);
 }
 
 }  // namespace dpb
