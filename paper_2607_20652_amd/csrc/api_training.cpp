@@ -44,8 +44,8 @@ dpb_status check_sizes(const dpb_attn* a)
     const int64_t group = a->heads / a->kv_heads;
     if (a->batch > kMaxRows || a->q_len > kMaxRows / group || a->k_len > kMaxRows) return DPB_EUNSUPPORTED;
     if (a->q_starts && (a->q_rows > kMaxRows || a->k_rows > kMaxRows)) return DPB_EUNSUPPORTED;
-    // workgroups: at most one per 32 rows and head, and per 128 keys and head
-    const int64_t tiles = std::max((a->q_len * group + 31) / 32, (a->k_len + 127) / 128);
+    // workgroups: at most 64 per 32 rows and key head, and per 128 keys and key head
+    const int64_t tiles = std::max((a->q_len * group + 31) / 32, (a->k_len + 127) / 128) * 64;
     if (a->batch > 0 && tiles > 0 && (a->kv_heads > kMaxRows / a->batch || a->kv_heads * a->batch > kMaxRows / tiles))
         return DPB_EUNSUPPORTED;
     return DPB_OK;
@@ -75,6 +75,9 @@ dpb_status take(const dpb_attn* a, dpb_dtype t, const dpb_heads* x, bool q, Attn
     }
     return out->ts >= kMaxTokenBytes ? DPB_EUNSUPPORTED : DPB_OK;
 }
+
+// The backward's two floats per query row and head, before its parts.
+size_t stats_bytes(const dpb_attn* a) { return ((size_t)rows_of(a, true) * a->heads * 8 + 15) / 16 * 16; }
 
 void fill_args(const dpb_attn* a, AttnArgs* g)
 {
@@ -110,7 +113,11 @@ size_t dpb_attention_workspace_bytes(const dpb_attn* a)
 size_t dpb_attention_bwd_workspace_bytes(const dpb_attn* a)
 {
     if (check_sizes(a)) return 0;
-    return (size_t)rows_of(a, true) * a->heads * 8;
+    int q_parts, k_parts;
+    dpb::attention_parts((int)a->batch, (int)a->q_len, (int)a->k_len, a->heads, a->kv_heads, &q_parts, &k_parts);
+    const size_t dq = q_parts > 1 ? (size_t)q_parts * rows_of(a, true) * a->heads : 0;
+    const size_t dkv = k_parts > 1 ? (size_t)k_parts * rows_of(a, false) * a->kv_heads * 2 : 0;
+    return stats_bytes(a) + std::max(dq, dkv) * a->head_dim * 4;
 }
 
 dpb_status dpb_attention(const dpb_attn* a, dpb_dtype dtype, const dpb_heads* q, const dpb_heads* k,
@@ -153,8 +160,8 @@ dpb_status dpb_attention_bwd(const dpb_attn* a, dpb_dtype dtype, const dpb_heads
         if ((s = take(a, dtype, t.x, t.q, t.to))) return s;
     if (a->batch == 0 || (g.q_rows == 0 && g.k_rows == 0)) return DPB_OK;
     const size_t need = dpb_attention_bwd_workspace_bytes(a);
-    if (g.q_rows > 0 && (!lse || !aligned16(lse) || !workspace || !aligned16(workspace) || ws_bytes < need))
-        return DPB_EINVAL;
+    if (g.q_rows > 0 && (!lse || !aligned16(lse))) return DPB_EINVAL;
+    if (need && (!workspace || !aligned16(workspace) || ws_bytes < need)) return DPB_EINVAL;
     // an output that is an input (or another output) would be read after it is written
     const void* outs[3] = {g.gq.p, g.gk.p, g.gv.p};
     const void* ins[5] = {g.go.p, g.q.p, g.k.p, g.v.p, g.o.p};
@@ -166,6 +173,8 @@ dpb_status dpb_attention_bwd(const dpb_attn* a, dpb_dtype dtype, const dpb_heads
     }
     g.lse = const_cast<float*>(lse);
     g.row_stats = (float*)workspace;
+    g.part = (float*)((char*)workspace + stats_bytes(a));
+    dpb::attention_parts(g.batch, g.q_len, g.k_len, g.heads, g.kv_heads, &g.q_parts, &g.k_parts);
     return launched(dpb::launch_attention_bwd(g, dtype == DPB_BF16, (hipStream_t)stream));
 }
 

@@ -36,15 +36,16 @@ struct AttnArgs {
     AttnRows go, gq, gk, gv;         // backward: gradient of o (read), of q, k, v (written)
     float* lse;                      // [query rows, heads]
     float* row_stats;                // backward scratch [heads][query rows][2]: lse * log2(e), sum_d go * o
-    float* part;                     // scratch of a split call: [query rows][heads][splits][4 + dim]
-                                     // (base, sum, -, -, output)
+    float* part;                     // scratch of a split call.  Forward: [query rows][heads][splits][4 + dim]
+                                     // (base, sum, -, -, output); backward: [parts][rows][heads][dim]
     const int32_t *q_lens, *k_lens;      // padded: lengths, or null
     const int32_t *q_starts, *k_starts;  // packed: starts, or null
     int64_t q_rows, k_rows;          // rows of q and k in all
     int batch, q_len, k_len;         // sequences; padded lengths, or the longest packed ones
     int heads, kv_heads, group, dim;
     int causal;
-    int splits;                      // parts the keys are split into
+    int splits;                      // forward: parts the keys are split into
+    int q_parts, k_parts;            // backward: workgroups that share a tile of dQ, of dK and dV
     float scale;
 };
 
@@ -54,6 +55,7 @@ hipError_t launch_attention_bwd(const AttnArgs& a, bool bf16, hipStream_t stream
 // rows), and the scratch floats that takes.
 int attention_splits(int batch, int q_len, int k_len, int heads, int kv_heads);
 size_t attention_part_floats(int64_t q_rows, int heads, int dim, int splits);
+void attention_parts(int batch, int q_len, int k_len, int heads, int kv_heads, int* q_parts, int* k_parts);
 
 // Where sequence b lies: rows before it, its lengths, and the query (key) rows
 // of the outputs that belong to it.  Packed starts are clamped to the tensor, so

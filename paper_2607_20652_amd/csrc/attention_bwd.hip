@@ -4,10 +4,14 @@
 //     dV = P^T dO,   dQ = scale dS K,   dK = scale dS^T Q.
 //
 // Two kernels, each with its result in registers from the first key (query) to
-// the last: one over query rows for dQ, one over keys for dK and dV.  Scores and
+// the last: one over query rows for dQ, one over keys for dK and dV.  (Where that
+// leaves compute units idle, several workgroups share a result and their fp32
+// parts are added up afterwards, in order.)  Scores and
 // dP are computed in both (seven products in place of five), and in return no
 // gradient is added up in memory: no atomics, so the same bits every run, and
 // each score lies in registers as the operand that the next product takes.
+#include <algorithm>
+
 #include "attention.hpp"
 
 namespace dpb {
@@ -19,6 +23,22 @@ __device__ __forceinline__ void fill16(f32x16& c, float v)
 {
 #pragma unroll
     for (int r = 0; r < 16; ++r) c[r] = v;
+}
+
+// This lane's column of a transposed result, times f, as a row; zeros unless `live`.
+template <typename T, int DP>
+__device__ __forceinline__ void store_rows(char* row, int dim, const f32x16 (&c)[DP / 32], float f, bool live)
+{
+    const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int e = 32 * i + 8 * g + 4 * h;
+            if (e >= dim) continue;
+            if (live) store4<T>(row, e, c[i][4 * g] * f, c[i][4 * g + 1] * f, c[i][4 * g + 2] * f, c[i][4 * g + 3] * f);
+            else store4<T>(row, e, 0.f, 0.f, 0.f, 0.f);
+        }
 }
 
 // fp32 operands take twice the registers: there the products' LDS reads stay in
@@ -39,7 +59,7 @@ __global__ __launch_bounds__(256, W) void attention_dq_kernel(AttnArgs a)
     constexpr int kSteps = DP / 16, kParts = DP / 32;
     const int tiles = (a.q_len * a.group + 127) / 128;
     const int pairs = a.batch * a.kv_heads, bh = (int)blockIdx.x % pairs, b = bh / a.kv_heads, hk = bh % a.kv_heads;
-    const int tile = tiles - 1 - (int)blockIdx.x / pairs;
+    const int part = (int)blockIdx.x / pairs % a.q_parts, tile = tiles - 1 - (int)blockIdx.x / pairs / a.q_parts;
     const Sequence sq = sequence_of(a, b);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     if (tile * 128 >= sq.qw * a.group) return;
@@ -70,7 +90,7 @@ __global__ __launch_bounds__(256, W) void attention_dq_kernel(AttnArgs a)
     delta += other_half(delta);
     // a row that sees nothing: no score comes near its sum
     const float lse2 = limit > 0 ? a.lse[(sq.q0 + token) * a.heads + head] * kLog2e : INFINITY;
-    if (valid && h == 0) {
+    if (valid && h == 0 && part == 0) {
         dpb_f32x2 stats = {lse2, delta};
         *(dpb_f32x2*)(a.row_stats + 2 * (head * a.q_rows + sq.q0 + token)) = stats;
     }
@@ -82,10 +102,12 @@ __global__ __launch_bounds__(256, W) void attention_dq_kernel(AttnArgs a)
     const char* vb = head_base(a.v, a.k_starts, b, sq.k0, hk);
     const float c = a.scale * kLog2e;
     typename Tl::Reader rd;
-    const int n = (seen + KT - 1) / KT;
+    const int all = (seen + KT - 1) / KT, begin = (int)((int64_t)all * part / a.q_parts);
+    const int n = (int)((int64_t)all * (part + 1) / a.q_parts) - begin;
     const typename Tl::Fill kfill(a.k.ts, a.dim, wave), vfill(a.v.ts, a.dim, wave);
     auto fill = [&](char* lds, int t) {
-        const int left = t < n ? sq.kn - t * KT : 0;
+        const int left = t < n ? sq.kn - (begin + t) * KT : 0;
+        t += begin;
         kfill(lds, kb + (int64_t)t * KT * a.k.ts, left, wave);
         vfill(lds + Tl::kBytes, vb + (int64_t)t * KT * a.v.ts, left, wave);
     };
@@ -117,24 +139,18 @@ __global__ __launch_bounds__(256, W) void attention_dq_kernel(AttnArgs a)
     };
     auto step = [&](const char* kt, int t) {
         const char* vt = kt + Tl::kBytes;
+        t += begin;
         if (t * KT >= most) return;
         products(kt, vt, t, (t + 1) * KT > least);
     };
     ring<NS, 2 * Tl::kLoads, 2 * Tl::kBytes>(n, fill, step);
 
     if (token >= sq.qw) return;
-    const float f = limit > 0 ? a.scale : 0.f;
-    char* out = head_base(a.gq, a.q_starts, b, sq.q0, head) + (int64_t)token * a.gq.ts;
-#pragma unroll
-    for (int i = 0; i < kParts; ++i)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int e = 32 * i + 8 * g + 4 * h;
-            if (e < a.dim) {
-                if (limit > 0) store4<T>(out, e, dq[i][4 * g] * f, dq[i][4 * g + 1] * f, dq[i][4 * g + 2] * f, dq[i][4 * g + 3] * f);
-                else store4<T>(out, e, 0.f, 0.f, 0.f, 0.f);
-            }
-        }
+    if (a.q_parts > 1) {
+        store_rows<float, DP>((char*)(a.part + ((part * a.q_rows + sq.q0 + token) * a.heads + head) * a.dim), a.dim, dq, 1.f, limit > 0);
+        return;
+    }
+    store_rows<T, DP>(head_base(a.gq, a.q_starts, b, sq.q0, head) + (int64_t)token * a.gq.ts, a.dim, dq, a.scale, limit > 0);
 }
 
 // dK and dV of 128 keys of one key head: the queries of every head that shares it
@@ -152,7 +168,8 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
     typedef Tile<T, DP, 128, kWaves> Vl;
     __shared__ __align__(1024) char vt[kValuesInLds ? Vl::kBytes : 16];
     const int pairs = a.batch * a.kv_heads, bh = (int)blockIdx.x % pairs, b = bh / a.kv_heads, hk = bh % a.kv_heads;
-    const int tile = (int)blockIdx.x / pairs;   // of a causal sequence the keys that most queries see first
+    const int part = (int)blockIdx.x / pairs % a.k_parts;
+    const int tile = (int)blockIdx.x / pairs / a.k_parts;   // of a causal sequence the keys that most queries see first
     const Sequence sq = sequence_of(a, b);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     if (tile * 128 >= sq.kw) return;
@@ -183,12 +200,13 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
     const int first_token = a.causal ? key - behind : 0;
     const int from = tile * 128 >= sq.kn ? sq.qn : a.causal ? max(tile * 128 - behind, 0) / QT * QT : 0;
     const int per_head = from < sq.qn ? (sq.qn - from + QT - 1) / QT : 0;
-    const int n = per_head * a.group;
+    const int all = per_head * a.group, begin = (int)((int64_t)all * part / a.k_parts);
+    const int n = (int)((int64_t)all * (part + 1) / a.k_parts) - begin;
     const float c = a.scale * kLog2e;
     typename Tl::Reader rd;
     const typename Tl::Fill qfill(a.q.ts, a.dim, wave), gfill(a.go.ts, a.dim, wave);
     auto fill = [&](char* lds, int t) {
-        const int u = min(t, n - 1), head = hk * a.group + u / per_head, tok = from + (u % per_head) * QT;
+        const int u = begin + min(t, n - 1), head = hk * a.group + u / per_head, tok = from + (u % per_head) * QT;
         const int left = t < n ? sq.qn - tok : 0;
         qfill(lds, head_base(a.q, a.q_starts, b, sq.q0, head) + (int64_t)tok * a.q.ts, left, wave);
         gfill(lds + Tl::kBytes, head_base(a.go, a.q_starts, b, sq.q0, head) + (int64_t)tok * a.go.ts, left, wave);
@@ -248,7 +266,7 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
     };
     auto step = [&](const char* qt, int t) {
         const char *gt = qt + Tl::kBytes, *stats = gt + Tl::kBytes;
-        const int tok = from + (t % per_head) * QT;
+        const int tok = from + ((begin + t) % per_head) * QT;
         const int key_first = tile * 128 + wave * 32;
 #pragma unroll
         for (int at = 0; at < QT; at += 32) {
@@ -260,37 +278,75 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
     ring<NS, 2 * Tl::kLoads + kStatBytes / 256, 2 * Tl::kBytes + kStatBytes>(n, fill, step);
 
     if (key >= sq.kw) return;
-    char* okr = head_base(a.gk, a.k_starts, b, sq.k0, hk) + (int64_t)key * a.gk.ts;
-    char* ovr = head_base(a.gv, a.k_starts, b, sq.k0, hk) + (int64_t)key * a.gv.ts;
+    if (a.k_parts > 1) {
+        const int64_t at = ((part * a.k_rows + sq.k0 + key) * a.kv_heads + hk) * a.dim;
+        store_rows<float, DP>((char*)(a.part + at), a.dim, dk, 1.f, valid);
+        store_rows<float, DP>((char*)(a.part + a.k_parts * a.k_rows * a.kv_heads * a.dim + at), a.dim, dv, 1.f, valid);
+        return;
+    }
+    store_rows<T, DP>(head_base(a.gk, a.k_starts, b, sq.k0, hk) + (int64_t)key * a.gk.ts, a.dim, dk, a.scale, valid);
+    store_rows<T, DP>(head_base(a.gv, a.k_starts, b, sq.k0, hk) + (int64_t)key * a.gv.ts, a.dim, dv, 1.f, valid);
+}
+
+// Adds up the parts of dQ, or of dK and dV, in their order: four elements a lane.
+template <typename T, bool QUERY>
+__global__ __launch_bounds__(256) void attention_sum_kernel(AttnArgs a)
+{
+    const int len = QUERY ? a.q_len : a.k_len, heads = QUERY ? a.heads : a.kv_heads, parts = QUERY ? a.q_parts : a.k_parts;
+    const int64_t quads = (int64_t)len * heads * (a.dim / 4), per = (quads + 255) / 256;
+    const int b = (int)(blockIdx.x / per);
+    const int64_t id = (blockIdx.x % per) * 256 + threadIdx.x;
+    const Sequence sq = sequence_of(a, b);
+    const int e = 4 * (int)(id % (a.dim / 4)), head = (int)(id / (a.dim / 4) % heads);
+    const int64_t row = id / (a.dim / 4) / heads;
+    if (row >= (QUERY ? sq.qw : sq.kw)) return;
+    const int64_t first = QUERY ? sq.q0 : sq.k0, stride = (QUERY ? a.q_rows : a.k_rows) * heads * a.dim;
 #pragma unroll
-    for (int i = 0; i < kParts; ++i)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int e = 32 * i + 8 * g + 4 * h;
-            if (e >= a.dim) continue;
-            if (valid) {
-                store4<T>(okr, e, dk[i][4 * g] * a.scale, dk[i][4 * g + 1] * a.scale, dk[i][4 * g + 2] * a.scale, dk[i][4 * g + 3] * a.scale);
-                store4<T>(ovr, e, dv[i][4 * g], dv[i][4 * g + 1], dv[i][4 * g + 2], dv[i][4 * g + 3]);
-            } else {
-                store4<T>(okr, e, 0.f, 0.f, 0.f, 0.f);
-                store4<T>(ovr, e, 0.f, 0.f, 0.f, 0.f);
-            }
-        }
+    for (int which = 0; which < (QUERY ? 1 : 2); ++which) {
+        const float* from = a.part + which * parts * stride + ((first + row) * heads + head) * a.dim + e;
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int p = 0; p < parts; ++p) sum += *(const f32x4*)(from + p * stride);
+        const AttnRows& to = QUERY ? a.gq : which ? a.gv : a.gk;
+        const float f = which ? 1.f : a.scale;
+        store4<T>(head_base(to, QUERY ? a.q_starts : a.k_starts, b, first, head) + row * to.ts, e, sum[0] * f, sum[1] * f, sum[2] * f, sum[3] * f);
+    }
 }
 
 template <typename T, int DP, int KT, int WQ, int NQ, int QT, int WK, int NK>
 hipError_t launch_bwd(const AttnArgs& a, hipStream_t stream)
 {
     const int64_t rows = (int64_t)a.q_len * a.group, qt = (rows + 127) / 128, kt = ((int64_t)a.k_len + 127) / 128;
-    const unsigned heads = (unsigned)(a.batch * a.kv_heads);
-    if (qt > 0) attention_dq_kernel<T, DP, KT, WQ, NQ><<<dim3((unsigned)qt * heads), 256, 0, stream>>>(a);
-    hipError_t e = hipGetLastError();
+    const int64_t pairs = (int64_t)a.batch * a.kv_heads;
+    auto sums = [&](int64_t len, int heads) { return dim3((unsigned)((len * heads * (a.dim / 4) + 255) / 256 * a.batch)); };
+    if (qt > 0) {
+        attention_dq_kernel<T, DP, KT, WQ, NQ><<<dim3((unsigned)(qt * pairs * a.q_parts)), 256, 0, stream>>>(a);
+        if (a.q_parts > 1) attention_sum_kernel<T, true><<<sums(a.q_len, a.heads), 256, 0, stream>>>(a);
+    }
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (kt > 0) attention_dkv_kernel<T, DP, QT, WK, NK><<<dim3((unsigned)kt * heads), 256, 0, stream>>>(a);
+    if (kt > 0) {
+        attention_dkv_kernel<T, DP, QT, WK, NK><<<dim3((unsigned)(kt * pairs * a.k_parts)), 256, 0, stream>>>(a);
+        if (a.k_parts > 1) attention_sum_kernel<T, false><<<sums(a.k_len, a.kv_heads), 256, 0, stream>>>(a);
+    }
     return hipGetLastError();
 }
 
 }  // namespace
+
+void attention_parts(int batch, int q_len, int k_len, int heads, int kv_heads, int* q_parts, int* k_parts)
+{
+    // Work for every compute unit, in pieces short enough to even out: the products of
+    // few rows (keys) are parted along the keys (rows of all heads that share one), each
+    // part of 128 of those or more.
+    const int64_t cus = device_cus(), pairs = std::max<int64_t>(1, (int64_t)batch * kv_heads), group = heads / kv_heads;
+    const int64_t qt = std::max<int64_t>(1, (q_len * group + 127) / 128), kt = std::max<int64_t>(1, ((int64_t)k_len + 127) / 128);
+    auto parts = [&](int64_t want, int64_t units, int64_t most) {
+        return (int)std::max<int64_t>(1, std::min({(want + units - 1) / units, most, (int64_t)64}));
+    };
+    *q_parts = parts(2 * cus, qt * pairs, k_len / 128);
+    *k_parts = parts(4 * cus, kt * pairs, q_len * group / 128);
+}
 
 hipError_t launch_attention_bwd(const AttnArgs& a, bool bf16, hipStream_t stream)
 {
