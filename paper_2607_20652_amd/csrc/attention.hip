@@ -7,8 +7,6 @@
 namespace dpb {
 namespace {
 
-constexpr int kWaves = 4;
-
 // Weights are 2^(c s - base).  The base follows the largest score only where that
 // is this far above it: up to 2^8 a weight is as precise as one below 1, in bf16
 // and fp32, and the output need not be rescaled for every new maximum.
@@ -41,14 +39,10 @@ struct Rows {
         return s + other_half(s);
     }
 
-    // One tile of KT keys, the first of them key `first`; this lane's row sees the
-    // keys below `limit`, and every row of the wave sees all of the tile unless `edge`.
-    template <int KT, int W>
-    __device__ __forceinline__ void step(typename Tile<T, DP, KT, W>::Reader& rd, const char* kt, const char* vt, int first, int limit, bool edge, float c)
+    // Scores of a tile: KT keys (rows of the result) against the wave's rows.
+    template <int KT, typename R>
+    __device__ __forceinline__ void scores(f32x16 (&s)[KT / 32], const R& rd, const char* kt) const
     {
-        const int h = (threadIdx.x & 63) >> 5;
-        rd.fresh();
-        f32x16 s[KT / 32];
 #pragma unroll
         for (int m = 0; m < KT / 32; ++m) {
 #pragma unroll
@@ -56,12 +50,19 @@ struct Rows {
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) s[m] = mma(rd.rows(kt, 32 * m, i), q[i], s[m]);
         }
+    }
+
+    // Takes a tile's scores into account for the base, keys `seen` and on left out (where
+    // `edge`: some row of the wave does not see all of the tile).
+    template <int KT>
+    __device__ __forceinline__ void raise(f32x16 (&s)[KT / 32], int seen, bool edge, float c)
+    {
         if (edge) {
-            const int n = limit - first - 4 * h;
+            const int n = seen - 4 * ((threadIdx.x & 63) >> 5);
 #pragma unroll
             for (int m = 0; m < KT / 32; ++m)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[m][r] = 32 * m + 8 * (r >> 2) + (r & 3) < n ? s[m][r] : -INFINITY;
+                for (int r = 0; r < 16; ++r) s[m][r] = 32 * m + 8 * (r >> 2) + (r & 3) < n ? apart(s[m][r]) : -INFINITY;
         }
         float big = s[0][0];
 #pragma unroll
@@ -81,18 +82,30 @@ struct Rows {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[i][r] *= keep;
         }
+    }
+
+    // Scores to weights.
+    template <int KT>
+    __device__ __forceinline__ void weigh(f32x16 (&s)[KT / 32], float c)
+    {
         const float from = base == -INFINITY ? 0.f : base;   // nothing seen so far: every weight is 0
-        float add = 0.f;
+        float add[2] = {0.f, 0.f};
 #pragma unroll
         for (int m = 0; m < KT / 32; ++m)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 s[m][r] = __builtin_amdgcn_exp2f(fmaf(s[m][r], c, -from));
-                add += s[m][r];
+                add[r & 1] += s[m][r];
             }
-        const float old = sum, term = lost + add;
+        const float old = sum, term = lost + (add[0] + add[1]);
         sum = old + term;
         lost = term - (sum - old);
+    }
+
+    // Weights times the tile's values.
+    template <int KT, typename R>
+    __device__ __forceinline__ void gather(const f32x16 (&s)[KT / 32], const R& rd, const char* vt)
+    {
 #pragma unroll
         for (int j = 0; j < KT / 16; ++j) {
             const typename Operand<T>::type p = as_operand<T>(s[j / 2], j & 1);
@@ -113,27 +126,27 @@ __device__ __forceinline__ float log_sum(float base, float total)
 
 // One workgroup: 128 rows (tokens x the heads that share a key head) against the
 // keys they see.
-template <typename T, int DP, int KT, int W>
-__global__ __launch_bounds__(256, W) void attention_kernel(AttnArgs a)
+template <typename T, int DP, int KT, int WAVES, int W>
+__global__ __launch_bounds__(64 * WAVES, W) void attention_kernel(AttnArgs a)
 {
-    typedef Tile<T, DP, KT, kWaves> Tl;
-    __shared__ __align__(1024) char k0[Tl::kBytes], v0[Tl::kBytes], k1[Tl::kBytes], v1[Tl::kBytes];
-    const int tiles = (a.q_len * a.group + 127) / 128;
+    typedef Tile<T, DP, KT, WAVES> Tl;
+    constexpr int kRows = 32 * WAVES, kKeys = KT < 64 ? KT : 64;
+    const int tiles = (a.q_len * a.group + kRows - 1) / kRows;
     const int pairs = a.batch * a.kv_heads, bh = (int)blockIdx.x % pairs, b = bh / a.kv_heads, hk = bh % a.kv_heads;
     const int tile = tiles - 1 - (int)blockIdx.x / pairs;   // of causal sequences the longest rows first
     const Sequence sq = sequence_of(a, b);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (tile * 128 >= sq.qw * a.group) return;
+    if (tile * kRows >= sq.qw * a.group) return;
 
-    const int row = tile * 128 + wave * 32 + (lane & 31);
+    const int row = tile * kRows + wave * 32 + (lane & 31);
     const int token = row / a.group, head = hk * a.group + row % a.group;
     const bool valid = token < sq.qn;
     const int limit = visible_keys(a, sq, token);
     // keys that any row of the workgroup, that every row of this wave, and that any row of it sees
-    const int last = min((tile * 128 + 127) / a.group, sq.qn - 1);
-    const int seen = last * a.group + a.group - 1 >= tile * 128 ? visible_keys(a, sq, last) : 0;
+    const int last = min((tile * kRows + kRows - 1) / a.group, sq.qn - 1);
+    const int seen = last * a.group + a.group - 1 >= tile * kRows ? visible_keys(a, sq, last) : 0;
     const int least = __all(valid) ? __builtin_amdgcn_readfirstlane(limit) : 0;
-    const int wave_last = min((tile * 128 + wave * 32 + 31) / a.group, sq.qn - 1);
+    const int wave_last = min((tile * kRows + wave * 32 + 31) / a.group, sq.qn - 1);
     const int most = wave_last >= 0 ? visible_keys(a, sq, wave_last) : 0;
 
     Rows<T, DP> st;
@@ -148,26 +161,25 @@ __global__ __launch_bounds__(256, W) void attention_kernel(AttnArgs a)
     const float c = a.scale * kLog2e;
     const int n = (seen + KT - 1) / KT;
     const typename Tl::Fill kfill(a.k.ts, a.dim, wave), vfill(a.v.ts, a.dim, wave);
-    auto fill = [&](char* kt, char* vt, int t) {
-        kfill(kt, kb + (int64_t)t * KT * a.k.ts, sq.kn - t * KT, wave);
-        vfill(vt, vb + (int64_t)t * KT * a.v.ts, sq.kn - t * KT, wave);
+    auto fill = [&](char* lds, int t) {
+        const int left = t < n ? sq.kn - t * KT : 0;
+        kfill(lds, kb + (int64_t)t * KT * a.k.ts, left, wave);
+        vfill(lds + Tl::kBytes, vb + (int64_t)t * KT * a.v.ts, left, wave);
     };
-    auto step = [&](const char* kt, const char* vt, int t) {
-        if (t * KT < most) st.template step<KT, kWaves>(rd, kt, vt, t * KT, limit, (t + 1) * KT > least, c);
+    auto step = [&](const char* lds, int t) {
+#pragma unroll
+        for (int at = 0; at < KT; at += 64) {
+            const int first = t * KT + at;
+            if (first >= most) return;
+            f32x16 s[kKeys / 32];
+            rd.fresh();
+            st.template scores<kKeys>(s, rd, lds + at * Tl::kRowBytes);
+            st.template raise<kKeys>(s, limit - first, first + kKeys > least, c);
+            st.template weigh<kKeys>(s, c);
+            st.template gather<kKeys>(s, rd, lds + Tl::kBytes + at * Tl::kRowBytes);
+        }
     };
-    if (n > 0) fill(k0, v0, 0);
-    for (int t = 0; t < n; t += 2) {
-        // every wave is done with the tile before last, and tile t has landed
-        fill_wait();
-        __syncthreads();
-        if (t + 1 < n) fill(k1, v1, t + 1);
-        step(k0, v0, t);
-        if (t + 1 >= n) break;
-        fill_wait();
-        __syncthreads();
-        if (t + 2 < n) fill(k0, v0, t + 2);
-        step(k1, v1, t + 1);
-    }
+    ring<2, 2 * Tl::kLoads, 2 * Tl::kBytes>(n, fill, step);
 
     const float total = st.total();
     if (token >= sq.qw) return;
@@ -196,7 +208,6 @@ __global__ __launch_bounds__(64 * WAVES, 1) void attention_split_kernel(AttnArgs
 {
     typedef Tile<T, DP, 32, 1> Tl;
     constexpr int kLoads = 2 * Tl::kLoads;   // loads of one tile's keys and values
-    __shared__ __align__(1024) char k0[WAVES][Tl::kBytes], v0[WAVES][Tl::kBytes], k1[WAVES][Tl::kBytes], v1[WAVES][Tl::kBytes];
     __shared__ float bases[WAVES][32], totals[WAVES][32];
     const int tiles = (a.q_len * a.group + 31) / 32;
     const int pairs = a.batch * a.kv_heads, bh = (int)blockIdx.x % pairs, b = bh / a.kv_heads, hk = bh % a.kv_heads;
@@ -225,42 +236,43 @@ __global__ __launch_bounds__(64 * WAVES, 1) void attention_split_kernel(AttnArgs
     const char* vb = head_base(a.v, a.k_starts, b, sq.k0, hk);
     const float c = a.scale * kLog2e;
     const typename Tl::Fill kfill(a.k.ts, a.dim, 0), vfill(a.v.ts, a.dim, 0);
-    auto fill = [&](char* kt, char* vt, int t) {
-        kfill(kt, kb + (int64_t)t * 32 * a.k.ts, sq.kn - t * 32, 0);
-        vfill(vt, vb + (int64_t)t * 32 * a.v.ts, sq.kn - t * 32, 0);
+    char* const mine[2] = {stage_lds<2 * Tl::kBytes * WAVES, 0>() + 2 * Tl::kBytes * wave,
+                           stage_lds<2 * Tl::kBytes * WAVES, 1>() + 2 * Tl::kBytes * wave};
+    auto fill = [&](char* lds, int t) {
+        kfill(lds, kb + (int64_t)t * 32 * a.k.ts, sq.kn - t * 32, 0);
+        vfill(lds + Tl::kBytes, vb + (int64_t)t * 32 * a.v.ts, sq.kn - t * 32, 0);
     };
-    auto step = [&](const char* kt, const char* vt, int t) {
-        st.template step<32, 1>(rd, kt, vt, t * 32, limit, (t + 1) * 32 > least, c);
+    auto step = [&](const char* lds, int t) {
+        f32x16 s[1];
+        rd.fresh();
+        st.template scores<32>(s, rd, lds);
+        st.template raise<32>(s, limit - t * 32, (t + 1) * 32 > least, c);
+        st.template weigh<32>(s, c);
+        st.template gather<32>(s, rd, lds + Tl::kBytes);
     };
     int t = begin + wave;
-    if (t < end) fill(k0[wave], v0[wave], t);
+    if (t < end) fill(mine[0], t);
     while (t < end) {
-        // the buffer's last reads are done; the older of the two tiles in flight has landed
-        wait_lds();
-        if (t + WAVES < end) {
-            fill(k1[wave], v1[wave], t + WAVES);
-            wait_loads<kLoads>();
-        } else {
-            wait_loads<0>();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (t >= end) break;
+            // the other buffer's last reads are done; of the two tiles in flight the older has landed
+            wait_lds();
+            if (t + WAVES < end) {
+                fill(mine[i ^ 1], t + WAVES);
+                wait_loads<kLoads>();
+            } else {
+                wait_loads<0>();
+            }
+            step(mine[i], t);
+            t += WAVES;
         }
-        step(k0[wave], v0[wave], t);
-        t += WAVES;
-        if (t >= end) break;
-        wait_lds();
-        if (t + WAVES < end) {
-            fill(k0[wave], v0[wave], t + WAVES);
-            wait_loads<kLoads>();
-        } else {
-            wait_loads<0>();
-        }
-        step(k1[wave], v1[wave], t);
-        t += WAVES;
     }
 
-    // the waves' states, a wave's output rows in its own key and value buffers
+    // the waves' states, a wave's output rows in its own buffers
     const float total = st.total();
     const int h = lane >> 5;
-    static_assert(Tl::kBytes >= 32 * DP * 2, "an output row tile takes two buffers");
+    static_assert(2 * Tl::kBytes >= 32 * DP * 4, "a wave's output rows fit its first buffer");
     __syncthreads();
     if (h == 0) {
         bases[wave][lane] = st.base;
@@ -271,8 +283,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void attention_split_kernel(AttnArgs
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const int e = 32 * i + 8 * g + 4 * h;
-            char* to = e < DP / 2 ? k0[wave] : v0[wave];
-            *(f32x4*)(to + (((lane & 31) * (DP / 2) + e % (DP / 2)) << 2)) =
+            *(f32x4*)(mine[0] + (((lane & 31) * DP + e) << 2)) =
                 (f32x4){st.o[i][4 * g], st.o[i][4 * g + 1], st.o[i][4 * g + 2], st.o[i][4 * g + 3]};
         }
     __syncthreads();
@@ -289,7 +300,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void attention_split_kernel(AttnArgs
         for (int w = 0; w < WAVES; ++w) {
             const float f = __builtin_amdgcn_exp2f(bases[w][r] - zero_of);
             sum = fmaf(totals[w][r], f, sum);
-            const f32x4 p = *(const f32x4*)((e < DP / 2 ? k0[w] : v0[w]) + ((r * (DP / 2) + e % (DP / 2)) << 2));
+            const f32x4 p = *(const f32x4*)(stage_lds<2 * Tl::kBytes * WAVES, 0>() + 2 * Tl::kBytes * w + ((r * DP + e) << 2));
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[i] = fmaf(p[i], f, o[i]);
         }
@@ -353,11 +364,11 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a)
     if (e == 0) a.lse[at] = log_sum(zero_of, sum);
 }
 
-template <typename T, int DP, int KT, int W>
+template <typename T, int DP, int KT, int WAVES, int W>
 hipError_t launch_tiles(const AttnArgs& a, hipStream_t stream)
 {
-    const int64_t rows = (int64_t)a.q_len * a.group, tiles = (rows + 127) / 128;
-    attention_kernel<T, DP, KT, W><<<dim3((unsigned)(tiles * a.batch * a.kv_heads)), 256, 0, stream>>>(a);
+    const int64_t rows = (int64_t)a.q_len * a.group, tiles = (rows + 32 * WAVES - 1) / (32 * WAVES);
+    attention_kernel<T, DP, KT, WAVES, W><<<dim3((unsigned)(tiles * a.batch * a.kv_heads)), 64 * WAVES, 0, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -396,8 +407,8 @@ hipError_t launch_attention(const AttnArgs& a, bool bf16, hipStream_t stream)
         if (bf16) return a.dim <= 64 ? launch_split<__bf16, 64, 4>(a, stream) : launch_split<__bf16, 128, 4>(a, stream);
         return a.dim <= 64 ? launch_split<float, 64, 4>(a, stream) : launch_split<float, 128, 2>(a, stream);
     }
-    if (bf16) return a.dim <= 64 ? launch_tiles<__bf16, 64, 64, 2>(a, stream) : launch_tiles<__bf16, 128, 64, 2>(a, stream);
-    return a.dim <= 64 ? launch_tiles<float, 64, 32, 2>(a, stream) : launch_tiles<float, 128, 32, 1>(a, stream);
+    if (bf16) return a.dim <= 64 ? launch_tiles<__bf16, 64, 64, 4, 3>(a, stream) : launch_tiles<__bf16, 128, 64, 4, 2>(a, stream);
+    return a.dim <= 64 ? launch_tiles<float, 64, 32, 4, 2>(a, stream) : launch_tiles<float, 128, 32, 4, 1>(a, stream);
 }
 
 }  // namespace dpb

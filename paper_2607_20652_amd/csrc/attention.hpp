@@ -282,17 +282,42 @@ struct Tile {
     };
 };
 
+// A value of a branch that few tiles take: keeps the compiler from turning the branch
+// into selects that all of them pay for.
+__device__ __forceinline__ float apart(float v)
+{
+    __asm__ volatile("" : "+v"(v));
+    return v;
+}
+
 // Waits for this wave's loads into LDS, all but the N issued last.
 template <int N>
 __device__ __forceinline__ void wait_loads()
 {
     static_assert(N < 64, "six bits count the loads in flight");
-    __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+    // (the builtin, which the compiler's own count of loads takes note of: after an asm
+    // statement it would wait once more, and for the loads just sent)
+    __asm__ volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | (N >> 4) << 14);
+    __asm__ volatile("" ::: "memory");
 }
-__device__ __forceinline__ void fill_wait() { wait_loads<0>(); }
 
 // Waits for this wave's reads of LDS (before a load is sent into what they read).
-__device__ __forceinline__ void wait_lds() { __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void wait_lds()
+{
+    __asm__ volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    __asm__ volatile("" ::: "memory");
+}
+
+// The same, then until every wave of the workgroup is here.
+template <int N>
+__device__ __forceinline__ void meet()
+{
+    wait_loads<N>();
+    __builtin_amdgcn_s_barrier();
+    __asm__ volatile("" ::: "memory");
+}
 
 // LDS of a ring's stage: an object each, so that the compiler sees that reads of
 // one and loads into another are independent.
@@ -321,9 +346,7 @@ __device__ __forceinline__ void ring(int n, F&& fill, S&& step)
         for (int s = 0; s < N; ++s) {
             if (t + s < n) {
                 wait_lds();
-                wait_loads<L * (N - 2)>();
-                __builtin_amdgcn_s_barrier();
-                __asm__ volatile("" ::: "memory");
+                meet<L*(N - 2)>();
                 fill(lds[(s + N - 1) % N], t + s + N - 1);
                 step(lds[s], t + s);
             }

@@ -125,7 +125,7 @@ __global__ __launch_bounds__(256, W) void attention_dq_kernel(AttnArgs a)
             if (edge) {
                 const int left = limit - t * KT - 32 * m - 4 * h;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) < left ? s[r] : -INFINITY;
+                for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) < left ? apart(s[r]) : -INFINITY;
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -lse2)) * dp[r];
@@ -245,7 +245,7 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int i = 8 * (r >> 2) + (r & 3);
-                s[r] = i >= need && i < left ? s[r] : -INFINITY;
+                s[r] = i >= need && i < left ? apart(s[r]) : -INFINITY;
             }
         }
 #pragma unroll
