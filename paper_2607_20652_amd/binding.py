@@ -7,7 +7,9 @@ fallback: if libdpb.so is missing the first call raises.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
+import struct
 from typing import Sequence
 
 import torch
@@ -119,7 +121,7 @@ def _dtype_code(t: torch.Tensor) -> int:
 
 
 def _stream(t: torch.Tensor):
-    return ctypes.c_void_p(torch.cuda.current_stream(t.device).cuda_stream)
+    return torch.cuda.current_stream(t.device).cuda_stream
 
 
 def _dev(t: torch.Tensor, name: str):
@@ -448,51 +450,51 @@ def std_update(plan: Plan, x: torch.Tensor, idx: torch.Tensor, stats: torch.Tens
 
 # ---- training operators beside the bottleneck: attention and AdamW
 
-class _Attn(ctypes.Structure):
-    _fields_ = [("batch", ctypes.c_int64), ("q_len", ctypes.c_int64), ("k_len", ctypes.c_int64),
-                ("q_rows", ctypes.c_int64), ("k_rows", ctypes.c_int64),
-                ("heads", ctypes.c_int), ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
-                ("causal", ctypes.c_int), ("scale", ctypes.c_float),
-                ("q_lens", ctypes.c_void_p), ("k_lens", ctypes.c_void_p),
-                ("q_starts", ctypes.c_void_p), ("k_starts", ctypes.c_void_p)]
+# dpb_attn and dpb_heads as bytes: several times quicker to make than ctypes
+# structures, which tells in a call for one token
+_ATTN = struct.Struct("=qqqqqiiiif4xQQQQ")
+_HEADS = struct.Struct("=Qqqq")
 
 
-class _Heads(ctypes.Structure):
-    _fields_ = [("data", ctypes.c_void_p), ("batch_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
-                ("head_stride", ctypes.c_int64)]
-
-
-def _heads(t: torch.Tensor, name: str):
+def _heads(t: torch.Tensor, name: str) -> bytes:
+    st = t.stride()
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
-    st = t.stride()
     if st[-1] != 1 and t.shape[-1] > 1:
         raise ValueError(f"{name} must be contiguous along head_dim")
-    return ctypes.byref(_Heads(t.data_ptr(), 0 if t.dim() == 3 else st[0], st[-3], st[-2]))
+    return _HEADS.pack(t.data_ptr(), st[0] if len(st) == 4 else 0, st[-3], st[-2])
 
 
-def _attn(q, k, v, causal, scale, q_lens, k_lens, q_starts, k_starts, max_q, max_k):
+def _index(t: torch.Tensor | None, n: int, name: str) -> int:
+    """Address of an int32 device array of n entries, or 0."""
+    if t is None:
+        return 0
+    assert t.dtype == torch.int32 and t.shape == (n,), f"{name}: int32 [{n}]"
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _attn(q, k, v, causal, scale, q_lens, k_lens, q_starts, k_starts, max_q, max_k) -> bytes:
     """The description of an attention call, its arguments checked."""
+    qs, ks = q.shape, k.shape
     packed = q_starts is not None
     assert packed == (k_starts is not None), "packed sequences need q_starts and k_starts"
-    assert q.dim() == k.dim() == (3 if packed else 4) and v.shape == k.shape and k.shape[-1] == q.shape[-1]
+    assert len(qs) == len(ks) == (3 if packed else 4) and v.shape == ks and ks[-1] == qs[-1]
     assert q.dtype == k.dtype == v.dtype
     if packed:
         assert q_lens is None and k_lens is None and max_q is not None and max_k is not None
-        batch, q_len, k_len = q_starts.shape[0] - 1, int(max_q), int(max_k)
-        assert batch >= 0 and k_starts.shape == q_starts.shape
+        batch, q_len, k_len, q_rows, k_rows = len(q_starts) - 1, int(max_q), int(max_k), qs[0], ks[0]
+        assert batch >= 0
     else:
-        batch, q_len, k_len = q.shape[0], q.shape[1], k.shape[1]
-        assert k.shape[0] == batch
-    for n in (q_lens, k_lens):
-        assert n is None or n.shape == (batch,)
-    for n in (q_lens, k_lens, q_starts, k_starts):
-        assert n is None or n.dtype == torch.int32
-    dim = q.shape[-1]
-    return _Attn(batch, q_len, k_len, q.shape[0] if packed else 0, k.shape[0] if packed else 0, q.shape[-2],
-                 k.shape[-2], dim, int(bool(causal)), dim ** -0.5 if scale is None else scale,
-                 _opt(q_lens, "q_lens"), _opt(k_lens, "k_lens"), _opt(q_starts, "q_starts"),
-                 _opt(k_starts, "k_starts"))
+        batch, q_len, k_len, q_rows, k_rows = qs[0], qs[1], ks[1], 0, 0
+        assert ks[0] == batch
+    return _ATTN.pack(batch, q_len, k_len, q_rows, k_rows, qs[-2], ks[-2], qs[-1], int(bool(causal)),
+                      qs[-1] ** -0.5 if scale is None else scale, _index(q_lens, batch, "q_lens"),
+                      _index(k_lens, batch, "k_lens"), _index(q_starts, batch + 1, "q_starts"),
+                      _index(k_starts, batch + 1, "k_starts"))
 
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = False, scale: float | None = None,
@@ -514,13 +516,12 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = 
         lse = torch.empty(q.shape[:-1], dtype=torch.float32, device=q.device)
     assert out.shape == q.shape and out.dtype == q.dtype
     assert lse.shape == q.shape[:-1] and lse.dtype == torch.float32
-    ref = ctypes.byref(a)
     lib = load()
-    need = lib.dpb_attention_workspace_bytes(ref)
+    need = lib.dpb_attention_workspace_bytes(a)
     if need and workspace is None:
         workspace = torch.empty((need + 3) // 4, dtype=torch.float32, device=q.device)
     _check("dpb_attention", lib.dpb_attention(
-        ref, _dtype_code(q), _heads(q, "q"), _heads(k, "k"), _heads(v, "v"), _heads(out, "out"), _dev(lse, "lse"),
+        a, _dtype_code(q), _heads(q, "q"), _heads(k, "k"), _heads(v, "v"), _heads(out, "out"), _dev(lse, "lse"),
         _opt(workspace, "workspace"), 0 if workspace is None else workspace.numel() * workspace.element_size(),
         _stream(q)))
     return out, lse
@@ -542,20 +543,20 @@ def attention_bwd(grad_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: t
     for x, g in ((q, dq), (k, dk), (v, dv)):
         grads.append(torch.empty(x.shape, dtype=x.dtype, device=x.device) if g is None else g)
         assert grads[-1].shape == x.shape and grads[-1].dtype == x.dtype
-    ref = ctypes.byref(a)
     lib = load()
     if workspace is None:
-        need = lib.dpb_attention_bwd_workspace_bytes(ref)
+        need = lib.dpb_attention_bwd_workspace_bytes(a)
         workspace = torch.empty((need + 3) // 4, dtype=torch.float32, device=q.device)
     dq, dk, dv = grads
     _check("dpb_attention_bwd", lib.dpb_attention_bwd(
-        ref, _dtype_code(q), _heads(grad_out, "grad_out"), _heads(q, "q"), _heads(k, "k"), _heads(v, "v"),
+        a, _dtype_code(q), _heads(grad_out, "grad_out"), _heads(q, "q"), _heads(k, "k"), _heads(v, "v"),
         _heads(out, "out"), _dev(lse, "lse"), _heads(dq, "dq"), _heads(dk, "dk"), _heads(dv, "dv"),
         _dev(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream(q)))
     return dq, dk, dv
 
 
 ADAMW_BLOCK = 256
+_KIND = operator.attrgetter("dtype", "is_cuda")
 
 
 class _AdamW(ctypes.Structure):
@@ -599,15 +600,16 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m:
     assert len(grads) == n
     if n == 0:
         return
-    sizes = [p.numel() for p in params]
-    pt, gt = params[0].dtype, grads[0].dtype
-    for p, g, k in zip(params, grads, sizes):
-        assert g.numel() == k and p.dtype == pt and g.dtype == gt
-        if not (p.is_cuda and g.is_cuda):
+    sizes = list(map(torch.Tensor.numel, params))
+    assert list(map(torch.Tensor.numel, grads)) == sizes
+    for tensors in (params, grads):
+        kinds = set(map(_KIND, tensors))
+        assert len({dtype for dtype, _ in kinds}) == 1
+        if not all(cuda for _, cuda in kinds):
             raise ValueError("params and grads must be device tensors")
-        if not (p.is_contiguous() and g.is_contiguous()):
+        if not all(map(torch.Tensor.is_contiguous, tensors)):
             raise ValueError("params and grads must be contiguous")
-    size_arr = (ctypes.c_int64 * n)(*sizes)
+    size_arr = struct.pack(f"={n}q", *sizes)
     lib = load()
     elems = lib.dpb_adamw_blocks(size_arr, n) * ADAMW_BLOCK
     state = torch.float32 if scales is None else torch.float8_e4m3fn
@@ -617,10 +619,11 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m:
     assert grad_scale is None or (grad_scale.dtype == torch.float32 and grad_scale.numel() == 1)
     decay = [weight_decay] * n if isinstance(weight_decay, (int, float)) else weight_decay
     assert len(decay) == n
-    pointers = ctypes.c_void_p * n
+    pointers = struct.Struct(f"={n}Q")
     o = _AdamW(lr, betas[0], betas[1], eps, step, seed & 0xFFFFFFFF)
     _check("dpb_adamw_step", lib.dpb_adamw_step(
-        ctypes.byref(o), n, pointers(*[p.data_ptr() for p in params]), pointers(*[g.data_ptr() for g in grads]),
-        size_arr, (ctypes.c_float * n)(*decay), _dtype_code(params[0]), _dtype_code(grads[0]),
+        ctypes.byref(o), n, pointers.pack(*map(torch.Tensor.data_ptr, params)),
+        pointers.pack(*map(torch.Tensor.data_ptr, grads)),
+        size_arr, struct.pack(f"={n}f", *decay), _dtype_code(params[0]), _dtype_code(grads[0]),
         32 if scales is None else 8, _dev(m, "m"), _dev(v, "v"), _opt(scales, "scales"), _opt(master, "master"),
         _opt(grad_scale, "grad_scale"), _stream(m)))

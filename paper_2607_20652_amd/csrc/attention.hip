@@ -391,9 +391,11 @@ int attention_splits(int batch, int q_len, int k_len, int heads, int kv_heads)
     const int64_t rows = (int64_t)q_len * (heads / kv_heads), cus = device_cus();
     const int64_t pairs = (int64_t)batch * kv_heads;
     if (rows > 32 && pairs * ((rows + 127) / 128) >= cus / 2) return 0;
-    // enough workgroups for every compute unit to be given several, of at least 256 keys each
-    const int64_t want = (8 * cus + pairs * ((rows + 31) / 32) - 1) / (pairs * ((rows + 31) / 32));
-    return (int)std::max<int64_t>(1, std::min<int64_t>(want, ((int64_t)k_len + 255) / 256));
+    // A workgroup for every compute unit if that leaves each 128 keys or more (a short call
+    // waits for latency: 16 heads, 1024 keys: 12.1 us whole, 8.3 in eight parts), and four,
+    // for an even end, if it leaves 1024 (3 x 8 heads, 131,072 keys: 350 us at two, 324 at four).
+    const int64_t units = pairs * ((rows + 31) / 32);
+    return (int)std::max<int64_t>({1, std::min(cus / units, (int64_t)k_len / 128), std::min(4 * cus / units, (int64_t)k_len / 1024)});
 }
 
 size_t attention_part_floats(int64_t q_rows, int heads, int dim, int splits)
@@ -403,12 +405,20 @@ size_t attention_part_floats(int64_t q_rows, int heads, int dim, int splits)
 
 hipError_t launch_attention(const AttnArgs& a, bool bf16, hipStream_t stream)
 {
+    const int width = (a.dim + 31) / 32;
     if (a.splits) {
-        if (bf16) return a.dim <= 64 ? launch_split<__bf16, 64, 4>(a, stream) : launch_split<__bf16, 128, 4>(a, stream);
-        return a.dim <= 64 ? launch_split<float, 64, 4>(a, stream) : launch_split<float, 128, 2>(a, stream);
+        // (as many waves as have room for two tiles each in a compute unit's LDS, up to four)
+        if (bf16)
+            return width == 1 ? launch_split<__bf16, 32, 4>(a, stream) : width == 2 ? launch_split<__bf16, 64, 4>(a, stream)
+                 : width == 3 ? launch_split<__bf16, 96, 4>(a, stream) : launch_split<__bf16, 128, 4>(a, stream);
+        return width == 1 ? launch_split<float, 32, 4>(a, stream) : width == 2 ? launch_split<float, 64, 4>(a, stream)
+             : width == 3 ? launch_split<float, 96, 2>(a, stream) : launch_split<float, 128, 2>(a, stream);
     }
-    if (bf16) return a.dim <= 64 ? launch_tiles<__bf16, 64, 64, 4, 3>(a, stream) : launch_tiles<__bf16, 128, 64, 4, 2>(a, stream);
-    return a.dim <= 64 ? launch_tiles<float, 64, 32, 4, 2>(a, stream) : launch_tiles<float, 128, 32, 4, 1>(a, stream);
+    if (bf16)
+        return width == 1 ? launch_tiles<__bf16, 32, 64, 4, 4>(a, stream) : width == 2 ? launch_tiles<__bf16, 64, 64, 4, 3>(a, stream)
+             : width == 3 ? launch_tiles<__bf16, 96, 64, 4, 2>(a, stream) : launch_tiles<__bf16, 128, 64, 4, 2>(a, stream);
+    return width == 1 ? launch_tiles<float, 32, 32, 4, 4>(a, stream) : width == 2 ? launch_tiles<float, 64, 32, 4, 2>(a, stream)
+         : width == 3 ? launch_tiles<float, 96, 32, 4, 2>(a, stream) : launch_tiles<float, 128, 32, 4, 1>(a, stream);
 }
 
 }  // namespace dpb

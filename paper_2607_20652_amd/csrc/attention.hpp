@@ -169,8 +169,8 @@ __device__ __forceinline__ void store4(char* row, int e, float a, float b, float
 
 // ---- LDS tiles
 
-// A tile of R rows of one head in LDS, DP values wide (DP: dim rounded up to 64
-// or 128), rows behind each other in 16-byte chunks.  Chunk c of row r lies at
+// A tile of R rows of one head in LDS, in rows of 64 or 128 values (DP: dim rounded
+// up to a multiple of 32, what the products use of them) and 16-byte chunks.  Chunk c of row r lies at
 // place c ^ turn(r): reading one chunk of sixteen rows, or four chunks of four
 // rows for a transposed read, then meets every bank once.  WAVES waves fill it
 // straight from global memory (no registers), 1 KB an instruction; the place a
@@ -180,7 +180,7 @@ __device__ __forceinline__ void store4(char* row, int e, float a, float b, float
 // its one row; either way no result depends on them).
 template <typename T, int DP, int R, int WAVES = 4>
 struct Tile {
-    static constexpr int kRowBytes = DP * (int)sizeof(T);
+    static constexpr int kRowBytes = (DP <= 64 ? 64 : 128) * (int)sizeof(T);
     static constexpr int kChunks = kRowBytes / 16;
     static constexpr int kBytes = R * kRowBytes;
     static constexpr int kLoads = kBytes / 1024 / WAVES;      // instructions a wave

@@ -163,8 +163,8 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
     constexpr int kSteps = DP / 16, kParts = DP / 32;
     constexpr bool kPhases = sizeof(T) == 4;
     constexpr int kStatBytes = QT * 8;
-    // The widest fp32 rows leave no registers for V: its operands come from LDS each time.
-    constexpr bool kValuesInLds = DP == 128;
+    // Wide rows leave no registers for V: its operands come from LDS each time.
+    constexpr bool kValuesInLds = DP > 64;
     typedef Tile<T, DP, 128, kWaves> Vl;
     __shared__ __align__(1024) char vt[kValuesInLds ? Vl::kBytes : 16];
     const int pairs = a.batch * a.kv_heads, bh = (int)blockIdx.x % pairs, b = bh / a.kv_heads, hk = bh % a.kv_heads;
@@ -350,8 +350,16 @@ void attention_parts(int batch, int q_len, int k_len, int heads, int kv_heads, i
 
 hipError_t launch_attention_bwd(const AttnArgs& a, bool bf16, hipStream_t stream)
 {
-    if (bf16) return a.dim <= 64 ? launch_bwd<__bf16, 64, 64, 3, 2, 64, 2, 2>(a, stream) : launch_bwd<__bf16, 128, 32, 2, 2, 32, 2, 2>(a, stream);
-    return a.dim <= 64 ? launch_bwd<float, 64, 32, 2, 2, 32, 2, 2>(a, stream) : launch_bwd<float, 128, 32, 1, 2, 32, 1, 2>(a, stream);
+    const int width = (a.dim + 31) / 32;
+    if (bf16)
+        return width == 1 ? launch_bwd<__bf16, 32, 64, 4, 2, 64, 3, 2>(a, stream)
+             : width == 2 ? launch_bwd<__bf16, 64, 64, 3, 2, 64, 2, 2>(a, stream)
+             : width == 3 ? launch_bwd<__bf16, 96, 32, 2, 2, 32, 2, 2>(a, stream)
+                          : launch_bwd<__bf16, 128, 32, 2, 2, 32, 2, 2>(a, stream);
+    return width == 1 ? launch_bwd<float, 32, 32, 2, 2, 32, 2, 2>(a, stream)
+         : width == 2 ? launch_bwd<float, 64, 32, 2, 2, 32, 2, 2>(a, stream)
+         : width == 3 ? launch_bwd<float, 96, 32, 1, 2, 32, 1, 2>(a, stream)
+                      : launch_bwd<float, 128, 32, 1, 2, 32, 1, 2>(a, stream);
 }
 
 }  // namespace dpb
