@@ -76,8 +76,8 @@ dpb_status take(const dpb_attn* a, dpb_dtype t, const dpb_heads* x, bool q, Attn
     return out->ts >= kMaxTokenBytes ? DPB_EUNSUPPORTED : DPB_OK;
 }
 
-// The backward's two floats per query row and head, before its parts.
-size_t stats_bytes(const dpb_attn* a) { return ((size_t)rows_of(a, true) * a->heads * 8 + 15) / 16 * 16; }
+// One float per query row and head (the backward has two arrays of them, before its parts).
+size_t row_bytes(const dpb_attn* a) { return ((size_t)rows_of(a, true) * a->heads * 4 + 15) / 16 * 16; }
 
 void fill_args(const dpb_attn* a, AttnArgs* g)
 {
@@ -117,7 +117,7 @@ size_t dpb_attention_bwd_workspace_bytes(const dpb_attn* a)
     dpb::attention_parts((int)a->batch, (int)a->q_len, (int)a->k_len, a->heads, a->kv_heads, &q_parts, &k_parts);
     const size_t dq = q_parts > 1 ? (size_t)q_parts * rows_of(a, true) * a->heads : 0;
     const size_t dkv = k_parts > 1 ? (size_t)k_parts * rows_of(a, false) * a->kv_heads * 2 : 0;
-    return stats_bytes(a) + std::max(dq, dkv) * a->head_dim * 4;
+    return 2 * row_bytes(a) + std::max(dq, dkv) * a->head_dim * 4;
 }
 
 dpb_status dpb_attention(const dpb_attn* a, dpb_dtype dtype, const dpb_heads* q, const dpb_heads* k,
@@ -172,8 +172,9 @@ dpb_status dpb_attention_bwd(const dpb_attn* a, dpb_dtype dtype, const dpb_heads
             if (outs[i] && outs[i] == outs[j]) return DPB_EINVAL;
     }
     g.lse = const_cast<float*>(lse);
-    g.row_stats = (float*)workspace;
-    g.part = (float*)((char*)workspace + stats_bytes(a));
+    g.row_lse2 = (float*)workspace;
+    g.row_delta = (float*)((char*)workspace + row_bytes(a));
+    g.part = (float*)((char*)workspace + 2 * row_bytes(a));
     dpb::attention_parts(g.batch, g.q_len, g.k_len, g.heads, g.kv_heads, &g.q_parts, &g.k_parts);
     return launched(dpb::launch_attention_bwd(g, dtype == DPB_BF16, (hipStream_t)stream));
 }

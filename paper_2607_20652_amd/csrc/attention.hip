@@ -161,10 +161,14 @@ __global__ __launch_bounds__(64 * WAVES, W) void attention_kernel(AttnArgs a)
     const float c = a.scale * kLog2e;
     const int n = (seen + KT - 1) / KT;
     const typename Tl::Fill kfill(a.k.ts, a.dim, wave), vfill(a.v.ts, a.dim, wave);
+    int left = sq.kn;
     auto fill = [&](char* lds, int t) {
-        const int left = t < n ? sq.kn - t * KT : 0;
-        kfill(lds, kb + (int64_t)t * KT * a.k.ts, left, wave);
-        vfill(lds + Tl::kBytes, vb + (int64_t)t * KT * a.v.ts, left, wave);
+        if (t >= n) left = 0;
+        kfill(lds, kb, left, wave);
+        vfill(lds + Tl::kBytes, vb, left, wave);
+        kb += KT * a.k.ts;
+        vb += KT * a.v.ts;
+        left -= KT;
     };
     auto step = [&](const char* lds, int t) {
 #pragma unroll

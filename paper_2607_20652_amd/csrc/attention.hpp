@@ -35,7 +35,8 @@ struct AttnArgs {
     AttnRows q, k, v, o;             // o: written by the forward, read by the backward
     AttnRows go, gq, gk, gv;         // backward: gradient of o (read), of q, k, v (written)
     float* lse;                      // [query rows, heads]
-    float* row_stats;                // backward scratch [heads][query rows][2]: lse * log2(e), sum_d go * o
+    float* row_lse2;                 // backward scratch [heads][query rows]: lse * log2(e)
+    float* row_delta;                // and -sum_d go * o
     float* part;                     // scratch of a split call.  Forward: [query rows][heads][splits][4 + dim]
                                      // (base, sum, -, -, output); backward: [parts][rows][heads][dim]
     const int32_t *q_lens, *k_lens;      // padded: lengths, or null

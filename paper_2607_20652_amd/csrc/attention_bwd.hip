@@ -91,25 +91,28 @@ __global__ __launch_bounds__(256, W) void attention_dq_kernel(AttnArgs a)
     // a row that sees nothing: no score comes near its sum
     const float lse2 = limit > 0 ? a.lse[(sq.q0 + token) * a.heads + head] * kLog2e : INFINITY;
     if (valid && h == 0 && part == 0) {
-        dpb_f32x2 stats = {lse2, delta};
-        *(dpb_f32x2*)(a.row_stats + 2 * (head * a.q_rows + sq.q0 + token)) = stats;
+        a.row_lse2[head * a.q_rows + sq.q0 + token] = lse2;
+        a.row_delta[head * a.q_rows + sq.q0 + token] = -delta;
     }
 
     f32x16 dq[kParts];
 #pragma unroll
     for (int i = 0; i < kParts; ++i) fill16(dq[i], 0.f);
-    const char* kb = head_base(a.k, a.k_starts, b, sq.k0, hk);
-    const char* vb = head_base(a.v, a.k_starts, b, sq.k0, hk);
     const float c = a.scale * kLog2e;
     typename Tl::Reader rd;
     const int all = (seen + KT - 1) / KT, begin = (int)((int64_t)all * part / a.q_parts);
     const int n = (int)((int64_t)all * (part + 1) / a.q_parts) - begin;
     const typename Tl::Fill kfill(a.k.ts, a.dim, wave), vfill(a.v.ts, a.dim, wave);
+    const char* kp = head_base(a.k, a.k_starts, b, sq.k0, hk) + (int64_t)begin * KT * a.k.ts;
+    const char* vp = head_base(a.v, a.k_starts, b, sq.k0, hk) + (int64_t)begin * KT * a.v.ts;
+    int left = sq.kn - begin * KT;
     auto fill = [&](char* lds, int t) {
-        const int left = t < n ? sq.kn - (begin + t) * KT : 0;
-        t += begin;
-        kfill(lds, kb + (int64_t)t * KT * a.k.ts, left, wave);
-        vfill(lds + Tl::kBytes, vb + (int64_t)t * KT * a.v.ts, left, wave);
+        if (t >= n) left = 0;
+        kfill(lds, kp, left, wave);
+        vfill(lds + Tl::kBytes, vp, left, wave);
+        kp += KT * a.k.ts;
+        vp += KT * a.v.ts;
+        left -= KT;
     };
     auto products = [&](const char* kt, const char* vt, int t, bool edge) {
 #pragma unroll
@@ -162,7 +165,7 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
     typedef typename Operand<T>::type Op;
     constexpr int kSteps = DP / 16, kParts = DP / 32;
     constexpr bool kPhases = sizeof(T) == 4;
-    constexpr int kStatBytes = QT * 8;
+    static_assert(QT <= 64, "one load each brings the tile's row values");
     // Wide rows leave no registers for V: its operands come from LDS each time.
     constexpr bool kValuesInLds = DP > 64;
     typedef Tile<T, DP, 128, kWaves> Vl;
@@ -205,31 +208,40 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
     const float c = a.scale * kLog2e;
     typename Tl::Reader rd;
     const typename Tl::Fill qfill(a.q.ts, a.dim, wave), gfill(a.go.ts, a.dim, wave);
+    // what is loaded next: of which head of the group, from which token
+    int head = per_head ? begin / per_head : 0, tok = from + (per_head ? begin % per_head * QT : 0);
+    int step_tok = tok;
+    const char *qp = head_base(a.q, a.q_starts, b, sq.q0, hk * a.group + head), *gp = head_base(a.go, a.q_starts, b, sq.q0, hk * a.group + head);
     auto fill = [&](char* lds, int t) {
-        const int u = begin + min(t, n - 1), head = hk * a.group + u / per_head, tok = from + (u % per_head) * QT;
         const int left = t < n ? sq.qn - tok : 0;
-        qfill(lds, head_base(a.q, a.q_starts, b, sq.q0, head) + (int64_t)tok * a.q.ts, left, wave);
-        gfill(lds + Tl::kBytes, head_base(a.go, a.q_starts, b, sq.q0, head) + (int64_t)tok * a.go.ts, left, wave);
+        qfill(lds, qp + (int64_t)tok * a.q.ts, left, wave);
+        gfill(lds + Tl::kBytes, gp + (int64_t)tok * a.go.ts, left, wave);
         // the rows' two values each, by every wave alike
-        const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(
-            (void*)(a.row_stats + 2 * (head * a.q_rows + sq.q0 + tok)), 0, min(left, QT) * 8, 0x00027000);
-#pragma unroll
-        for (int i = 0; i < kStatBytes; i += 256)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lds_void*)(lds + 2 * Tl::kBytes + i), 4, lane * 4 + i, 0, 0, 0);
+        const int64_t at = (hk * a.group + head) * a.q_rows + sq.q0 + tok;
+        const __amdgpu_buffer_rsrc_t l = __builtin_amdgcn_make_buffer_rsrc((void*)(a.row_lse2 + at), 0, min(left, QT) * 4, 0x00027000);
+        const __amdgpu_buffer_rsrc_t d = __builtin_amdgcn_make_buffer_rsrc((void*)(a.row_delta + at), 0, min(left, QT) * 4, 0x00027000);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(l, (lds_void*)(lds + 2 * Tl::kBytes), 4, lane * 4, 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(d, (lds_void*)(lds + 2 * Tl::kBytes + 256), 4, lane * 4, 0, 0, 0);
+        tok += QT;
+        if (tok >= sq.qn) {
+            tok = from;
+            ++head;
+            qp += a.q.hs;
+            gp += a.go.hs;
+        }
     };
     // rows at..at+31 of a tile, the first of them `tok` of the sequence
     auto products = [&](const char* qt, const char* gt, const char* stats, int at, int tok, bool edge) {
         f32x16 s, dp;
         rd.fresh();
         fill16(s, 0.f);
-        float l[16];
+        f32x4 l[4];
 #pragma unroll
-        for (int r = 0; r < 16; r += 2) {
-            const f32x4 x = *(const f32x4*)(stats + (at + 8 * (r >> 2) + (r & 3) + 4 * h) * 8);
-            l[r] = x[0];
-            dp[r] = -x[1];
-            l[r + 1] = x[2];
-            dp[r + 1] = -x[3];
+        for (int g = 0; g < 4; ++g) {
+            l[g] = *(const f32x4*)(stats + (at + 8 * g + 4 * h) * 4);
+            const f32x4 d = *(const f32x4*)(stats + 256 + (at + 8 * g + 4 * h) * 4);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) dp[4 * g + j] = d[j];
         }
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) s = mma(rd.rows(qt, at, i), k[i], s);
@@ -250,7 +262,7 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -l[r]));
+            s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -l[r >> 2][r & 3]));
             dp[r] *= s[r];
         }
 #pragma unroll
@@ -266,16 +278,17 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
     };
     auto step = [&](const char* qt, int t) {
         const char *gt = qt + Tl::kBytes, *stats = gt + Tl::kBytes;
-        const int tok = from + ((begin + t) % per_head) * QT;
         const int key_first = tile * 128 + wave * 32;
 #pragma unroll
         for (int at = 0; at < QT; at += 32) {
-            const int first = tok + at;
+            const int first = step_tok + at;
             if ((a.causal && first + 31 + behind < key_first) || first >= sq.qn) continue;   // nothing to see
             products(qt, gt, stats, at, first, (a.causal && key_first + 31 > first + behind) || first + 32 > sq.qn);
         }
+        step_tok += QT;
+        if (step_tok >= sq.qn) step_tok = from;
     };
-    ring<NS, 2 * Tl::kLoads + kStatBytes / 256, 2 * Tl::kBytes + kStatBytes>(n, fill, step);
+    ring<NS, 2 * Tl::kLoads + 2, 2 * Tl::kBytes + 512>(n, fill, step);
 
     if (key >= sq.kw) return;
     if (a.k_parts > 1) {
