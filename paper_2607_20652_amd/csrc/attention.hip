@@ -149,13 +149,6 @@ __global__ __launch_bounds__(64 * WAVES, W) void attention_kernel(AttnArgs a)
     const int wave_last = min((tile * kRows + wave * 32 + 31) / a.group, sq.qn - 1);
     const int most = wave_last >= 0 ? visible_keys(a, sq, wave_last) : 0;
 
-    Rows<T, DP> st;
-    st.clear();
-    typename Tl::Reader rd;
-    const char* qrow = head_base(a.q, a.q_starts, b, sq.q0, head) + (int64_t)token * a.q.ts;
-#pragma unroll
-    for (int i = 0; i < DP / 16; ++i) st.q[i] = global_operand<T>(qrow, i, a.dim, valid);
-
     const char* kb = head_base(a.k, a.k_starts, b, sq.k0, hk);
     const char* vb = head_base(a.v, a.k_starts, b, sq.k0, hk);
     const float c = a.scale * kLog2e;
@@ -170,6 +163,14 @@ __global__ __launch_bounds__(64 * WAVES, W) void attention_kernel(AttnArgs a)
         vb += KT * a.v.ts;
         left -= KT;
     };
+    begin_ring<2, 2 * Tl::kBytes>(n, fill);
+    Rows<T, DP> st;
+    st.clear();
+    typename Tl::Reader rd;
+    const char* qrow = head_base(a.q, a.q_starts, b, sq.q0, head) + (int64_t)token * a.q.ts;
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i) st.q[i] = global_operand<T>(qrow, i, a.dim, valid);
+
     auto step = [&](const char* lds, int t) {
 #pragma unroll
         for (int at = 0; at < KT; at += 64) {
@@ -185,21 +186,14 @@ __global__ __launch_bounds__(64 * WAVES, W) void attention_kernel(AttnArgs a)
     };
     ring<2, 2 * Tl::kLoads, 2 * Tl::kBytes>(n, fill, step);
 
-    const float total = st.total();
-    if (token >= sq.qw) return;
-    const float inv = inverse(total);
-    char* out = head_base(a.o, a.q_starts, b, sq.q0, head) + (int64_t)token * a.o.ts;
-    const int h = lane >> 5;
-#pragma unroll
-    for (int i = 0; i < DP / 32; ++i)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int e = 32 * i + 8 * g + 4 * h;
-            if (e < a.dim)
-                store4<T>(out, e, st.o[i][4 * g] * inv, st.o[i][4 * g + 1] * inv, st.o[i][4 * g + 2] * inv,
-                          st.o[i][4 * g + 3] * inv);
-        }
-    if (h == 0) a.lse[(sq.q0 + token) * a.heads + head] = log_sum(st.base, total);
+    const float total = st.total(), inv = inverse(total);
+    if (lane < 32 && token < sq.qw) a.lse[(sq.q0 + token) * a.heads + head] = log_sum(st.base, total);
+    static_assert(2 * Tl::kBytes >= WAVES * kStoreBytes, "a stage holds what the waves store");
+    __syncthreads();
+    store_rows<T, DP>(stage_lds<2 * Tl::kBytes, 0>() + wave * kStoreBytes, st.o, inv, inv != 0.f, a.dim, [&](int r) {
+        const int x = tile * kRows + wave * 32 + r, tok = x / a.group;
+        return tok < sq.qw ? head_base(a.o, a.q_starts, b, sq.q0, hk * a.group + x % a.group) + (int64_t)tok * a.o.ts : nullptr;
+    });
 }
 
 // Few rows against many keys: one workgroup takes 32 rows and one of the call's

@@ -160,12 +160,47 @@ __device__ __forceinline__ typename Operand<T>::type global_operand(const char* 
     return v;
 }
 
-// Four values of column `lane % 32` of a result, as values 8g + 4h.. of a row.
+// Four values of a row, from element e.
 template <typename T>
 __device__ __forceinline__ void store4(char* row, int e, float a, float b, float c, float d)
 {
     if constexpr (sizeof(T) == 2) *(u32x2*)(row + e * 2) = (u32x2){pack_bf16x2(a, b), pack_bf16x2(c, d)};
     else *(f32x4*)(row + e * 4) = (f32x4){a, b, c, d};
+}
+
+// Stores a wave's transposed result, its columns as 32 rows of dim values: this lane's
+// column times f, or zeros unless `live`.  to(r) is where row r goes, or null.  A lane
+// holds four values here and there of one row; through 4 KB of LDS (the wave's own) a row
+// leaves in whole lines, not in pieces of eight or sixteen bytes (dK and dV of 16 x 1024
+// tokens: 108 -> 102 us).
+constexpr int kStoreBytes = 4096;
+template <typename T, int DP, typename F>
+__device__ __forceinline__ void store_rows(char* lds, const f32x16 (&c)[DP / 32], float f, bool live, int dim, F&& to)
+{
+    constexpr int kEach = sizeof(T) == 2 ? 2 : 1;   // 32-value parts of a line of 128 bytes
+    const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int p = 0; p < DP / 32; p += kEach) {
+        wave_sync();
+#pragma unroll
+        for (int i = p; i < p + kEach && i < DP / 32; ++i)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int e = 32 * (i - p) + 8 * g + 4 * h, byte = e * (int)sizeof(T);
+                char* at = lds + r * 128 + (((byte >> 4) ^ (r & 7)) << 4 | (byte & 15));
+                store4<T>(at, 0, live ? c[i][4 * g] * f : 0.f, live ? c[i][4 * g + 1] * f : 0.f, live ? c[i][4 * g + 2] * f : 0.f,
+                          live ? c[i][4 * g + 3] * f : 0.f);
+            }
+        wave_sync();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int row = 8 * k + (lane >> 3), chunk = lane & 7;
+            const int byte = p * 32 * (int)sizeof(T) + chunk * 16;
+            char* out = to(row);
+            if (out && byte < dim * (int)sizeof(T) && (p * 32 * (int)sizeof(T) + 128 <= DP * (int)sizeof(T) || chunk * 16 < (DP - p * 32) * (int)sizeof(T)))
+                *(u32x4*)(out + byte) = *(const u32x4*)(lds + row * 128 + ((chunk ^ (row & 7)) << 4));
+        }
+    }
 }
 
 // ---- LDS tiles
@@ -332,24 +367,37 @@ __device__ __forceinline__ char* stage_lds()
 // Steps 0..n-1 of a workgroup, the loads of each sent N - 1 steps ahead.
 // fill(lds, t) enqueues exactly L loads a wave (of nothing, where t >= n); step(lds,
 // t) uses them.  Before a step every wave has waited for its part of the stage and is
-// done with the step before, whose stage the loads sent next go into.
-template <int N, int L, int BYTES, typename F, typename S>
-__device__ __forceinline__ void ring(int n, F&& fill, S&& step)
-{
+// done with the step before, whose stage the loads sent next go into.  begin_ring() sends the
+// first loads; what else a kernel loads up front then comes in beside them.
+template <int N, int BYTES>
+struct Stages {
     static_assert(N >= 2 && N <= 5, "stages");
     char* const lds[5] = {stage_lds<BYTES, 0>(), stage_lds<BYTES, 1>(), stage_lds<BYTES, (N > 2 ? 2 : 0)>(),
                           stage_lds<BYTES, (N > 3 ? 3 : 0)>(), stage_lds<BYTES, (N > 4 ? 4 : 0)>()};
+};
+
+template <int N, int BYTES, typename F>
+__device__ __forceinline__ void begin_ring(int n, F&& fill)
+{
+    const Stages<N, BYTES> st;
     if (n <= 0) return;
 #pragma unroll
-    for (int s = 0; s < N - 1; ++s) fill(lds[s], s);
+    for (int s = 0; s < N - 1; ++s) fill(st.lds[s], s);
+}
+
+template <int N, int L, int BYTES, typename F, typename S>
+__device__ __forceinline__ void ring(int n, F&& fill, S&& step)
+{
+    const Stages<N, BYTES> st;
+    if (n <= 0) return;
     for (int t = 0; t < n; t += N) {
 #pragma unroll
         for (int s = 0; s < N; ++s) {
             if (t + s < n) {
                 wait_lds();
                 meet<L*(N - 2)>();
-                fill(lds[(s + N - 1) % N], t + s + N - 1);
-                step(lds[s], t + s);
+                fill(st.lds[(s + N - 1) % N], t + s + N - 1);
+                step(st.lds[s], t + s);
             }
         }
     }

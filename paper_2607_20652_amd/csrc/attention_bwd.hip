@@ -25,22 +25,6 @@ __device__ __forceinline__ void fill16(f32x16& c, float v)
     for (int r = 0; r < 16; ++r) c[r] = v;
 }
 
-// This lane's column of a transposed result, times f, as a row; zeros unless `live`.
-template <typename T, int DP>
-__device__ __forceinline__ void store_rows(char* row, int dim, const f32x16 (&c)[DP / 32], float f, bool live)
-{
-    const int h = (threadIdx.x & 63) >> 5;
-#pragma unroll
-    for (int i = 0; i < DP / 32; ++i)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int e = 32 * i + 8 * g + 4 * h;
-            if (e >= dim) continue;
-            if (live) store4<T>(row, e, c[i][4 * g] * f, c[i][4 * g + 1] * f, c[i][4 * g + 2] * f, c[i][4 * g + 3] * f);
-            else store4<T>(row, e, 0.f, 0.f, 0.f, 0.f);
-        }
-}
-
 // fp32 operands take twice the registers: there the products' LDS reads stay in
 // their own phase, or the compiler, which issues them early, runs out of registers.
 template <bool ON>
@@ -74,6 +58,24 @@ __global__ __launch_bounds__(256, W) void attention_dq_kernel(AttnArgs a)
     const int wave_last = min((tile * 128 + wave * 32 + 31) / a.group, sq.qn - 1);
     const int most = wave_last >= 0 ? visible_keys(a, sq, wave_last) : 0;
 
+    const float c = a.scale * kLog2e;
+    typename Tl::Reader rd;
+    const int all = (seen + KT - 1) / KT, begin = (int)((int64_t)all * part / a.q_parts);
+    const int n = (int)((int64_t)all * (part + 1) / a.q_parts) - begin;
+    const typename Tl::Fill kfill(a.k.ts, a.dim, wave), vfill(a.v.ts, a.dim, wave);
+    const char* kp = head_base(a.k, a.k_starts, b, sq.k0, hk) + (int64_t)begin * KT * a.k.ts;
+    const char* vp = head_base(a.v, a.k_starts, b, sq.k0, hk) + (int64_t)begin * KT * a.v.ts;
+    int left = sq.kn - begin * KT;
+    auto fill = [&](char* lds, int t) {
+        if (t >= n) left = 0;
+        kfill(lds, kp, left, wave);
+        vfill(lds + Tl::kBytes, vp, left, wave);
+        kp += KT * a.k.ts;
+        vp += KT * a.v.ts;
+        left -= KT;
+    };
+    begin_ring<NS, 2 * Tl::kBytes>(n, fill);
+
     const char* qrow = head_base(a.q, a.q_starts, b, sq.q0, head) + (int64_t)token * a.q.ts;
     const char* grow = head_base(a.go, a.q_starts, b, sq.q0, head) + (int64_t)token * a.go.ts;
     const char* orow = head_base(a.o, a.q_starts, b, sq.q0, head) + (int64_t)token * a.o.ts;
@@ -98,22 +100,6 @@ __global__ __launch_bounds__(256, W) void attention_dq_kernel(AttnArgs a)
     f32x16 dq[kParts];
 #pragma unroll
     for (int i = 0; i < kParts; ++i) fill16(dq[i], 0.f);
-    const float c = a.scale * kLog2e;
-    typename Tl::Reader rd;
-    const int all = (seen + KT - 1) / KT, begin = (int)((int64_t)all * part / a.q_parts);
-    const int n = (int)((int64_t)all * (part + 1) / a.q_parts) - begin;
-    const typename Tl::Fill kfill(a.k.ts, a.dim, wave), vfill(a.v.ts, a.dim, wave);
-    const char* kp = head_base(a.k, a.k_starts, b, sq.k0, hk) + (int64_t)begin * KT * a.k.ts;
-    const char* vp = head_base(a.v, a.k_starts, b, sq.k0, hk) + (int64_t)begin * KT * a.v.ts;
-    int left = sq.kn - begin * KT;
-    auto fill = [&](char* lds, int t) {
-        if (t >= n) left = 0;
-        kfill(lds, kp, left, wave);
-        vfill(lds + Tl::kBytes, vp, left, wave);
-        kp += KT * a.k.ts;
-        vp += KT * a.v.ts;
-        left -= KT;
-    };
     auto products = [&](const char* kt, const char* vt, int t, bool edge) {
 #pragma unroll
         for (int m = 0; m < KT / 32; ++m) {
@@ -148,12 +134,21 @@ __global__ __launch_bounds__(256, W) void attention_dq_kernel(AttnArgs a)
     };
     ring<NS, 2 * Tl::kLoads, 2 * Tl::kBytes>(n, fill, step);
 
-    if (token >= sq.qw) return;
-    if (a.q_parts > 1) {
-        store_rows<float, DP>((char*)(a.part + ((part * a.q_rows + sq.q0 + token) * a.heads + head) * a.dim), a.dim, dq, 1.f, limit > 0);
-        return;
-    }
-    store_rows<T, DP>(head_base(a.gq, a.q_starts, b, sq.q0, head) + (int64_t)token * a.gq.ts, a.dim, dq, a.scale, limit > 0);
+    static_assert(2 * Tl::kBytes >= kWaves * kStoreBytes, "a stage holds what the waves store");
+    char* const lds = stage_lds<2 * Tl::kBytes, 0>() + wave * kStoreBytes;
+    auto place = [&](int r, auto&& at) {
+        const int x = tile * 128 + wave * 32 + r, tok = x / a.group;
+        return tok < sq.qw ? at(tok, hk * a.group + x % a.group) : nullptr;
+    };
+    __syncthreads();
+    if (a.q_parts > 1)
+        store_rows<float, DP>(lds, dq, 1.f, limit > 0, a.dim, [&](int r) {
+            return place(r, [&](int tok, int hd) { return (char*)(a.part + ((part * a.q_rows + sq.q0 + tok) * a.heads + hd) * a.dim); });
+        });
+    else
+        store_rows<T, DP>(lds, dq, a.scale, limit > 0, a.dim, [&](int r) {
+            return place(r, [&](int tok, int hd) { return head_base(a.gq, a.q_starts, b, sq.q0, hd) + (int64_t)tok * a.gq.ts; });
+        });
 }
 
 // dK and dV of 128 keys of one key head: the queries of every head that shares it
@@ -179,24 +174,6 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
 
     const int key = tile * 128 + wave * 32 + (lane & 31);
     const bool valid = key < sq.kn;
-    const char* krow = head_base(a.k, a.k_starts, b, sq.k0, hk) + (int64_t)key * a.k.ts;
-    const char* vrow = head_base(a.v, a.k_starts, b, sq.k0, hk) + (int64_t)key * a.v.ts;
-    Op k[kSteps], v[kValuesInLds ? 1 : kSteps];
-#pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-        k[i] = global_operand<T>(krow, i, a.dim, valid);
-        if constexpr (!kValuesInLds) v[i] = global_operand<T>(vrow, i, a.dim, valid);
-    }
-    if constexpr (kValuesInLds)
-        typename Vl::Fill(a.v.ts, a.dim, wave)(vt, head_base(a.v, a.k_starts, b, sq.k0, hk) + (int64_t)tile * 128 * a.v.ts,
-                                               sq.kn - tile * 128, wave);
-    f32x16 dk[kParts], dv[kParts];
-#pragma unroll
-    for (int i = 0; i < kParts; ++i) {
-        fill16(dk[i], 0.f);
-        fill16(dv[i], 0.f);
-    }
-
     // Query `token` sees this lane's key if token >= first_token; the tiles from the
     // first token that sees any key of the workgroup on, once per head of the group.
     const int behind = a.causal ? sq.kn - sq.qn : (1 << 30);
@@ -230,6 +207,26 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
             gp += a.go.hs;
         }
     };
+    begin_ring<NS, 2 * Tl::kBytes + 512>(n, fill);
+
+    const char* krow = head_base(a.k, a.k_starts, b, sq.k0, hk) + (int64_t)key * a.k.ts;
+    const char* vrow = head_base(a.v, a.k_starts, b, sq.k0, hk) + (int64_t)key * a.v.ts;
+    Op k[kSteps], v[kValuesInLds ? 1 : kSteps];
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+        k[i] = global_operand<T>(krow, i, a.dim, valid);
+        if constexpr (!kValuesInLds) v[i] = global_operand<T>(vrow, i, a.dim, valid);
+    }
+    if constexpr (kValuesInLds)
+        typename Vl::Fill(a.v.ts, a.dim, wave)(vt, head_base(a.v, a.k_starts, b, sq.k0, hk) + (int64_t)tile * 128 * a.v.ts,
+                                               sq.kn - tile * 128, wave);
+    f32x16 dk[kParts], dv[kParts];
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) {
+        fill16(dk[i], 0.f);
+        fill16(dv[i], 0.f);
+    }
+
     // rows at..at+31 of a tile, the first of them `tok` of the sequence
     auto products = [&](const char* qt, const char* gt, const char* stats, int at, int tok, bool edge) {
         f32x16 s, dp;
@@ -290,15 +287,24 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
     };
     ring<NS, 2 * Tl::kLoads + 2, 2 * Tl::kBytes + 512>(n, fill, step);
 
-    if (key >= sq.kw) return;
+    static_assert(2 * Tl::kBytes + 512 >= kWaves * kStoreBytes, "a stage holds what the waves store");
+    char* const lds = stage_lds<2 * Tl::kBytes + 512, 0>() + wave * kStoreBytes;
+    const int first = tile * 128 + wave * 32;
+    __syncthreads();
     if (a.k_parts > 1) {
-        const int64_t at = ((part * a.k_rows + sq.k0 + key) * a.kv_heads + hk) * a.dim;
-        store_rows<float, DP>((char*)(a.part + at), a.dim, dk, 1.f, valid);
-        store_rows<float, DP>((char*)(a.part + a.k_parts * a.k_rows * a.kv_heads * a.dim + at), a.dim, dv, 1.f, valid);
-        return;
+        float* const sum = a.part + ((part * a.k_rows + sq.k0 + first) * a.kv_heads + hk) * a.dim;
+        const int64_t values = a.k_parts * a.k_rows * a.kv_heads * a.dim;
+        auto place = [&](float* p) { return [=, &a](int r) { return first + r < sq.kw ? (char*)(p + (int64_t)r * a.kv_heads * a.dim) : nullptr; }; };
+        store_rows<float, DP>(lds, dk, 1.f, valid, a.dim, place(sum));
+        store_rows<float, DP>(lds, dv, 1.f, valid, a.dim, place(sum + values));
+    } else {
+        auto place = [&](const AttnRows& t) {
+            char* const p = head_base(t, a.k_starts, b, sq.k0, hk) + (int64_t)first * t.ts;
+            return [=, &t](int r) { return first + r < sq.kw ? p + (int64_t)r * t.ts : nullptr; };
+        };
+        store_rows<T, DP>(lds, dk, a.scale, valid, a.dim, place(a.gk));
+        store_rows<T, DP>(lds, dv, 1.f, valid, a.dim, place(a.gv));
     }
-    store_rows<T, DP>(head_base(a.gk, a.k_starts, b, sq.k0, hk) + (int64_t)key * a.gk.ts, a.dim, dk, a.scale, valid);
-    store_rows<T, DP>(head_base(a.gv, a.k_starts, b, sq.k0, hk) + (int64_t)key * a.gv.ts, a.dim, dv, 1.f, valid);
 }
 
 // Adds up the parts of dQ, or of dK and dV, in their order: four elements a lane.
