@@ -21,6 +21,11 @@
 and RMSNorm, the position the paper's ParityTransformer gives it (§3.1: a
 bottleneck before the input to every MLP).  The MLP's matrices are ordinary
 torch layers; everything of the DPB itself runs in libdpb.so.
+
+`AttentionLayer.apply(q, k, v, causal, scale, q_lens, k_lens)` is softmax
+attention as a differentiable function (dpb_attention, dpb_attention_bwd);
+`CausalAttention` the sublayer around it, with a key-value cache for generation,
+and `ParityBlock` the two sublayers of one transformer block.
 """
 from __future__ import annotations
 
@@ -118,3 +123,90 @@ class DPBMLP(torch.nn.Module):
         y, loss_var = DPBLayer.apply(z, self.plan, self.normalized, self.n_min, self.std)
         out = h + self.fc2(torch.nn.functional.gelu(self.fc1(y))).reshape(shape)
         return out, loss_var
+
+
+class AttentionLayer(torch.autograd.Function):
+    """Attention of padded sequences, q [B, Sq, H, D], k and v [B, Sk, Hkv, D] -> [B, Sq, H, D];
+    the backward recomputes the probabilities from the log-sum-exp."""
+
+    @staticmethod
+    def forward(ctx, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = False,
+                scale: float | None = None, q_lens: torch.Tensor | None = None, k_lens: torch.Tensor | None = None):
+        out, lse = B.attention(q, k, v, causal, scale, q_lens, k_lens)
+        ctx.causal, ctx.scale = causal, scale
+        ctx.save_for_backward(q, k, v, out, lse, q_lens, k_lens)
+        return out
+
+    @staticmethod
+    def backward(ctx, grad: torch.Tensor):
+        q, k, v, out, lse, q_lens, k_lens = ctx.saved_tensors
+        if grad.stride() != out.stride():   # an expanded gradient, say
+            grad = grad.contiguous()
+        dq, dk, dv = B.attention_bwd(grad, q, k, v, out, lse, ctx.causal, ctx.scale, q_lens, k_lens)
+        return dq, dk, dv, None, None, None, None
+
+
+def attention_layer(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = False,
+                    scale: float | None = None, q_lens: torch.Tensor | None = None,
+                    k_lens: torch.Tensor | None = None):
+    """Functional form of AttentionLayer."""
+    return AttentionLayer.apply(q, k, v, causal, scale, q_lens, k_lens)
+
+
+class KeyValueCache:
+    """Keys and values of up to `length` tokens of `batch` sequences for one attention sublayer."""
+
+    def __init__(self, batch: int, length: int, kv_heads: int, head_dim: int, dtype: torch.dtype, device=None):
+        self.k = torch.zeros(batch, length, kv_heads, head_dim, dtype=dtype, device=device)
+        self.v = torch.zeros_like(self.k)
+        self.used = 0
+
+    def append(self, k: torch.Tensor, v: torch.Tensor):
+        """Adds the tokens' keys and values; all of them so far, as views."""
+        end = self.used + k.shape[1]
+        if end > self.k.shape[1]:
+            raise ValueError(f"the cache holds {self.k.shape[1]} tokens, not {end}")
+        self.k[:, self.used:end], self.v[:, self.used:end] = k, v
+        self.used = end
+        return self.k[:, :end], self.v[:, :end]
+
+
+class CausalAttention(torch.nn.Module):
+    """h + W_o attention(rmsnorm(h)), queries, keys and values from one projection; `kv_heads`
+    key heads are shared by `heads` query heads.  With a cache, h holds the tokens behind
+    those in it."""
+
+    def __init__(self, d: int, heads: int, kv_heads: int | None = None, dtype: torch.dtype = torch.float32, device=None):
+        super().__init__()
+        self.heads, self.kv_heads, self.head_dim = heads, kv_heads or heads, d // heads
+        if self.head_dim * heads != d:
+            raise ValueError(f"{heads} heads do not divide a width of {d}")
+        self.norm = torch.nn.RMSNorm(d, dtype=dtype, device=device)
+        self.qkv = torch.nn.Linear(d, (heads + 2 * self.kv_heads) * self.head_dim, bias=False, dtype=dtype, device=device)
+        self.out = torch.nn.Linear(d, d, bias=False, dtype=dtype, device=device)
+
+    def forward(self, h: torch.Tensor, cache: KeyValueCache | None = None):
+        x = self.qkv(self.norm(h)).unflatten(-1, (-1, self.head_dim))
+        q, k, v = x.split((self.heads, self.kv_heads, self.kv_heads), dim=2)   # views of one tensor
+        if cache is not None:
+            k, v = cache.append(k, v)
+        y = AttentionLayer.apply(q, k, v, True)
+        return h + self.out(y.flatten(-2))
+
+    def cache(self, batch: int, length: int) -> KeyValueCache:
+        w = self.qkv.weight
+        return KeyValueCache(batch, length, self.kv_heads, self.head_dim, w.dtype, w.device)
+
+
+class ParityBlock(torch.nn.Module):
+    """One block of a Parity Transformer: causal attention, then DPBMLP (§3.1).  forward
+    returns (output, loss_var)."""
+
+    def __init__(self, plan: B.Plan, heads: int, d_ff: int, kv_heads: int | None = None,
+                 dtype: torch.dtype = torch.float32, device=None, **mlp):
+        super().__init__()
+        self.attention = CausalAttention(plan.d, heads, kv_heads, dtype, device)
+        self.mlp = DPBMLP(plan, d_ff, dtype=dtype, device=device, **mlp)
+
+    def forward(self, h: torch.Tensor, cache: KeyValueCache | None = None):
+        return self.mlp(self.attention(h, cache))

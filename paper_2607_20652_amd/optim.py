@@ -1,0 +1,75 @@
+"""AdamW for the parameters of a model, in the library's kernel.
+
+`AdamW(params).step()` updates all parameters of one type in one call of
+dpb_adamw_step: fp32 or 8-bit states, optional fp32 masters of bf16
+parameters, and decay of matrices only if asked for.  It keeps torch's
+step / zero_grad / state_dict manner.
+"""
+from __future__ import annotations
+
+from typing import Iterable
+
+import torch
+
+from . import binding as B
+
+
+class AdamW:
+    """params: tensors with gradients (or (tensor, weight_decay) pairs).
+
+    bits: of the states, 32 or 8; master: fp32 copies of bf16 parameters that
+    the steps update (default: whenever parameters are bf16); seed: of the
+    rounding of 8-bit states."""
+
+    def __init__(self, params: Iterable, lr: float = 1e-3, betas: tuple[float, float] = (0.9, 0.999),
+                 eps: float = 1e-8, weight_decay: float = 0.0, bits: int = 32, master: bool | None = None,
+                 seed: int = 0):
+        self.lr, self.betas, self.eps, self.bits, self.seed = lr, betas, eps, bits, seed
+        self.steps = 0
+        pairs = [p if isinstance(p, tuple) else (p, weight_decay) for p in params]
+        self.groups = []
+        for dtype in (torch.float32, torch.bfloat16):
+            mine = [(p, wd) for p, wd in pairs if p.dtype == dtype]
+            if mine:
+                tensors = [p for p, _ in mine]
+                keep = dtype == torch.bfloat16 if master is None else master
+                m, v, scales, weights = B.adamw_state(tensors, bits, keep)
+                self.groups.append(dict(params=tensors, decay=[float(wd) for _, wd in mine], m=m, v=v, scales=scales,
+                                        master=weights))
+        if sum(len(g["params"]) for g in self.groups) != len(pairs):
+            raise TypeError("parameters have to be float32 or bfloat16")
+
+    @torch.no_grad()
+    def step(self, grad_scale: torch.Tensor | None = None):
+        """One step from the parameters' gradients, times the device scalar grad_scale; a
+        parameter without a gradient is an error."""
+        self.steps += 1
+        for i, g in enumerate(self.groups):
+            grads = [p.grad for p in g["params"]]
+            if any(x is None for x in grads):
+                raise ValueError("a parameter has no gradient")
+            # the places of two groups' states are the same numbers: their seeds are not
+            B.adamw_step(g["params"], [x.contiguous() for x in grads], g["m"], g["v"], g["scales"], g["master"],
+                         step=self.steps, lr=self.lr, betas=self.betas, eps=self.eps, weight_decay=g["decay"],
+                         grad_scale=grad_scale, seed=self.seed + 2 * self.steps + i)
+
+    def zero_grad(self):
+        for g in self.groups:
+            for p in g["params"]:
+                p.grad = None
+
+    def state_dict(self) -> dict:
+        return {"steps": self.steps, "groups": [{k: g[k] for k in ("m", "v", "scales", "master")} for g in self.groups]}
+
+    def load_state_dict(self, state: dict):
+        if len(state["groups"]) != len(self.groups):
+            raise ValueError("the state is of other parameters")
+        for g, s in zip(self.groups, state["groups"]):
+            for k in ("m", "v", "scales", "master"):
+                if (g[k] is None) != (s[k] is None) or (g[k] is not None and g[k].shape != s[k].shape):
+                    raise ValueError("the state is of other parameters")
+        for g, s in zip(self.groups, state["groups"]):
+            for k in ("m", "v", "scales", "master"):
+                if g[k] is not None:
+                    g[k].copy_(s[k])
+        self.steps = int(state["steps"])
