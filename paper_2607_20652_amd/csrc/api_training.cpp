@@ -113,11 +113,15 @@ size_t dpb_attention_workspace_bytes(const dpb_attn* a)
 size_t dpb_attention_bwd_workspace_bytes(const dpb_attn* a)
 {
     if (check_sizes(a)) return 0;
-    int q_parts, k_parts;
-    dpb::attention_parts((int)a->batch, (int)a->q_len, (int)a->k_len, a->heads, a->kv_heads, &q_parts, &k_parts);
-    const size_t dq = q_parts > 1 ? (size_t)q_parts * rows_of(a, true) * a->heads : 0;
-    const size_t dkv = k_parts > 1 ? (size_t)k_parts * rows_of(a, false) * a->kv_heads * 2 : 0;
-    return 2 * row_bytes(a) + std::max(dq, dkv) * a->head_dim * 4;
+    size_t rows = 0;   // of the parts; the same answer for either type
+    for (const bool bf16 : {false, true}) {
+        int q_parts, k_parts;
+        dpb::attention_parts((int)a->batch, (int)a->q_len, (int)a->k_len, a->heads, a->kv_heads, a->head_dim, a->causal != 0,
+                             bf16, &q_parts, &k_parts);
+        if (q_parts > 1) rows = std::max(rows, (size_t)q_parts * rows_of(a, true) * a->heads);
+        if (k_parts > 1) rows = std::max(rows, (size_t)k_parts * rows_of(a, false) * a->kv_heads * 2);
+    }
+    return 2 * row_bytes(a) + rows * a->head_dim * 4;
 }
 
 dpb_status dpb_attention(const dpb_attn* a, dpb_dtype dtype, const dpb_heads* q, const dpb_heads* k,
@@ -175,7 +179,8 @@ dpb_status dpb_attention_bwd(const dpb_attn* a, dpb_dtype dtype, const dpb_heads
     g.row_lse2 = (float*)workspace;
     g.row_delta = (float*)((char*)workspace + row_bytes(a));
     g.part = (float*)((char*)workspace + 2 * row_bytes(a));
-    dpb::attention_parts(g.batch, g.q_len, g.k_len, g.heads, g.kv_heads, &g.q_parts, &g.k_parts);
+    dpb::attention_parts(g.batch, g.q_len, g.k_len, g.heads, g.kv_heads, g.dim, g.causal != 0, dtype == DPB_BF16, &g.q_parts,
+                         &g.k_parts);
     return launched(dpb::launch_attention_bwd(g, dtype == DPB_BF16, (hipStream_t)stream));
 }
 

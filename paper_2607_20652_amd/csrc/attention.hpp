@@ -56,7 +56,9 @@ hipError_t launch_attention_bwd(const AttnArgs& a, bool bf16, hipStream_t stream
 // rows), and the scratch floats that takes.
 int attention_splits(int batch, int q_len, int k_len, int heads, int kv_heads);
 size_t attention_part_floats(int64_t q_rows, int heads, int dim, int splits);
-void attention_parts(int batch, int q_len, int k_len, int heads, int kv_heads, int* q_parts, int* k_parts);
+// Workgroups that share a tile of the backward's dQ, and of its dK and dV.
+void attention_parts(int batch, int q_len, int k_len, int heads, int kv_heads, int dim, bool causal, bool bf16, int* q_parts,
+                     int* k_parts);
 
 // Where sequence b lies: rows before it, its lengths, and the query (key) rows
 // of the outputs that belong to it.  Packed starts are clamped to the tensor, so

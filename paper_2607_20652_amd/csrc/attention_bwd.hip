@@ -353,18 +353,25 @@ hipError_t launch_bwd(const AttnArgs& a, hipStream_t stream)
 
 }  // namespace
 
-void attention_parts(int batch, int q_len, int k_len, int heads, int kv_heads, int* q_parts, int* k_parts)
+void attention_parts(int batch, int q_len, int k_len, int heads, int kv_heads, int dim, bool causal, bool bf16, int* q_parts,
+                     int* k_parts)
 {
-    // Work for every compute unit, in pieces short enough to even out: the products of
-    // few rows (keys) are parted along the keys (rows of all heads that share one), each
-    // part of 128 of those or more.
+    // Workgroups that fill the chip once, or, where causal masks make them uneven, twice, the
+    // rest taking the place of those that end: the products of few rows (keys) are parted along the
+    // keys (rows of all heads that share one), each part of 128 of those or more.  (A
+    // little over a whole round costs another: fp32, 3 x 511 tokens over 1203, width 72: dK and
+    // dV 97 us as 660 workgroups, 64 as 240.)
     const int64_t cus = device_cus(), pairs = std::max<int64_t>(1, (int64_t)batch * kv_heads), group = heads / kv_heads;
     const int64_t qt = std::max<int64_t>(1, (q_len * group + 127) / 128), kt = std::max<int64_t>(1, ((int64_t)k_len + 127) / 128);
-    auto parts = [&](int64_t want, int64_t units, int64_t most) {
-        return (int)std::max<int64_t>(1, std::min({(want + units - 1) / units, most, (int64_t)64}));
+    // the kernels' workgroups a compute unit holds, by their registers and LDS
+    const int64_t q_slots = cus * (bf16 ? dim <= 64 ? 3 : 2 : dim <= 32 ? 4 : dim <= 64 ? 2 : 1);
+    const int64_t k_slots = cus * (bf16 ? dim <= 32 ? 3 : 2 : dim <= 32 ? 3 : dim <= 64 ? 2 : 1);
+    auto parts = [&](int64_t slots, int64_t units, int64_t most) {
+        const int64_t want = causal ? (2 * slots + units - 1) / units : slots / units;
+        return (int)std::max<int64_t>(1, std::min({want, most, (int64_t)64}));
     };
-    *q_parts = parts(2 * cus, qt * pairs, k_len / 128);
-    *k_parts = parts(4 * cus, kt * pairs, q_len * group / 128);
+    *q_parts = parts(q_slots, qt * pairs, k_len / 128);
+    *k_parts = parts(k_slots, kt * pairs, q_len * group / 128);
 }
 
 hipError_t launch_attention_bwd(const AttnArgs& a, bool bf16, hipStream_t stream)
