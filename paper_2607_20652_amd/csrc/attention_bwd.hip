@@ -25,14 +25,6 @@ __device__ __forceinline__ void fill16(f32x16& c, float v)
     for (int r = 0; r < 16; ++r) c[r] = v;
 }
 
-// fp32 operands take twice the registers: there the products' LDS reads stay in
-// their own phase, or the compiler, which issues them early, runs out of registers.
-template <bool ON>
-__device__ __forceinline__ void phase()
-{
-    if constexpr (ON) __builtin_amdgcn_sched_barrier(0);
-}
-
 // dQ of 128 rows (tokens x the heads that share a key head); also leaves each
 // row's lse * log2(e) and delta for the other kernel.
 template <typename T, int DP, int KT, int W, int NS>
@@ -159,12 +151,11 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
     typedef Tile<T, DP, QT, kWaves> Tl;
     typedef typename Operand<T>::type Op;
     constexpr int kSteps = DP / 16, kParts = DP / 32;
-    constexpr bool kPhases = sizeof(T) == 4;
     static_assert(QT <= 64, "one load each brings the tile's row values");
-    // Wide rows leave no registers for V: its operands come from LDS each time.
-    constexpr bool kValuesInLds = DP > 64;
+    // K's operands stay in registers, V's come from LDS each time: one more wave per SIMD
+    // (bf16, width 64: 179 -> 163 registers, 106 -> 97 us for 16 x 1024 tokens; at 128 both spill).
     typedef Tile<T, DP, 128, kWaves> Vl;
-    __shared__ __align__(1024) char vt[kValuesInLds ? Vl::kBytes : 16];
+    __shared__ __align__(1024) char vt[Vl::kBytes];
     const int pairs = a.batch * a.kv_heads, bh = (int)blockIdx.x % pairs, b = bh / a.kv_heads, hk = bh % a.kv_heads;
     const int part = (int)blockIdx.x / pairs % a.k_parts;
     const int tile = (int)blockIdx.x / pairs / a.k_parts;   // of a causal sequence the keys that most queries see first
@@ -210,16 +201,12 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
     begin_ring<NS, 2 * Tl::kBytes + 512>(n, fill);
 
     const char* krow = head_base(a.k, a.k_starts, b, sq.k0, hk) + (int64_t)key * a.k.ts;
-    const char* vrow = head_base(a.v, a.k_starts, b, sq.k0, hk) + (int64_t)key * a.v.ts;
-    Op k[kSteps], v[kValuesInLds ? 1 : kSteps];
+    Op k[kSteps];
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-        k[i] = global_operand<T>(krow, i, a.dim, valid);
-        if constexpr (!kValuesInLds) v[i] = global_operand<T>(vrow, i, a.dim, valid);
-    }
-    if constexpr (kValuesInLds)
-        typename Vl::Fill(a.v.ts, a.dim, wave)(vt, head_base(a.v, a.k_starts, b, sq.k0, hk) + (int64_t)tile * 128 * a.v.ts,
-                                               sq.kn - tile * 128, wave);
+    for (int i = 0; i < kSteps; ++i) k[i] = global_operand<T>(krow, i, a.dim, valid);
+    // (landed, like the ring's first stage, when the waves first meet)
+    typename Vl::Fill(a.v.ts, a.dim, wave)(vt, head_base(a.v, a.k_starts, b, sq.k0, hk) + (int64_t)tile * 128 * a.v.ts,
+                                           sq.kn - tile * 128, wave);
     f32x16 dk[kParts], dv[kParts];
 #pragma unroll
     for (int i = 0; i < kParts; ++i) {
@@ -242,11 +229,9 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
         }
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) s = mma(rd.rows(qt, at, i), k[i], s);
-        phase<kPhases>();
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            if constexpr (kValuesInLds) dp = mma(rd.rows(gt, at, i), rd.rows(vt, 32 * wave, i), dp);
-            else dp = mma(rd.rows(gt, at, i), v[i], dp);
+            dp = mma(rd.rows(gt, at, i), rd.rows(vt, 32 * wave, i), dp);
         }
         if (edge) {
             // rows from `need` on see the key, and those before `left` are the sequence's
@@ -267,7 +252,6 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
             const Op p = as_operand<T>(s, j), ds = as_operand<T>(dp, j);
 #pragma unroll
             for (int i = 0; i < kParts; ++i) {
-                if (i % 2 == 0) phase<kPhases>();
                 dv[i] = mma(rd.columns(gt, at / 16 + j, i), p, dv[i]);
                 dk[i] = mma(rd.columns(qt, at / 16 + j, i), ds, dk[i]);
             }
@@ -365,7 +349,7 @@ void attention_parts(int batch, int q_len, int k_len, int heads, int kv_heads, i
     const int64_t qt = std::max<int64_t>(1, (q_len * group + 127) / 128), kt = std::max<int64_t>(1, ((int64_t)k_len + 127) / 128);
     // the kernels' workgroups a compute unit holds, by their registers and LDS
     const int64_t q_slots = cus * (bf16 ? dim <= 64 ? 3 : 2 : dim <= 32 ? 4 : dim <= 64 ? 2 : 1);
-    const int64_t k_slots = cus * (bf16 ? dim <= 32 ? 3 : 2 : dim <= 32 ? 3 : dim <= 64 ? 2 : 1);
+    const int64_t k_slots = cus * (bf16 ? dim <= 64 ? 3 : 2 : dim <= 32 ? 3 : dim <= 64 ? 2 : 1);
     auto parts = [&](int64_t slots, int64_t units, int64_t most) {
         const int64_t want = causal ? (2 * slots + units - 1) / units : slots / units;
         return (int)std::max<int64_t>(1, std::min({want, most, (int64_t)64}));
@@ -379,7 +363,7 @@ hipError_t launch_attention_bwd(const AttnArgs& a, bool bf16, hipStream_t stream
     const int width = (a.dim + 31) / 32;
     if (bf16)
         return width == 1 ? launch_bwd<__bf16, 32, 64, 4, 2, 64, 3, 2>(a, stream)
-             : width == 2 ? launch_bwd<__bf16, 64, 64, 3, 2, 64, 2, 2>(a, stream)
+             : width == 2 ? launch_bwd<__bf16, 64, 64, 3, 2, 64, 3, 2>(a, stream)
              : width == 3 ? launch_bwd<__bf16, 96, 32, 2, 2, 32, 2, 2>(a, stream)
                           : launch_bwd<__bf16, 128, 32, 2, 2, 32, 2, 2>(a, stream);
     return width == 1 ? launch_bwd<float, 32, 32, 2, 2, 32, 2, 2>(a, stream)
