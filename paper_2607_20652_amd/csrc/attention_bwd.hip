@@ -349,7 +349,7 @@ void attention_parts(int batch, int q_len, int k_len, int heads, int kv_heads, i
     const int64_t qt = std::max<int64_t>(1, (q_len * group + 127) / 128), kt = std::max<int64_t>(1, ((int64_t)k_len + 127) / 128);
     // the kernels' workgroups a compute unit holds, by their registers and LDS
     const int64_t q_slots = cus * (bf16 ? dim <= 64 ? 3 : 2 : dim <= 32 ? 4 : dim <= 64 ? 2 : 1);
-    const int64_t k_slots = cus * (bf16 ? dim <= 64 ? 3 : 2 : dim <= 32 ? 3 : dim <= 64 ? 2 : 1);
+    const int64_t k_slots = cus * (bf16 ? dim <= 64 ? 3 : 2 : dim <= 64 ? 2 : 1);
     auto parts = [&](int64_t slots, int64_t units, int64_t most) {
         const int64_t want = causal ? (2 * slots + units - 1) / units : slots / units;
         return (int)std::max<int64_t>(1, std::min({want, most, (int64_t)64}));

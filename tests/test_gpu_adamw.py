@@ -187,6 +187,28 @@ def test_gradients_that_are_not_finite():
         assert (~torch.isfinite(m)).sum() == 1 and (~torch.isfinite(v)).sum() == 1
 
 
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_tensor_of_more_than_2_to_the_31_elements(bits):
+    n, tail = 2**31 + 2**20 + 77, 5000
+    p = [torch.zeros(n, dtype=BF16, device=DEV)]
+    g = [torch.zeros(n, dtype=BF16, device=DEV)]
+    gen = torch.Generator().manual_seed(7)
+    p[0][-tail:] = torch.randn(tail, generator=gen).to(BF16).to(DEV)
+    g[0][-tail:] = torch.randn(tail, generator=gen).to(BF16).to(DEV)
+    w64, g64 = p[0][-tail:].double().cpu(), g[0][-tail:].double().cpu()
+    m, v, scales, _ = dpb.adamw_state(p, bits)
+    dpb.adamw_step(p, g, m, v, scales, step=1, lr=1e-2, weight_decay=0.1, seed=3)
+    want, m1, v1 = formulas(w64, g64, 0 * w64, 0 * w64, 1, 1e-2, (0.9, 0.999), 1e-8, 0.1)
+    assert bool(((p[0][-tail:].double().cpu() - want).abs() <= 2.0 ** -8 * want.abs() + 1e-6).all())
+    assert not p[0][:-tail].any() and not g[0][:-tail].any()
+    got = m[n - tail:n].double().cpu()
+    if bits == 8:
+        got *= scales[torch.arange(n - tail, n, device=DEV) // 256, 0].double().cpu()
+        assert bool(((got - m1).abs() <= 0.13 * m1.abs() + 0.1 * 2.0 ** -9 / 448 * 5).all())   # a neighbour: at most 1/8 off
+    else:
+        near(got, m1, 3e-6)
+
+
 def test_zero_gradients_and_tiny_ones():
     p, g = [torch.ones(512, device=DEV)], [torch.zeros(512, device=DEV)]
     g[0][256:] = 1e-41

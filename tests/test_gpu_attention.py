@@ -151,6 +151,23 @@ def test_broadcast_inputs():
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_rows_far_apart(dtype):
+    """Rows 4 MiB apart: the last ones lie 5 GB behind the first."""
+    pitch, n, D = (4 << 20) // (2 if dtype == BF16 else 4), 1250, 64
+    q, k, v, g = make(14, 1, 3, n, 2, 1, D, dtype)
+    ref = reference(q, k, v, True, D ** -0.5, g)
+    far = []
+    for x in (k, v):
+        room = torch.empty(pitch * (n - 1) + D, dtype=dtype, device=DEV)
+        far.append(room.as_strided((1, n, 1, D), (0, pitch, D, 1)))
+        far[-1].copy_(x)
+    out, lse = dpb.attention(q.to(DEV), *far, True)
+    dk, dv = (torch.empty(1, n, 1, D, dtype=dtype, device=DEV) for _ in range(2))
+    dq, dk, dv = dpb.attention_bwd(g.to(DEV), q.to(DEV), *far, out, lse, True, dk=dk, dv=dv)
+    agree({"out": out, "lse": lse, "dq": dq, "dk": dk, "dv": dv}, ref, dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
 def test_large_scores(dtype):
     """Scores far apart: the softmax picks one key; no overflow, no NaN."""
     q, k, v, g = make(7, 1, 80, 200, 2, 2, 64, dtype)
