@@ -121,7 +121,8 @@ def _dtype_code(t: torch.Tensor) -> int:
 
 
 def _stream(t: torch.Tensor):
-    return torch.cuda.current_stream(t.device).cuda_stream
+    # torch.cuda.current_stream(t.device).cuda_stream without the Stream object (2 us a call)
+    return torch._C._cuda_getCurrentRawStream(t.device.index)
 
 
 def _dev(t: torch.Tensor, name: str):

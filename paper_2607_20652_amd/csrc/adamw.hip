@@ -14,6 +14,13 @@
 // seed and the element's place (the same bits for the same seed, in any order
 // of execution).  A positive u is never rounded to zero, since w's step divides
 // by it.  All arithmetic is fp32 in the written order, without contraction.
+//
+// Bound by memory: 202M parameters, fp32 with fp32 states (28 bytes an element) 1.10 ms,
+// 5.2 TB/s; bf16 with fp32 masters and 8-bit states (16 bytes) 0.645 ms, 5.0 TB/s (a
+// 4 GiB copy: 4.8).  Half a wave takes a block, eight elements a lane in two runs of
+// four, so that every access of 32 lanes is contiguous for each type and a block's
+// largest magnitudes are five exchanges away; the tensors' table rides in the kernel's
+// arguments, and a workgroup finds its tensor by one comparison a lane.
 #include "adamw.hpp"
 
 namespace dpb {
