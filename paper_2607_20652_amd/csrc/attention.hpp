@@ -391,7 +391,6 @@ template <int N, int L, int BYTES, typename F, typename S>
 __device__ __forceinline__ void ring(int n, F&& fill, S&& step)
 {
     const Stages<N, BYTES> st;
-    if (n <= 0) return;
     for (int t = 0; t < n; t += N) {
 #pragma unroll
         for (int s = 0; s < N; ++s) {
@@ -403,7 +402,9 @@ __device__ __forceinline__ void ring(int n, F&& fill, S&& step)
             }
         }
     }
-    wait_loads<0>();   // none is under way when the workgroup ends or its LDS is used again
+    // no load into LDS (the ring's or another) is under way when it is used again, or when the
+    // workgroup ends and another gets it
+    wait_loads<0>();
 }
 
 }  // namespace dpb
