@@ -145,11 +145,11 @@ __device__ __forceinline__ float log_sum(float base, float total)
 
 // One workgroup: 128 rows (tokens x the heads that share a key head) against the
 // keys they see.
-template <typename T, int DP, int KT, int WAVES, int W>
-__global__ __launch_bounds__(64 * WAVES, W) void attention_kernel(AttnArgs a)
+template <typename T, int DP, int KT, int W>
+__global__ __launch_bounds__(256, W) void attention_kernel(AttnArgs a)
 {
-    typedef Tile<T, DP, KT, WAVES> Tl;
-    constexpr int kRows = 32 * WAVES, kKeys = KT < 64 ? KT : 64;
+    typedef Tile<T, DP, KT> Tl;
+    constexpr int kRows = 32 * kWaves;
     const int tiles = (a.q_len * a.group + kRows - 1) / kRows;
     const int pairs = a.batch * a.kv_heads, bh = (int)blockIdx.x % pairs, b = bh / a.kv_heads, hk = bh % a.kv_heads;
     const int tile = tiles - 1 - (int)blockIdx.x / pairs;   // of causal sequences the longest rows first
@@ -182,7 +182,7 @@ __global__ __launch_bounds__(64 * WAVES, W) void attention_kernel(AttnArgs a)
         vb += KT * a.v.ts;
         left -= KT;
     };
-    begin_ring<2, 2 * Tl::kBytes>(n, fill);
+    begin_steps<2 * Tl::kBytes>(n, fill);
     Rows<T, DP> st;
     st.clear();
     typename Tl::Reader rd;
@@ -191,23 +191,20 @@ __global__ __launch_bounds__(64 * WAVES, W) void attention_kernel(AttnArgs a)
     for (int i = 0; i < DP / 16; ++i) st.q[i] = global_operand<T>(qrow, i, a.dim, valid);
 
     auto step = [&](const char* lds, int t) {
-#pragma unroll
-        for (int at = 0; at < KT; at += 64) {
-            const int first = t * KT + at;
-            if (first >= most) return;
-            f32x16 s[kKeys / 32];
-            rd.fresh();
-            st.template scores<kKeys>(s, rd, lds + at * Tl::kRowBytes);
-            st.template raise<kKeys>(s, limit - first, first + kKeys > least, c);
-            st.template weigh<kKeys>(s, c);
-            st.template gather<kKeys>(s, rd, lds + Tl::kBytes + at * Tl::kRowBytes);
-        }
+        const int first = t * KT;
+        if (first >= most) return;
+        f32x16 s[KT / 32];
+        rd.fresh();
+        st.template scores<KT>(s, rd, lds);
+        st.template raise<KT>(s, limit - first, first + KT > least, c);
+        st.template weigh<KT>(s, c);
+        st.template gather<KT>(s, rd, lds + Tl::kBytes);
     };
-    ring<2, 2 * Tl::kLoads, 2 * Tl::kBytes>(n, fill, step);
+    run_steps<2 * Tl::kBytes>(n, fill, step);
 
     const float total = st.total(), inv = inverse(total);
     if (lane < 32 && token < sq.qw) a.lse[(sq.q0 + token) * a.heads + head] = log_sum(st.base, total);
-    static_assert(2 * Tl::kBytes >= WAVES * kStoreBytes, "a stage holds what the waves store");
+    static_assert(2 * Tl::kBytes >= kWaves * kStoreBytes, "a stage holds what the waves store");
     __syncthreads();
     store_rows<T, DP>(stage_lds<2 * Tl::kBytes, 0>() + wave * kStoreBytes, st.o, inv, inv != 0.f, a.dim, [&](int r) {
         const int x = tile * kRows + wave * 32 + r, tok = x / a.group;
@@ -384,11 +381,12 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a)
     if (e == 0) a.lse[at] = log_sum(zero_of, sum);
 }
 
-template <typename T, int DP, int KT, int WAVES, int W>
+// W: waves per SIMD that the registers are to allow.
+template <typename T, int DP, int KT, int W>
 hipError_t launch_tiles(const AttnArgs& a, hipStream_t stream)
 {
-    const int64_t rows = (int64_t)a.q_len * a.group, tiles = (rows + 32 * WAVES - 1) / (32 * WAVES);
-    attention_kernel<T, DP, KT, WAVES, W><<<dim3((unsigned)(tiles * a.batch * a.kv_heads)), 64 * WAVES, 0, stream>>>(a);
+    const int64_t rows = (int64_t)a.q_len * a.group, tiles = (rows + 127) / 128;
+    attention_kernel<T, DP, KT, W><<<dim3((unsigned)(tiles * a.batch * a.kv_heads)), 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -435,10 +433,10 @@ hipError_t launch_attention(const AttnArgs& a, bool bf16, hipStream_t stream)
              : width == 3 ? launch_split<float, 96, 2>(a, stream) : launch_split<float, 128, 2>(a, stream);
     }
     if (bf16)
-        return width == 1 ? launch_tiles<__bf16, 32, 64, 4, 4>(a, stream) : width == 2 ? launch_tiles<__bf16, 64, 64, 4, 3>(a, stream)
-             : width == 3 ? launch_tiles<__bf16, 96, 64, 4, 2>(a, stream) : launch_tiles<__bf16, 128, 64, 4, 2>(a, stream);
-    return width == 1 ? launch_tiles<float, 32, 32, 4, 4>(a, stream) : width == 2 ? launch_tiles<float, 64, 32, 4, 2>(a, stream)
-         : width == 3 ? launch_tiles<float, 96, 32, 4, 2>(a, stream) : launch_tiles<float, 128, 32, 4, 1>(a, stream);
+        return width == 1 ? launch_tiles<__bf16, 32, 64, 4>(a, stream) : width == 2 ? launch_tiles<__bf16, 64, 64, 3>(a, stream)
+             : width == 3 ? launch_tiles<__bf16, 96, 64, 2>(a, stream) : launch_tiles<__bf16, 128, 64, 2>(a, stream);
+    return width == 1 ? launch_tiles<float, 32, 32, 4>(a, stream) : width == 2 ? launch_tiles<float, 64, 32, 2>(a, stream)
+         : width == 3 ? launch_tiles<float, 96, 32, 2>(a, stream) : launch_tiles<float, 128, 32, 1>(a, stream);
 }
 
 }  // namespace dpb

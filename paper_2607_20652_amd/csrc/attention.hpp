@@ -22,6 +22,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
+constexpr int kWaves = 4;   // of a workgroup
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
@@ -216,7 +217,7 @@ __device__ __forceinline__ void store_rows(char* lds, const f32x16 (&c)[DP / 32]
 // past the sequence and chunks past dim lie out of the buffer's range and arrive
 // as zeros (of a tensor whose token stride is 0, rows past the sequence arrive as
 // its one row; either way no result depends on them).
-template <typename T, int DP, int R, int WAVES = 4>
+template <typename T, int DP, int R, int WAVES = kWaves>
 struct Tile {
     static constexpr int kRowBytes = (DP <= 64 ? 64 : 128) * (int)sizeof(T);
     static constexpr int kChunks = kRowBytes / 16;
@@ -348,17 +349,8 @@ __device__ __forceinline__ void wait_lds()
     __asm__ volatile("" ::: "memory");
 }
 
-// The same, then until every wave of the workgroup is here.
-template <int N>
-__device__ __forceinline__ void meet()
-{
-    wait_loads<N>();
-    __builtin_amdgcn_s_barrier();
-    __asm__ volatile("" ::: "memory");
-}
-
-// LDS of a ring's stage: an object each, so that the compiler sees that reads of
-// one and loads into another are independent.
+// LDS of a stage: an object each, so that the compiler sees that reads of one and
+// loads into the other are independent.
 template <int BYTES, int STAGE>
 __device__ __forceinline__ char* stage_lds()
 {
@@ -366,43 +358,35 @@ __device__ __forceinline__ char* stage_lds()
     return lds;
 }
 
-// Steps 0..n-1 of a workgroup, the loads of each sent N - 1 steps ahead.
-// fill(lds, t) enqueues exactly L loads a wave (of nothing, where t >= n); step(lds,
-// t) uses them.  Before a step every wave has waited for its part of the stage and is
-// done with the step before, whose stage the loads sent next go into.  begin_ring() sends the
-// first loads; what else a kernel loads up front then comes in beside them.
-template <int N, int BYTES>
-struct Stages {
-    static_assert(N >= 2 && N <= 5, "stages");
-    char* const lds[5] = {stage_lds<BYTES, 0>(), stage_lds<BYTES, 1>(), stage_lds<BYTES, (N > 2 ? 2 : 0)>(),
-                          stage_lds<BYTES, (N > 3 ? 3 : 0)>(), stage_lds<BYTES, (N > 4 ? 4 : 0)>()};
-};
-
-template <int N, int BYTES, typename F>
-__device__ __forceinline__ void begin_ring(int n, F&& fill)
+// Steps 0..n-1 of a workgroup over two stages, the loads of each sent a step ahead.
+// fill(lds, t) enqueues a wave's loads (of nothing, where t >= n); step(lds, t) uses what
+// all waves loaded.  Before a step every wave has waited for its loads and is done
+// with the step before, whose stage the loads sent next go into.  begin_steps() sends
+// the first loads; what else a kernel loads up front then comes in beside them.
+template <int BYTES, typename F>
+__device__ __forceinline__ void begin_steps(int n, F&& fill)
 {
-    const Stages<N, BYTES> st;
-    if (n <= 0) return;
-#pragma unroll
-    for (int s = 0; s < N - 1; ++s) fill(st.lds[s], s);
+    if (n > 0) fill(stage_lds<BYTES, 0>(), 0);
 }
 
-template <int N, int L, int BYTES, typename F, typename S>
-__device__ __forceinline__ void ring(int n, F&& fill, S&& step)
+template <int BYTES, typename F, typename S>
+__device__ __forceinline__ void run_steps(int n, F&& fill, S&& step)
 {
-    const Stages<N, BYTES> st;
-    for (int t = 0; t < n; t += N) {
+    char* const lds[2] = {stage_lds<BYTES, 0>(), stage_lds<BYTES, 1>()};
+    for (int t = 0; t < n; t += 2) {
 #pragma unroll
-        for (int s = 0; s < N; ++s) {
+        for (int s = 0; s < 2; ++s) {
             if (t + s < n) {
                 wait_lds();
-                meet<L*(N - 2)>();
-                fill(st.lds[(s + N - 1) % N], t + s + N - 1);
-                step(st.lds[s], t + s);
+                wait_loads<0>();
+                __builtin_amdgcn_s_barrier();
+                __asm__ volatile("" ::: "memory");
+                fill(lds[s ^ 1], t + s + 1);
+                step(lds[s], t + s);
             }
         }
     }
-    // no load into LDS (the ring's or another) is under way when it is used again, or when the
+    // no load into LDS (a stage's or another) is under way when it is used again, or when the
     // workgroup ends and another gets it
     wait_loads<0>();
 }

@@ -27,8 +27,6 @@
 namespace dpb {
 namespace {
 
-constexpr int kWaves = 4;
-
 __device__ __forceinline__ void fill16(f32x16& c, float v)
 {
 #pragma unroll
@@ -37,10 +35,10 @@ __device__ __forceinline__ void fill16(f32x16& c, float v)
 
 // dQ of 128 rows (tokens x the heads that share a key head); also leaves each
 // row's lse * log2(e) and delta for the other kernel.
-template <typename T, int DP, int KT, int W, int NS>
+template <typename T, int DP, int KT, int W>
 __global__ __launch_bounds__(256, W) void attention_dq_kernel(AttnArgs a)
 {
-    typedef Tile<T, DP, KT, kWaves> Tl;
+    typedef Tile<T, DP, KT> Tl;
     typedef typename Operand<T>::type Op;
     constexpr int kSteps = DP / 16, kParts = DP / 32;
     const int tiles = (a.q_len * a.group + 127) / 128;
@@ -76,7 +74,7 @@ __global__ __launch_bounds__(256, W) void attention_dq_kernel(AttnArgs a)
         vp += KT * a.v.ts;
         left -= KT;
     };
-    begin_ring<NS, 2 * Tl::kBytes>(n, fill);
+    begin_steps<2 * Tl::kBytes>(n, fill);
 
     const char* qrow = head_base(a.q, a.q_starts, b, sq.q0, head) + (int64_t)token * a.q.ts;
     const char* grow = head_base(a.go, a.q_starts, b, sq.q0, head) + (int64_t)token * a.go.ts;
@@ -134,7 +132,7 @@ __global__ __launch_bounds__(256, W) void attention_dq_kernel(AttnArgs a)
         if (t * KT >= most) return;
         products(kt, vt, t, (t + 1) * KT > least);
     };
-    ring<NS, 2 * Tl::kLoads, 2 * Tl::kBytes>(n, fill, step);
+    run_steps<2 * Tl::kBytes>(n, fill, step);
 
     static_assert(2 * Tl::kBytes >= kWaves * kStoreBytes, "a stage holds what the waves store");
     char* const lds = stage_lds<2 * Tl::kBytes, 0>() + wave * kStoreBytes;
@@ -155,16 +153,16 @@ __global__ __launch_bounds__(256, W) void attention_dq_kernel(AttnArgs a)
 
 // dK and dV of 128 keys of one key head: the queries of every head that shares it
 // pass by, QT rows at a time.
-template <typename T, int DP, int QT, int W, int NS>
+template <typename T, int DP, int QT, int W>
 __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
 {
-    typedef Tile<T, DP, QT, kWaves> Tl;
+    typedef Tile<T, DP, QT> Tl;
     typedef typename Operand<T>::type Op;
     constexpr int kSteps = DP / 16, kParts = DP / 32;
     static_assert(QT <= 64, "one load each brings the tile's row values");
     // K's operands stay in registers, V's come from LDS each time: one more wave per SIMD
     // (bf16, width 64: 179 -> 163 registers, 106 -> 97 us for 16 x 1024 tokens; at 128 both spill).
-    typedef Tile<T, DP, 128, kWaves> Vl;
+    typedef Tile<T, DP, 128> Vl;
     __shared__ __align__(1024) char vt[Vl::kBytes];
     const int pairs = a.batch * a.kv_heads, bh = (int)blockIdx.x % pairs, b = bh / a.kv_heads, hk = bh % a.kv_heads;
     const int part = (int)blockIdx.x / pairs % a.k_parts;
@@ -208,13 +206,13 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
             gp += a.go.hs;
         }
     };
-    begin_ring<NS, 2 * Tl::kBytes + 512>(n, fill);
+    begin_steps<2 * Tl::kBytes + 512>(n, fill);
 
     const char* krow = head_base(a.k, a.k_starts, b, sq.k0, hk) + (int64_t)key * a.k.ts;
     Op k[kSteps];
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) k[i] = global_operand<T>(krow, i, a.dim, valid);
-    // (landed, like the ring's first stage, when the waves first meet)
+    // (landed, like the first stage, at the first barrier)
     typename Vl::Fill(a.v.ts, a.dim, wave)(vt, head_base(a.v, a.k_starts, b, sq.k0, hk) + (int64_t)tile * 128 * a.v.ts,
                                            sq.kn - tile * 128, wave);
     f32x16 dk[kParts], dv[kParts];
@@ -279,7 +277,7 @@ __global__ __launch_bounds__(256, W) void attention_dkv_kernel(AttnArgs a)
         step_tok += QT;
         if (step_tok >= sq.qn) step_tok = from;
     };
-    ring<NS, 2 * Tl::kLoads + 2, 2 * Tl::kBytes + 512>(n, fill, step);
+    run_steps<2 * Tl::kBytes + 512>(n, fill, step);
 
     static_assert(2 * Tl::kBytes + 512 >= kWaves * kStoreBytes, "a stage holds what the waves store");
     char* const lds = stage_lds<2 * Tl::kBytes + 512, 0>() + wave * kStoreBytes;
@@ -326,20 +324,21 @@ __global__ __launch_bounds__(256) void attention_sum_kernel(AttnArgs a)
     }
 }
 
-template <typename T, int DP, int KT, int WQ, int NQ, int QT, int WK, int NK>
+// WQ, WK: waves per SIMD that the kernels' registers are to allow.
+template <typename T, int DP, int KT, int WQ, int QT, int WK>
 hipError_t launch_bwd(const AttnArgs& a, hipStream_t stream)
 {
     const int64_t rows = (int64_t)a.q_len * a.group, qt = (rows + 127) / 128, kt = ((int64_t)a.k_len + 127) / 128;
     const int64_t pairs = (int64_t)a.batch * a.kv_heads;
     auto sums = [&](int64_t len, int heads) { return dim3((unsigned)((len * heads * (a.dim / 4) + 255) / 256 * a.batch)); };
     if (qt > 0) {
-        attention_dq_kernel<T, DP, KT, WQ, NQ><<<dim3((unsigned)(qt * pairs * a.q_parts)), 256, 0, stream>>>(a);
+        attention_dq_kernel<T, DP, KT, WQ><<<dim3((unsigned)(qt * pairs * a.q_parts)), 256, 0, stream>>>(a);
         if (a.q_parts > 1) attention_sum_kernel<T, true><<<sums(a.q_len, a.heads), 256, 0, stream>>>(a);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (kt > 0) {
-        attention_dkv_kernel<T, DP, QT, WK, NK><<<dim3((unsigned)(kt * pairs * a.k_parts)), 256, 0, stream>>>(a);
+        attention_dkv_kernel<T, DP, QT, WK><<<dim3((unsigned)(kt * pairs * a.k_parts)), 256, 0, stream>>>(a);
         if (a.k_parts > 1) attention_sum_kernel<T, false><<<sums(a.k_len, a.kv_heads), 256, 0, stream>>>(a);
     }
     return hipGetLastError();
@@ -372,14 +371,14 @@ hipError_t launch_attention_bwd(const AttnArgs& a, bool bf16, hipStream_t stream
 {
     const int width = (a.dim + 31) / 32;
     if (bf16)
-        return width == 1 ? launch_bwd<__bf16, 32, 64, 4, 2, 64, 3, 2>(a, stream)
-             : width == 2 ? launch_bwd<__bf16, 64, 64, 3, 2, 64, 3, 2>(a, stream)
-             : width == 3 ? launch_bwd<__bf16, 96, 32, 2, 2, 32, 2, 2>(a, stream)
-                          : launch_bwd<__bf16, 128, 32, 2, 2, 32, 2, 2>(a, stream);
-    return width == 1 ? launch_bwd<float, 32, 32, 2, 2, 32, 2, 2>(a, stream)
-         : width == 2 ? launch_bwd<float, 64, 32, 2, 2, 32, 2, 2>(a, stream)
-         : width == 3 ? launch_bwd<float, 96, 32, 1, 2, 32, 1, 2>(a, stream)
-                      : launch_bwd<float, 128, 32, 1, 2, 32, 1, 2>(a, stream);
+        return width == 1 ? launch_bwd<__bf16, 32, 64, 4, 64, 3>(a, stream)
+             : width == 2 ? launch_bwd<__bf16, 64, 64, 3, 64, 3>(a, stream)
+             : width == 3 ? launch_bwd<__bf16, 96, 32, 2, 32, 2>(a, stream)
+                          : launch_bwd<__bf16, 128, 32, 2, 32, 2>(a, stream);
+    return width == 1 ? launch_bwd<float, 32, 32, 2, 32, 2>(a, stream)
+         : width == 2 ? launch_bwd<float, 64, 32, 2, 32, 2>(a, stream)
+         : width == 3 ? launch_bwd<float, 96, 32, 1, 32, 1>(a, stream)
+                      : launch_bwd<float, 128, 32, 1, 32, 1>(a, stream);
 }
 
 }  // namespace dpb
