@@ -421,7 +421,7 @@ typedef struct {
 /* Bytes of device workspace that dpb_attention / dpb_attention_bwd need (0 for
  * a NULL or empty description).  The forward needs some where it splits the keys
  * of few query rows over many workgroups; the backward two floats per query row and
- * head. */
+ * head, and its gradients in fp32 per part where it splits them. */
 size_t dpb_attention_workspace_bytes(const dpb_attn* a);
 size_t dpb_attention_bwd_workspace_bytes(const dpb_attn* a);
 
@@ -430,7 +430,8 @@ size_t dpb_attention_bwd_workspace_bytes(const dpb_attn* a);
  * A query that sees no key, and a padded row that takes no part, gets out = 0 and
  * lse = -inf.
  *   dtype   : of q, k, v and out (DPB_F32 or DPB_BF16)
- *   q, out  : heads heads;  k, v: kv_heads heads
+ *   q, out  : heads heads;  k, v: kv_heads heads (out is written; must not
+ *             overlap the inputs)
  *   lse     : device fp32 [rows of q, heads] (padded: [batch, q_len, heads])
  * Scores, softmax and sums are fp32; with bf16 the probabilities are rounded to
  * bf16 as operands of the product with V.  The forms: tiles of query rows against

@@ -76,6 +76,19 @@ dpb_status take(const dpb_attn* a, dpb_dtype t, const dpb_heads* x, bool q, Attn
     return out->ts >= kMaxTokenBytes ? DPB_EUNSUPPORTED : DPB_OK;
 }
 
+// An output that is an input (or another output) would be read after it is written.
+template <int NO, int NI>
+bool overlap(const void* const (&outs)[NO], const void* const (&ins)[NI])
+{
+    for (int i = 0; i < NO; ++i) {
+        for (const void* p : ins)
+            if (outs[i] && outs[i] == p) return true;
+        for (int j = 0; j < i; ++j)
+            if (outs[i] && outs[i] == outs[j]) return true;
+    }
+    return false;
+}
+
 // One float per query row and head (the backward has two arrays of them, before its parts).
 size_t row_bytes(const dpb_attn* a) { return ((size_t)rows_of(a, true) * a->heads * 4 + 15) / 16 * 16; }
 
@@ -143,6 +156,7 @@ dpb_status dpb_attention(const dpb_attn* a, dpb_dtype dtype, const dpb_heads* q,
     g.splits = dpb::attention_splits(g.batch, g.q_len, g.k_len, g.heads, g.kv_heads);
     const size_t need = dpb::attention_part_floats(g.q_rows, g.heads, g.dim, g.splits) * 4;
     if (need && (!workspace || !aligned16(workspace) || ws_bytes < need)) return DPB_EINVAL;
+    if (overlap<1, 3>({g.o.p}, {g.q.p, g.k.p, g.v.p})) return DPB_EINVAL;
     g.part = (float*)workspace;
     return launched(dpb::launch_attention(g, dtype == DPB_BF16, (hipStream_t)stream));
 }
@@ -166,15 +180,7 @@ dpb_status dpb_attention_bwd(const dpb_attn* a, dpb_dtype dtype, const dpb_heads
     const size_t need = dpb_attention_bwd_workspace_bytes(a);
     if (g.q_rows > 0 && (!lse || !aligned16(lse))) return DPB_EINVAL;
     if (need && (!workspace || !aligned16(workspace) || ws_bytes < need)) return DPB_EINVAL;
-    // an output that is an input (or another output) would be read after it is written
-    const void* outs[3] = {g.gq.p, g.gk.p, g.gv.p};
-    const void* ins[5] = {g.go.p, g.q.p, g.k.p, g.v.p, g.o.p};
-    for (int i = 0; i < 3; ++i) {
-        for (const void* p : ins)
-            if (outs[i] && outs[i] == p) return DPB_EINVAL;
-        for (int j = 0; j < i; ++j)
-            if (outs[i] && outs[i] == outs[j]) return DPB_EINVAL;
-    }
+    if (overlap<3, 5>({g.gq.p, g.gk.p, g.gv.p}, {g.go.p, g.q.p, g.k.p, g.v.p, g.o.p})) return DPB_EINVAL;
     g.lse = const_cast<float*>(lse);
     g.row_lse2 = (float*)workspace;
     g.row_delta = (float*)((char*)workspace + row_bytes(a));

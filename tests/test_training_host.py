@@ -22,7 +22,8 @@ def heads(data=1 << 20, batch=4096, token=256, head=64):
 
 
 def forward(a, dtype=1, q=None, k=None, v=None, out=None, lse=1 << 20, ws=None, n=0):
-    return dpb.load().dpb_attention(a, dtype, q or heads(), k or heads(), v or heads(), out or heads(), lse, ws, n, None)
+    return dpb.load().dpb_attention(a, dtype, q or heads(), k or heads(), v or heads(), out or heads(2 << 20),
+                                    lse, ws, n, None)
 
 
 def backward(a, dtype=1, outs=(2 << 20, 3 << 20, 4 << 20), lse=1 << 20, ws=1 << 20, n=1 << 40):
@@ -71,6 +72,8 @@ def test_bad_workspaces_and_overlaps():
     assert forward(a) == EINVAL and forward(a, ws=1 << 20, n=need - 1) == EINVAL
     assert forward(a, ws=(1 << 20) + 4, n=need) == EINVAL
     a = attn()
+    for name in ("q", "k", "v"):
+        assert forward(a, **{name: heads(5 << 20)}, out=heads(5 << 20)) == EINVAL, name
     need = dpb.load().dpb_attention_bwd_workspace_bytes(a)
     assert need >= 2 * 4 * 2 * 5 * 4
     assert backward(a, n=need - 1) == EINVAL and backward(a, ws=0) == EINVAL
