@@ -403,7 +403,8 @@ typedef struct {
  *    starts[b + 1], at most q_len / k_len of them (the longest sequence, or more).
  *    q_rows, k_rows: rows of the tensors.  q_lens and k_lens must be NULL.  Starts
  *    outside the tensor are clamped to it; output rows that belong to no sequence
- *    are not written.
+ *    are not written, so that several calls may share a tensor
+ *    (dpb_attention_clear writes those rows).
  *  - Query heads share key heads: head h reads key head h / (heads / kv_heads).
  *  - With `causal`, query i of a sequence of q queries and k keys sees the keys
  *    j <= i + k - q (the last query sees them all); without it, all k.
@@ -461,6 +462,13 @@ dpb_status dpb_attention_bwd(const dpb_attn* a, dpb_dtype dtype, const dpb_heads
                              const dpb_heads* k, const dpb_heads* v, const dpb_heads* out, const float* lse,
                              const dpb_heads* dq, const dpb_heads* dk, const dpb_heads* dv, void* workspace,
                              size_t ws_bytes, void* stream);
+
+/* ROWS OF NO SEQUENCE of a packed call become what padded rows that take no part
+ * get: 0 in out (or dq), dk and dv, -inf in lse.  These are the rows before the first
+ * start, behind the last one, and behind a sequence's first q_len / k_len.  Any of
+ * the four may be NULL; padded calls have no such rows. */
+dpb_status dpb_attention_clear(const dpb_attn* a, dpb_dtype dtype, const dpb_heads* out, float* lse,
+                               const dpb_heads* dk, const dpb_heads* dv, void* stream);
 
 /* Elements that share the scales of 8-bit optimizer states. */
 #define DPB_ADAMW_BLOCK 256

@@ -71,6 +71,7 @@ def load():
         "dpb_attention_bwd_workspace_bytes": (ctypes.c_size_t, [P]),
         "dpb_attention": (i32, [P, i32] + [P] * 6 + [ctypes.c_size_t, P]),
         "dpb_attention_bwd": (i32, [P, i32] + [P] * 10 + [ctypes.c_size_t, P]),
+        "dpb_attention_clear": (i32, [P, i32] + [P] * 5),
         "dpb_adamw_blocks": (i64, [P, i32]),
         "dpb_adamw_step": (i32, [P, i32, P, P, P, P, i32, i32, i32, P, P, P, P, P, P]),
     }
@@ -509,8 +510,11 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = 
     lengths q_lens / k_lens int32 [B] or none; packed: q [rows, H, D], k and v
     [rows, Hkv, D] with q_starts / k_starts int32 [B + 1] and the longest sequences
     max_q / max_k.  scale defaults to 1 / sqrt(D); causal: query i sees the keys
-    j <= i + k_len - q_len.  A query that sees none gets 0 and lse -inf."""
+    j <= i + k_len - q_len.  A query that sees none gets 0 and lse -inf, and so do packed
+    rows of no sequence in outputs made here; in an out or lse that is given those
+    rows are left as they are."""
     a = _attn(q, k, v, causal, scale, q_lens, k_lens, q_starts, k_starts, max_q, max_k)
+    new_out, new_lse = out is None, lse is None
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     if lse is None:
@@ -525,6 +529,10 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = 
         a, _dtype_code(q), _heads(q, "q"), _heads(k, "k"), _heads(v, "v"), _heads(out, "out"), _dev(lse, "lse"),
         _opt(workspace, "workspace"), 0 if workspace is None else workspace.numel() * workspace.element_size(),
         _stream(q)))
+    if q_starts is not None and (new_out or new_lse):
+        _check("dpb_attention_clear", lib.dpb_attention_clear(
+            a, _dtype_code(q), _heads(out, "out") if new_out else None, _dev(lse, "lse") if new_lse else None, None, None,
+            _stream(q)))
     return out, lse
 
 
@@ -536,10 +544,12 @@ def attention_bwd(grad_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: t
                   dk: torch.Tensor | None = None, dv: torch.Tensor | None = None,
                   workspace: torch.Tensor | None = None):
     """Gradients (dq, dk, dv) of attention for grad_out, from its out and lse; the
-    other arguments as in the forward call."""
+    other arguments as in the forward call.  Packed rows of no sequence are 0 in
+    gradients made here and left as they are in those that are given."""
     a = _attn(q, k, v, causal, scale, q_lens, k_lens, q_starts, k_starts, max_q, max_k)
     assert grad_out.shape == out.shape == q.shape and grad_out.dtype == out.dtype == q.dtype
     assert lse.shape == q.shape[:-1] and lse.dtype == torch.float32
+    new_q, new_k, new_v = dq is None, dk is None, dv is None
     grads = []
     for x, g in ((q, dq), (k, dk), (v, dv)):
         grads.append(torch.empty(x.shape, dtype=x.dtype, device=x.device) if g is None else g)
@@ -553,6 +563,10 @@ def attention_bwd(grad_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: t
         a, _dtype_code(q), _heads(grad_out, "grad_out"), _heads(q, "q"), _heads(k, "k"), _heads(v, "v"),
         _heads(out, "out"), _dev(lse, "lse"), _heads(dq, "dq"), _heads(dk, "dk"), _heads(dv, "dv"),
         _dev(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream(q)))
+    if q_starts is not None and (new_q or new_k or new_v):
+        _check("dpb_attention_clear", lib.dpb_attention_clear(
+            a, _dtype_code(q), _heads(dq, "dq") if new_q else None, None, _heads(dk, "dk") if new_k else None,
+            _heads(dv, "dv") if new_v else None, _stream(q)))
     return dq, dk, dv
 
 

@@ -161,6 +161,22 @@ dpb_status dpb_attention(const dpb_attn* a, dpb_dtype dtype, const dpb_heads* q,
     return launched(dpb::launch_attention(g, dtype == DPB_BF16, (hipStream_t)stream));
 }
 
+dpb_status dpb_attention_clear(const dpb_attn* a, dpb_dtype dtype, const dpb_heads* out, float* lse,
+                               const dpb_heads* dk, const dpb_heads* dv, void* stream)
+{
+    dpb_status s = check_sizes(a);
+    if (s) return s;
+    if (!dtype_ok(dtype) || !aligned16(lse)) return DPB_EINVAL;
+    AttnArgs g;
+    fill_args(a, &g);
+    const struct { const dpb_heads* x; bool q; AttnRows* to; } all[3] = {{out, true, &g.o}, {dk, false, &g.gk}, {dv, false, &g.gv}};
+    for (const auto& t : all)
+        if (t.x && (s = take(a, dtype, t.x, t.q, t.to))) return s;
+    if (!packed(a) || !(out || lse || dk || dv)) return DPB_OK;
+    g.lse = lse;
+    return launched(dpb::launch_attention_clear(g, dtype == DPB_BF16, (hipStream_t)stream));
+}
+
 dpb_status dpb_attention_bwd(const dpb_attn* a, dpb_dtype dtype, const dpb_heads* grad_out, const dpb_heads* q,
                              const dpb_heads* k, const dpb_heads* v, const dpb_heads* out, const float* lse,
                              const dpb_heads* dq, const dpb_heads* dk, const dpb_heads* dv, void* workspace,

@@ -381,6 +381,49 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a)
     if (e == 0) a.lse[at] = log_sum(zero_of, sum);
 }
 
+// Rows of a packed call that belong to no sequence: before the first, behind the last, and
+// where a sequence is longer than the longest.  A workgroup takes whole sequences' rows,
+// and all share the rows at the two ends.  Nothing but the starts is read where
+// every row has a sequence: the launch is what it costs.
+constexpr int kClearBlocks = 1024;
+
+template <typename F>
+__device__ __forceinline__ void each_loose_row(const int32_t* starts, int64_t rows, int len, int batch, F&& clear)
+{
+    for (int b = blockIdx.x; b < batch; b += gridDim.x) {
+        int64_t first;
+        int n, written;
+        sequence_rows(starts, nullptr, rows, len, b, first, n, written);
+        const int64_t end = min(max((int64_t)starts[b + 1], first), rows);
+        clear(first + written, end, (int64_t)threadIdx.x, (int64_t)blockDim.x);
+    }
+    const int64_t at = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, step = (int64_t)gridDim.x * blockDim.x;
+    const int64_t begin = min(max((int64_t)starts[0], (int64_t)0), rows);
+    const int64_t end = batch > 0 ? min(max((int64_t)starts[batch], begin), rows) : begin;
+    clear((int64_t)0, begin, at, step);
+    clear(end, rows, at, step);
+}
+
+__global__ __launch_bounds__(256) void attention_clear_kernel(AttnArgs a, int chunks)
+{
+    // rows `from` to `to` of t, 16 bytes at a time, of which this thread has at, at + step, ...
+    auto zero = [&](const AttnRows& t, int heads, int64_t from, int64_t to, int64_t at, int64_t step) {
+        const int64_t per = (int64_t)heads * chunks;
+        for (int64_t x = at; t.p && x < (to - from) * per; x += step) {
+            const int64_t row = from + x / per, head = x % per / chunks, c = x % chunks;
+            *(u32x4*)(t.p + row * t.ts + head * t.hs + c * 16) = (u32x4){0, 0, 0, 0};
+        }
+    };
+    each_loose_row(a.q_starts, a.q_rows, a.q_len, a.batch, [&](int64_t from, int64_t to, int64_t at, int64_t step) {
+        zero(a.o, a.heads, from, to, at, step);
+        for (int64_t x = at; a.lse && x < (to - from) * a.heads; x += step) a.lse[from * a.heads + x] = -INFINITY;
+    });
+    each_loose_row(a.k_starts, a.k_rows, a.k_len, a.batch, [&](int64_t from, int64_t to, int64_t at, int64_t step) {
+        zero(a.gk, a.kv_heads, from, to, at, step);
+        zero(a.gv, a.kv_heads, from, to, at, step);
+    });
+}
+
 // W: waves per SIMD that the registers are to allow.
 template <typename T, int DP, int KT, int W>
 hipError_t launch_tiles(const AttnArgs& a, hipStream_t stream)
@@ -419,6 +462,12 @@ int attention_splits(int batch, int q_len, int k_len, int heads, int kv_heads)
 size_t attention_part_floats(int64_t q_rows, int heads, int dim, int splits)
 {
     return splits > 1 ? (size_t)q_rows * heads * splits * (dim + 4) : 0;
+}
+
+hipError_t launch_attention_clear(const AttnArgs& a, bool bf16, hipStream_t stream)
+{
+    attention_clear_kernel<<<kClearBlocks, 256, 0, stream>>>(a, a.dim * (bf16 ? 2 : 4) / 16);
+    return hipGetLastError();
 }
 
 hipError_t launch_attention(const AttnArgs& a, bool bf16, hipStream_t stream)

@@ -53,6 +53,9 @@ struct AttnArgs {
 
 hipError_t launch_attention(const AttnArgs& a, bool bf16, hipStream_t stream);
 hipError_t launch_attention_bwd(const AttnArgs& a, bool bf16, hipStream_t stream);
+// Packed calls: rows that belong to no sequence become 0 in o, gk and gv, -inf in lse
+// (each where it is not null).
+hipError_t launch_attention_clear(const AttnArgs& a, bool bf16, hipStream_t stream);
 // Parts that the keys of a forward call are split into (0: whole, by tiles of 128
 // rows), and the scratch floats that takes.
 int attention_splits(int batch, int q_len, int k_len, int heads, int kv_heads);
