@@ -51,7 +51,8 @@ typedef enum {
     DPB_EINVAL = -1,       /* bad argument (shape, pointer, alignment, dtype) */
     DPB_EUNSUPPORTED = -2, /* valid per the paper but outside what this library supports */
     DPB_EHIP = -3,         /* a HIP runtime call or kernel launch failed */
-    DPB_ENOMEM = -4        /* device or host allocation failed (plan creation only) */
+    DPB_ENOMEM = -4        /* device or host allocation failed (plan creation; an
+                              optimizer step over more than 96 tensors) */
 } dpb_status;
 
 /* Opaque plan: the hierarchy and the constant tables derived from it
@@ -505,8 +506,10 @@ typedef struct {
  *                   neighbour's distance is lost)
  *   grad_scale    : device fp32 scalar (loss scaling, clipping), or NULL for 1
  * m, v, scales and master are 16-byte aligned; tensor i's part starts at block
- * dpb_adamw_blocks(sizes, i).  Arithmetic is fp32.  DPB_EINVAL for a bad pointer,
- * size or setting (0 <= beta < 1, eps > 0, step >= 1, finite values). */
+ * dpb_adamw_blocks(sizes, i).  Arithmetic is fp32.  What is written (params, m, v,
+ * scales, master) may not overlap anything else of the call: a tensor given twice
+ * would be two workgroups' at once.  DPB_EINVAL for that and for a bad pointer, size or
+ * setting (0 <= beta < 1, eps > 0, step >= 1, finite values). */
 dpb_status dpb_adamw_step(const dpb_adamw* settings, int count, void* const* params, const void* const* grads,
                           const int64_t* sizes, const float* weight_decay, dpb_dtype param_dtype,
                           dpb_dtype grad_dtype, int state_bits, void* m, void* v, float* scales, float* master,

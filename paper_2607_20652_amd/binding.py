@@ -610,7 +610,8 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m:
     """One AdamW step over all params in place, with the states of adamw_state (8
     bits when scales are given).  weight_decay: one for all, or one per tensor; seed:
     of the rounding of 8-bit states, another one each step; grad_scale: a device
-    scalar that multiplies the gradients.  All params have one type, all grads one."""
+    scalar that multiplies the gradients.  All params have one type, all grads one;
+    what is written (params and states) overlaps nothing else."""
     n = len(params)
     assert len(grads) == n
     if n == 0:

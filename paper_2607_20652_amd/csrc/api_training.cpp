@@ -4,6 +4,8 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <memory>
+#include <new>
 
 #include "../../include/dpb.h"
 #include "adamw.hpp"
@@ -85,6 +87,25 @@ bool overlap(const void* const (&outs)[NO], const void* const (&ins)[NI])
             if (outs[i] && outs[i] == p) return true;
         for (int j = 0; j < i; ++j)
             if (outs[i] && outs[i] == outs[j]) return true;
+    }
+    return false;
+}
+
+// A stretch of memory that a call reads, or writes (and reads).
+struct Span {
+    uintptr_t begin, end;
+    bool written;
+};
+
+// Does one that is written share a byte with any other?
+bool races(Span* s, size_t n)
+{
+    std::sort(s, s + n, [](const Span& a, const Span& b) { return a.begin < b.begin; });
+    uintptr_t read = 0, written = 0;   // ends of what begins before
+    for (size_t i = 0; i < n; ++i) {
+        if (s[i].begin < written || (s[i].written && s[i].begin < read)) return true;
+        uintptr_t& end = s[i].written ? written : read;
+        end = std::max(end, s[i].end);
     }
     return false;
 }
@@ -239,6 +260,30 @@ dpb_status dpb_adamw_step(const dpb_adamw* o, int count, void* const* params, co
     if (!m || !v || !aligned16(m) || !aligned16(v) || !aligned16(scales) || !aligned16(master) ||
         ((uintptr_t)grad_scale & 3u) || (state_bits == 8 && !scales))
         return DPB_EINVAL;
+    // every weight and state is one workgroup's: a tensor given twice, or one that lies in another, is not
+    constexpr int kOthers = 5, kOnStack = 2 * 96 + kOthers;
+    Span some[kOnStack], *spans = some;
+    std::unique_ptr<Span[]> many;
+    if (2 * (int64_t)count + kOthers > kOnStack) {
+        many.reset(new (std::nothrow) Span[2 * (size_t)count + kOthers]);
+        if (!(spans = many.get())) return DPB_ENOMEM;
+    }
+    size_t n_spans = 0;
+    auto span = [&](const void* p, int64_t bytes, bool written) {
+        if (p) spans[n_spans++] = {(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, written};
+    };
+    for (int i = 0; i < count; ++i)
+        if (sizes[i] > 0) {
+            span(params[i], sizes[i] * bytes_of(param_dtype), true);
+            span(grads[i], sizes[i] * bytes_of(grad_dtype), false);
+        }
+    const int64_t states = blocks * DPB_ADAMW_BLOCK;
+    span(m, states * state_bits / 8, true);
+    span(v, states * state_bits / 8, true);
+    if (state_bits == 8) span(scales, blocks * 8, true);
+    span(master, states * 4, true);
+    span(grad_scale, 4, false);
+    if (races(spans, n_spans)) return DPB_EINVAL;
 
     dpb::AdamwArgs g;
     std::memset((void*)&g, 0, sizeof g);

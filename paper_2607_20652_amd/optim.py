@@ -27,6 +27,8 @@ class AdamW:
         self.lr, self.betas, self.eps, self.bits, self.seed = lr, betas, eps, bits, seed
         self.steps = 0
         pairs = [p if isinstance(p, tuple) else (p, weight_decay) for p in params]
+        if len({id(p) for p, _ in pairs}) != len(pairs):
+            raise ValueError("a parameter is given twice")
         self.groups = []
         for dtype in (torch.float32, torch.bfloat16):
             mine = [(p, wd) for p, wd in pairs if p.dtype == dtype]
