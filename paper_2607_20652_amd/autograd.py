@@ -30,6 +30,7 @@ and `ParityBlock` the two sublayers of one transformer block.
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as B
 
@@ -127,7 +128,8 @@ class DPBMLP(torch.nn.Module):
 
 class AttentionLayer(torch.autograd.Function):
     """Attention of padded sequences, q [B, Sq, H, D], k and v [B, Sk, Hkv, D] -> [B, Sq, H, D];
-    the backward recomputes the probabilities from the log-sum-exp."""
+    the backward recomputes the probabilities from the log-sum-exp.  Second derivatives are
+    an error: the library's gradients have no graph."""
 
     @staticmethod
     def forward(ctx, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = False,
@@ -138,6 +140,7 @@ class AttentionLayer(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad: torch.Tensor):
         q, k, v, out, lse, q_lens, k_lens = ctx.saved_tensors
         if grad.stride() != out.stride():   # an expanded gradient, say

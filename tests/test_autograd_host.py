@@ -1,0 +1,51 @@
+"""The differentiable functions without a GPU: the library's calls are replaced by the same
+formulas in torch, so that what is tested is how the results meet autograd."""
+import math
+
+import pytest
+import torch
+
+from paper_2607_20652_amd import autograd as A
+from paper_2607_20652_amd import binding as B
+
+
+def plain_attention(q, k, v, causal=False, scale=None, q_lens=None, k_lens=None):
+    k, v = (x.repeat_interleave(q.shape[2] // x.shape[2], 2) for x in (k, v))
+    s = torch.einsum("bihd,bjhd->bhij", q, k) * (q.shape[-1] ** -0.5 if scale is None else scale)
+    if causal:
+        n, m = s.shape[-2:]
+        s = s.masked_fill(torch.arange(m) > torch.arange(n)[:, None] + m - n, -math.inf)
+    return torch.einsum("bhij,bjhd->bihd", s.softmax(-1), v), s.logsumexp(-1).transpose(1, 2)
+
+
+def plain_attention_bwd(grad, q, k, v, out, lse, causal=False, scale=None, q_lens=None, k_lens=None):
+    with torch.enable_grad():
+        x = [t.detach().requires_grad_() for t in (q, k, v)]
+        return torch.autograd.grad(plain_attention(*x, causal, scale)[0], x, grad)
+
+
+@pytest.fixture
+def plain(monkeypatch):
+    """The calls of attention as they are without a graph (the library records none)."""
+    monkeypatch.setattr(B, "attention", torch.no_grad()(plain_attention))
+    monkeypatch.setattr(B, "attention_bwd", lambda *a, **kw: tuple(t.detach() for t in plain_attention_bwd(*a, **kw)))
+
+
+def qkv(dtype=torch.float64):
+    g = torch.Generator().manual_seed(0)
+    return [torch.randn(2, 5, h, 8, generator=g, dtype=dtype).requires_grad_() for h in (4, 2, 2)]
+
+
+def test_gradients_are_the_formulas(plain):
+    q, k, v = qkv()
+    assert torch.autograd.gradcheck(lambda *x: A.attention_layer(*x, True), (q, k, v))
+
+
+def test_a_second_derivative_through_attention_is_an_error(plain):
+    """A gradient penalty whose loss has another path to q: without the error it lacked attention's part."""
+    q, k, v = qkv()
+    (first,) = torch.autograd.grad((A.attention_layer(q, k, v, True) ** 2).sum() + (q ** 3).sum(), q, create_graph=True)
+    want = plain_attention_bwd(2 * plain_attention(q, k, v, True)[0].detach(), q, k, v, None, None, True)[0] + 3 * q ** 2
+    assert torch.allclose(first, want)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        first.square().sum().backward()
