@@ -70,6 +70,7 @@ class DPBLayer(torch.autograd.Function):
         return y, loss
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, gy: torch.Tensor | None, gloss: torch.Tensor | None):
         plan = ctx.plan
         x, idx, coef, u, ws = ctx.saved_tensors

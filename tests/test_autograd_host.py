@@ -49,3 +49,19 @@ def test_a_second_derivative_through_attention_is_an_error(plain):
     assert torch.allclose(first, want)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         first.square().sum().backward()
+
+
+def test_a_second_derivative_through_the_bottleneck_is_an_error(monkeypatch):
+    """A bottleneck that doubles its input, whose gradient is not differentiable either."""
+    class Plan:
+        pass
+
+    monkeypatch.setattr(B, "encode", lambda plan, x: (torch.zeros(1, dtype=torch.int32), x.detach().clone()))
+    monkeypatch.setattr(B, "decode", lambda plan, idx, coef, dtype: 2 * coef)
+    monkeypatch.setattr(B, "decode_bwd_ex", lambda plan, idx, gu, **kw: (None, 2 * gu.detach()))
+    x = torch.randn(3, 4, requires_grad=True)
+    y, _ = A.dpb_layer(x, Plan(), normalized=False)
+    (first,) = torch.autograd.grad((y ** 2).sum() + (x ** 3).sum(), x, create_graph=True)
+    assert torch.allclose(first, 8 * x + 3 * x ** 2)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        first.sum().backward()
