@@ -452,6 +452,12 @@ def std_update(plan: Plan, x: torch.Tensor, idx: torch.Tensor, stats: torch.Tens
 
 # ---- training operators beside the bottleneck: attention and AdamW
 
+def _written(tensors):
+    """Tells autograd that the library wrote these of the caller's tensors, as torch's own
+    in-place operations do: a graph that saved one before is an error afterwards."""
+    torch.autograd.graph.increment_version([t for t in tensors if t is not None and not t.is_inference()])
+
+
 # dpb_attn and dpb_heads as bytes: several times quicker to make than ctypes
 # structures, which tells in a call for one token
 _ATTN = struct.Struct("=qqqqqiiiif4xQQQQ")
@@ -514,7 +520,7 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = 
     rows of no sequence in outputs made here; in an out or lse that is given those
     rows are left as they are."""
     a = _attn(q, k, v, causal, scale, q_lens, k_lens, q_starts, k_starts, max_q, max_k)
-    new_out, new_lse = out is None, lse is None
+    new_out, new_lse, given = out is None, lse is None, (out, lse)
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     if lse is None:
@@ -533,6 +539,8 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = 
         _check("dpb_attention_clear", lib.dpb_attention_clear(
             a, _dtype_code(q), _heads(out, "out") if new_out else None, _dev(lse, "lse") if new_lse else None, None, None,
             _stream(q)))
+    if not (new_out and new_lse):
+        _written(given)
     return out, lse
 
 
@@ -549,7 +557,7 @@ def attention_bwd(grad_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: t
     a = _attn(q, k, v, causal, scale, q_lens, k_lens, q_starts, k_starts, max_q, max_k)
     assert grad_out.shape == out.shape == q.shape and grad_out.dtype == out.dtype == q.dtype
     assert lse.shape == q.shape[:-1] and lse.dtype == torch.float32
-    new_q, new_k, new_v = dq is None, dk is None, dv is None
+    new_q, new_k, new_v, given = dq is None, dk is None, dv is None, (dq, dk, dv)
     grads = []
     for x, g in ((q, dq), (k, dk), (v, dv)):
         grads.append(torch.empty(x.shape, dtype=x.dtype, device=x.device) if g is None else g)
@@ -567,6 +575,8 @@ def attention_bwd(grad_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: t
         _check("dpb_attention_clear", lib.dpb_attention_clear(
             a, _dtype_code(q), _heads(dq, "dq") if new_q else None, None, _heads(dk, "dk") if new_k else None,
             _heads(dv, "dv") if new_v else None, _stream(q)))
+    if not (new_q and new_k and new_v):
+        _written(given)
     return dq, dk, dv
 
 
@@ -643,3 +653,4 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m:
         size_arr, struct.pack(f"={n}f", *decay), _dtype_code(params[0]), _dtype_code(grads[0]),
         32 if scales is None else 8, _dev(m, "m"), _dev(v, "v"), _opt(scales, "scales"), _opt(master, "master"),
         _opt(grad_scale, "grad_scale"), _stream(m)))
+    _written([*params, m, v, scales, master])
