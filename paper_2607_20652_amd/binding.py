@@ -6,6 +6,7 @@ fallback: if libdpb.so is missing the first call raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import operator
 import os
@@ -126,9 +127,17 @@ def _stream(t: torch.Tensor):
     return torch._C._cuda_getCurrentRawStream(t.device.index)
 
 
-def _dev(t: torch.Tensor, name: str):
+def _elsewhere(t: torch.Tensor, name: str, device: int | None):
+    """The refusal of a tensor that is not on this device (None: on any)."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
+    if device is not None:
+        raise ValueError(f"{name} is on device {t.get_device()}, other tensors of the call on {device}")
+
+
+def _dev(t: torch.Tensor, name: str, device: int | None = None):
+    if t.get_device() != device:
+        _elsewhere(t, name, device)
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return ctypes.c_void_p(t.data_ptr())
@@ -287,8 +296,8 @@ def decode_bwd(plan: Plan, idx: torch.Tensor, grad_y: torch.Tensor, gx_dtype: to
     return grad_coef, grad_x
 
 
-def _opt(t: torch.Tensor | None, name: str):
-    return None if t is None else _dev(t, name)
+def _opt(t: torch.Tensor | None, name: str, device: int | None = None):
+    return None if t is None else _dev(t, name, device)
 
 
 def decode_bwd_ex(plan: Plan, idx: torch.Tensor, grad_y: torch.Tensor, add_grad_coef: torch.Tensor | None = None,
@@ -455,7 +464,11 @@ def std_update(plan: Plan, x: torch.Tensor, idx: torch.Tensor, stats: torch.Tens
 def _written(tensors):
     """Tells autograd that the library wrote these of the caller's tensors, as torch's own
     in-place operations do: a graph that saved one before is an error afterwards."""
-    torch.autograd.graph.increment_version([t for t in tensors if t is not None and not t.is_inference()])
+    tensors = [t for t in tensors if t is not None]
+    try:
+        torch.autograd.graph.increment_version(tensors)
+    except RuntimeError:   # inference tensors have no versions
+        torch.autograd.graph.increment_version([t for t in tensors if not t.is_inference()])
 
 
 # dpb_attn and dpb_heads as bytes: several times quicker to make than ctypes
@@ -464,30 +477,38 @@ _ATTN = struct.Struct("=qqqqqiiiif4xQQQQ")
 _HEADS = struct.Struct("=Qqqq")
 
 
-def _heads(t: torch.Tensor, name: str) -> bytes:
+_SAME_DEVICE = contextlib.nullcontext()
+
+
+def _device_of(t: torch.Tensor, name: str):
+    """(device, context in which it is the current one): the training operators, which have no
+    plan, run on the current device, and that has to be their tensors'."""
+    device = t.get_device()
+    if device < 0:
+        _elsewhere(t, name, None)
+    return device, _SAME_DEVICE if device == torch._C._cuda_getDevice() else torch.cuda.device(device)
+
+
+def _heads(t: torch.Tensor, name: str, device: int | None = None) -> bytes:
     st = t.stride()
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a device tensor")
+    if t.get_device() != device:
+        _elsewhere(t, name, device)
     if st[-1] != 1 and t.shape[-1] > 1:
         raise ValueError(f"{name} must be contiguous along head_dim")
     return _HEADS.pack(t.data_ptr(), st[0] if len(st) == 4 else 0, st[-3], st[-2])
 
 
-def _index(t: torch.Tensor | None, n: int, name: str) -> int:
+def _index(t: torch.Tensor | None, n: int, name: str, device: int) -> int:
     """Address of an int32 device array of n entries, or 0."""
     if t is None:
         return 0
     assert t.dtype == torch.int32 and t.shape == (n,), f"{name}: int32 [{n}]"
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a device tensor")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return t.data_ptr()
+    return _dev(t, name, device).value or 0
 
 
 def _attn(q, k, v, causal, scale, q_lens, k_lens, q_starts, k_starts, max_q, max_k) -> bytes:
     """The description of an attention call, its arguments checked."""
-    qs, ks = q.shape, k.shape
+    qs, ks, device = q.shape, k.shape, q.get_device()
     packed = q_starts is not None
     assert packed == (k_starts is not None), "packed sequences need q_starts and k_starts"
     assert len(qs) == len(ks) == (3 if packed else 4) and v.shape == ks and ks[-1] == qs[-1]
@@ -500,9 +521,9 @@ def _attn(q, k, v, causal, scale, q_lens, k_lens, q_starts, k_starts, max_q, max
         batch, q_len, k_len, q_rows, k_rows = qs[0], qs[1], ks[1], 0, 0
         assert ks[0] == batch
     return _ATTN.pack(batch, q_len, k_len, q_rows, k_rows, qs[-2], ks[-2], qs[-1], int(bool(causal)),
-                      qs[-1] ** -0.5 if scale is None else scale, _index(q_lens, batch, "q_lens"),
-                      _index(k_lens, batch, "k_lens"), _index(q_starts, batch + 1, "q_starts"),
-                      _index(k_starts, batch + 1, "k_starts"))
+                      qs[-1] ** -0.5 if scale is None else scale, _index(q_lens, batch, "q_lens", device),
+                      _index(k_lens, batch, "k_lens", device), _index(q_starts, batch + 1, "q_starts", device),
+                      _index(k_starts, batch + 1, "k_starts", device))
 
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = False, scale: float | None = None,
@@ -522,23 +543,25 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = 
     a = _attn(q, k, v, causal, scale, q_lens, k_lens, q_starts, k_starts, max_q, max_k)
     new_out, new_lse, given = out is None, lse is None, (out, lse)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if lse is None:
-        lse = torch.empty(q.shape[:-1], dtype=torch.float32, device=q.device)
+        lse = q.new_empty(q.shape[:-1], dtype=torch.float32)
     assert out.shape == q.shape and out.dtype == q.dtype
     assert lse.shape == q.shape[:-1] and lse.dtype == torch.float32
     lib = load()
-    need = lib.dpb_attention_workspace_bytes(a)
-    if need and workspace is None:
-        workspace = torch.empty((need + 3) // 4, dtype=torch.float32, device=q.device)
-    _check("dpb_attention", lib.dpb_attention(
-        a, _dtype_code(q), _heads(q, "q"), _heads(k, "k"), _heads(v, "v"), _heads(out, "out"), _dev(lse, "lse"),
-        _opt(workspace, "workspace"), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-        _stream(q)))
-    if q_starts is not None and (new_out or new_lse):
-        _check("dpb_attention_clear", lib.dpb_attention_clear(
-            a, _dtype_code(q), _heads(out, "out") if new_out else None, _dev(lse, "lse") if new_lse else None, None, None,
+    device, here = _device_of(q, "q")
+    with here:
+        need = lib.dpb_attention_workspace_bytes(a)
+        if need and workspace is None:
+            workspace = torch.empty((need + 3) // 4, dtype=torch.float32, device=q.device)
+        o, l = _heads(out, "out", device), _dev(lse, "lse", device)
+        _check("dpb_attention", lib.dpb_attention(
+            a, _dtype_code(q), _heads(q, "q"), _heads(k, "k", device), _heads(v, "v", device), o, l,
+            _opt(workspace, "workspace", device), 0 if workspace is None else workspace.numel() * workspace.element_size(),
             _stream(q)))
+        if q_starts is not None and (new_out or new_lse):
+            _check("dpb_attention_clear", lib.dpb_attention_clear(
+                a, _dtype_code(q), o if new_out else None, l if new_lse else None, None, None, _stream(q)))
     if not (new_out and new_lse):
         _written(given)
     return out, lse
@@ -560,28 +583,30 @@ def attention_bwd(grad_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: t
     new_q, new_k, new_v, given = dq is None, dk is None, dv is None, (dq, dk, dv)
     grads = []
     for x, g in ((q, dq), (k, dk), (v, dv)):
-        grads.append(torch.empty(x.shape, dtype=x.dtype, device=x.device) if g is None else g)
+        grads.append(torch.empty_like(x, memory_format=torch.contiguous_format) if g is None else g)
         assert grads[-1].shape == x.shape and grads[-1].dtype == x.dtype
     lib = load()
-    if workspace is None:
-        need = lib.dpb_attention_bwd_workspace_bytes(a)
-        workspace = torch.empty((need + 3) // 4, dtype=torch.float32, device=q.device)
     dq, dk, dv = grads
-    _check("dpb_attention_bwd", lib.dpb_attention_bwd(
-        a, _dtype_code(q), _heads(grad_out, "grad_out"), _heads(q, "q"), _heads(k, "k"), _heads(v, "v"),
-        _heads(out, "out"), _dev(lse, "lse"), _heads(dq, "dq"), _heads(dk, "dk"), _heads(dv, "dv"),
-        _dev(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream(q)))
-    if q_starts is not None and (new_q or new_k or new_v):
-        _check("dpb_attention_clear", lib.dpb_attention_clear(
-            a, _dtype_code(q), _heads(dq, "dq") if new_q else None, None, _heads(dk, "dk") if new_k else None,
-            _heads(dv, "dv") if new_v else None, _stream(q)))
+    device, here = _device_of(q, "q")
+    with here:
+        if workspace is None:
+            need = lib.dpb_attention_bwd_workspace_bytes(a)
+            workspace = torch.empty((need + 3) // 4, dtype=torch.float32, device=q.device)
+        gq, gk, gv = _heads(dq, "dq", device), _heads(dk, "dk", device), _heads(dv, "dv", device)
+        _check("dpb_attention_bwd", lib.dpb_attention_bwd(
+            a, _dtype_code(q), _heads(grad_out, "grad_out", device), _heads(q, "q"), _heads(k, "k", device),
+            _heads(v, "v", device), _heads(out, "out", device), _dev(lse, "lse", device), gq, gk, gv,
+            _dev(workspace, "workspace", device), workspace.numel() * workspace.element_size(), _stream(q)))
+        if q_starts is not None and (new_q or new_k or new_v):
+            _check("dpb_attention_clear", lib.dpb_attention_clear(
+                a, _dtype_code(q), gq if new_q else None, None, gk if new_k else None, gv if new_v else None, _stream(q)))
     if not (new_q and new_k and new_v):
         _written(given)
     return dq, dk, dv
 
 
 ADAMW_BLOCK = 256
-_KIND = operator.attrgetter("dtype", "is_cuda")
+_DTYPE = operator.attrgetter("dtype")
 
 
 class _AdamW(ctypes.Structure):
@@ -629,10 +654,9 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m:
     sizes = list(map(torch.Tensor.numel, params))
     assert list(map(torch.Tensor.numel, grads)) == sizes
     for tensors in (params, grads):
-        kinds = set(map(_KIND, tensors))
-        assert len({dtype for dtype, _ in kinds}) == 1
-        if not all(cuda for _, cuda in kinds):
-            raise ValueError("params and grads must be device tensors")
+        assert len(set(map(_DTYPE, tensors))) == 1
+        if set(map(torch.Tensor.get_device, tensors)) != {m.get_device()} or not m.is_cuda:
+            raise ValueError("params and grads must be device tensors, on the states' device")
         if not all(map(torch.Tensor.is_contiguous, tensors)):
             raise ValueError("params and grads must be contiguous")
     size_arr = struct.pack(f"={n}q", *sizes)
@@ -647,10 +671,12 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m:
     assert len(decay) == n
     pointers = struct.Struct(f"={n}Q")
     o = _AdamW(lr, betas[0], betas[1], eps, step, seed & 0xFFFFFFFF)
-    _check("dpb_adamw_step", lib.dpb_adamw_step(
-        ctypes.byref(o), n, pointers.pack(*map(torch.Tensor.data_ptr, params)),
-        pointers.pack(*map(torch.Tensor.data_ptr, grads)),
-        size_arr, struct.pack(f"={n}f", *decay), _dtype_code(params[0]), _dtype_code(grads[0]),
-        32 if scales is None else 8, _dev(m, "m"), _dev(v, "v"), _opt(scales, "scales"), _opt(master, "master"),
-        _opt(grad_scale, "grad_scale"), _stream(m)))
+    device, here = _device_of(m, "m")
+    with here:
+        _check("dpb_adamw_step", lib.dpb_adamw_step(
+            ctypes.byref(o), n, pointers.pack(*map(torch.Tensor.data_ptr, params)),
+            pointers.pack(*map(torch.Tensor.data_ptr, grads)),
+            size_arr, struct.pack(f"={n}f", *decay), _dtype_code(params[0]), _dtype_code(grads[0]),
+            32 if scales is None else 8, _dev(m, "m"), _dev(v, "v", device), _opt(scales, "scales", device),
+            _opt(master, "master", device), _opt(grad_scale, "grad_scale", device), _stream(m)))
     _written([*params, m, v, scales, master])
