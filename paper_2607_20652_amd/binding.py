@@ -647,10 +647,17 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m:
     of the rounding of 8-bit states, another one each step; grad_scale: a device
     scalar that multiplies the gradients.  All params have one type, all grads one;
     what is written (params and states) overlaps nothing else."""
+    _adamw(params, grads, m, v, scales, master, step, lr, betas, eps, weight_decay, grad_scale, seed)()
+
+
+def _adamw(params, grads, m, v, scales, master, step, lr, betas, eps, weight_decay, grad_scale, seed):
+    """adamw_step with its arguments checked and nothing done yet, as a function without
+    arguments (which holds the tensors' addresses: the caller keeps them alive).  A step over
+    tensors of several types thus checks all before it writes any."""
     n = len(params)
     assert len(grads) == n
     if n == 0:
-        return
+        return lambda: None
     sizes = list(map(torch.Tensor.numel, params))
     assert list(map(torch.Tensor.numel, grads)) == sizes
     for tensors in (params, grads):
@@ -672,11 +679,14 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m:
     pointers = struct.Struct(f"={n}Q")
     o = _AdamW(lr, betas[0], betas[1], eps, step, seed & 0xFFFFFFFF)
     device, here = _device_of(m, "m")
-    with here:
-        _check("dpb_adamw_step", lib.dpb_adamw_step(
-            ctypes.byref(o), n, pointers.pack(*map(torch.Tensor.data_ptr, params)),
-            pointers.pack(*map(torch.Tensor.data_ptr, grads)),
-            size_arr, struct.pack(f"={n}f", *decay), _dtype_code(params[0]), _dtype_code(grads[0]),
-            32 if scales is None else 8, _dev(m, "m"), _dev(v, "v", device), _opt(scales, "scales", device),
-            _opt(master, "master", device), _opt(grad_scale, "grad_scale", device), _stream(m)))
-    _written([*params, m, v, scales, master])
+    args = (pointers.pack(*map(torch.Tensor.data_ptr, params)), pointers.pack(*map(torch.Tensor.data_ptr, grads)), size_arr,
+            struct.pack(f"={n}f", *decay), _dtype_code(params[0]), _dtype_code(grads[0]), 32 if scales is None else 8,
+            _dev(m, "m"), _dev(v, "v", device), _opt(scales, "scales", device), _opt(master, "master", device),
+            _opt(grad_scale, "grad_scale", device))
+
+    def call():
+        with here:
+            _check("dpb_adamw_step", lib.dpb_adamw_step(ctypes.byref(o), n, *args, _stream(m)))
+        _written([*params, m, v, scales, master])
+
+    return call

@@ -44,16 +44,19 @@ class AdamW:
     @torch.no_grad()
     def step(self, grad_scale: torch.Tensor | None = None):
         """One step from the parameters' gradients, times the device scalar grad_scale; a
-        parameter without a gradient is an error."""
-        self.steps += 1
-        for i, g in enumerate(self.groups):
-            grads = [p.grad for p in g["params"]]
-            if any(x is None for x in grads):
-                raise ValueError("a parameter has no gradient")
-            # the places of two groups' states are the same numbers: their seeds are not
-            B.adamw_step(g["params"], [x.contiguous() for x in grads], g["m"], g["v"], g["scales"], g["master"],
-                         step=self.steps, lr=self.lr, betas=self.betas, eps=self.eps, weight_decay=g["decay"],
-                         grad_scale=grad_scale, seed=self.seed + 2 * self.steps + i)
+        parameter without a gradient is an error, before which nothing is changed."""
+        grads = [[p.grad for p in g["params"]] for g in self.groups]
+        if any(x is None for mine in grads for x in mine):
+            raise ValueError("a parameter has no gradient")
+        grads = [[x.contiguous() for x in mine] for mine in grads]
+        steps = self.steps + 1
+        # the places of two groups' states are the same numbers: their seeds are not
+        calls = [B._adamw(g["params"], mine, g["m"], g["v"], g["scales"], g["master"], steps, self.lr, self.betas, self.eps,
+                          g["decay"], grad_scale, self.seed + 2 * steps + i)
+                 for i, (g, mine) in enumerate(zip(self.groups, grads))]
+        for call in calls:
+            call()
+        self.steps = steps
 
     def zero_grad(self):
         for g in self.groups:
