@@ -14,12 +14,20 @@ import torch
 from . import binding as B
 
 
+def _versions(tensors) -> list:
+    return [None if t.is_inference() else t._version for t in tensors]
+
+
 class AdamW:
     """params: tensors with gradients (or (tensor, weight_decay) pairs).
 
     bits: of the states, 32 or 8; master: fp32 copies of bf16 parameters that
     the steps update (default: whenever parameters are bf16); seed: of the
-    rounding of 8-bit states."""
+    rounding of 8-bit states.
+
+    Parameters that were changed since the last step (loaded, say) are taken over into their
+    masters by the next one.  It goes by their versions, which writes through .data do not
+    change: take_parameters() then does it."""
 
     def __init__(self, params: Iterable, lr: float = 1e-3, betas: tuple[float, float] = (0.9, 0.999),
                  eps: float = 1e-8, weight_decay: float = 0.0, bits: int = 32, master: bool | None = None,
@@ -37,7 +45,7 @@ class AdamW:
                 keep = dtype == torch.bfloat16 if master is None else master
                 m, v, scales, weights = B.adamw_state(tensors, bits, keep)
                 self.groups.append(dict(params=tensors, decay=[float(wd) for _, wd in mine], m=m, v=v, scales=scales,
-                                        master=weights))
+                                        master=weights, versions=_versions(tensors)))
         if sum(len(g["params"]) for g in self.groups) != len(pairs):
             raise TypeError("parameters have to be float32 or bfloat16")
 
@@ -54,9 +62,29 @@ class AdamW:
         calls = [B._adamw(g["params"], mine, g["m"], g["v"], g["scales"], g["master"], steps, self.lr, self.betas, self.eps,
                           g["decay"], grad_scale, self.seed + 2 * steps + i)
                  for i, (g, mine) in enumerate(zip(self.groups, grads))]
-        for call in calls:
+        for g, call in zip(self.groups, calls):
+            if g["master"] is not None and _versions(g["params"]) != g["versions"]:
+                self._take(g)
             call()
+            g["versions"] = _versions(g["params"])
         self.steps = steps
+
+    def take_parameters(self):
+        """Takes the parameters' present values over into the masters, where they are not
+        the masters' own, rounded."""
+        for g in self.groups:
+            if g["master"] is not None:
+                self._take(g)
+
+    @torch.no_grad()
+    def _take(self, g):
+        at = 0
+        for p in g["params"]:
+            n = p.numel()
+            mine, p = g["master"][at:at + n], p.reshape(-1)
+            mine.copy_(torch.where(mine.to(p.dtype) == p, mine, p.float()))
+            at += -(-n // B.ADAMW_BLOCK) * B.ADAMW_BLOCK
+        g["versions"] = _versions(g["params"])
 
     def zero_grad(self):
         for g in self.groups:
