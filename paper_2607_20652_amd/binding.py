@@ -624,6 +624,8 @@ def adamw_state(params: Sequence[torch.Tensor], bits: int = 32, master: bool = F
     """First states (m, v, scales, master) of adamw_step for these tensors: m and v
     fp32, or 8-bit floats with scales [blocks, 2]; master: fp32 copies of the
     tensors (or None)."""
+    if bits not in (8, 32):
+        raise ValueError(f"states have 8 or 32 bits, not {bits}")
     sizes = [p.numel() for p in params]
     blocks, dev = adamw_blocks(sizes), params[0].device
     m, v = (torch.zeros(blocks * ADAMW_BLOCK, dtype=torch.float32 if bits == 32 else torch.float8_e4m3fn, device=dev)
