@@ -386,8 +386,9 @@ dpb_status dpb_variance_grad(const dpb_plan* plan, int64_t T, const void* worksp
 /* One [sequences, tokens, heads, head_dim] tensor of an attention call: device
  * pointer, 16-byte aligned, and strides in ELEMENTS, each a multiple of 16
  * bytes; the elements of a head are contiguous.  Any order of the dimensions and
- * views into larger tensors are fine, and so are inputs whose strides are 0; a
- * stride along which there is one entry is ignored.  With packed sequences the
+ * views into larger tensors are fine, and so are inputs whose strides are 0 (an
+ * output's are head_dim or more: its rows may not share memory); a stride along
+ * which there is one entry is ignored.  With packed sequences the
  * tensor is [tokens, heads, head_dim] and batch_stride is ignored. */
 typedef struct {
     void* data;

@@ -59,8 +59,9 @@ int64_t rows_of(const dpb_attn* a, bool q)
     return packed(a) ? (q ? a->q_rows : a->k_rows) : a->batch * (q ? a->q_len : a->k_len);
 }
 
-// One tensor: its pointer and strides in bytes.  `q`: it has the query's rows and heads.
-dpb_status take(const dpb_attn* a, dpb_dtype t, const dpb_heads* x, bool q, AttnRows* out)
+// One tensor: its pointer and strides in bytes.  `q`: it has the query's rows and heads;
+// `written`: its rows are apart from one another.
+dpb_status take(const dpb_attn* a, dpb_dtype t, const dpb_heads* x, bool q, bool written, AttnRows* out)
 {
     if (!x) return DPB_EINVAL;
     const int64_t tokens = packed(a) ? (q ? a->q_rows : a->k_rows) : (q ? a->q_len : a->k_len);
@@ -70,6 +71,10 @@ dpb_status take(const dpb_attn* a, dpb_dtype t, const dpb_heads* x, bool q, Attn
     out->ts = tokens <= 1 ? a->head_dim : x->token_stride;
     out->hs = heads <= 1 ? 0 : x->head_stride;
     if (rows_of(a, q) > 0 && (!x->data || !aligned16(x->data))) return DPB_EINVAL;
+    if (written && rows_of(a, q) > 0 &&
+        ((!packed(a) && a->batch > 1 && out->bs < a->head_dim) || (tokens > 1 && out->ts < a->head_dim) ||
+         (heads > 1 && out->hs < a->head_dim)))
+        return DPB_EINVAL;
     int64_t* strides[3] = {&out->bs, &out->ts, &out->hs};
     for (int64_t* s : strides) {
         if (*s < 0 || *s > ((int64_t)1 << 56) || (*s * bytes_of(t)) % 16) return DPB_EINVAL;
@@ -167,10 +172,10 @@ dpb_status dpb_attention(const dpb_attn* a, dpb_dtype dtype, const dpb_heads* q,
     if (!dtype_ok(dtype)) return DPB_EINVAL;
     AttnArgs g;
     fill_args(a, &g);
-    const struct { const dpb_heads* x; bool q; AttnRows* to; } all[4] = {
-        {q, true, &g.q}, {k, false, &g.k}, {v, false, &g.v}, {out, true, &g.o}};
+    const struct { const dpb_heads* x; bool q, written; AttnRows* to; } all[4] = {
+        {q, true, false, &g.q}, {k, false, false, &g.k}, {v, false, false, &g.v}, {out, true, true, &g.o}};
     for (const auto& t : all)
-        if ((s = take(a, dtype, t.x, t.q, t.to))) return s;
+        if ((s = take(a, dtype, t.x, t.q, t.written, t.to))) return s;
     if (a->batch == 0 || a->q_len == 0 || g.q_rows == 0) return DPB_OK;
     if (!lse || !aligned16(lse)) return DPB_EINVAL;
     g.lse = lse;
@@ -192,7 +197,7 @@ dpb_status dpb_attention_clear(const dpb_attn* a, dpb_dtype dtype, const dpb_hea
     fill_args(a, &g);
     const struct { const dpb_heads* x; bool q; AttnRows* to; } all[3] = {{out, true, &g.o}, {dk, false, &g.gk}, {dv, false, &g.gv}};
     for (const auto& t : all)
-        if (t.x && (s = take(a, dtype, t.x, t.q, t.to))) return s;
+        if (t.x && (s = take(a, dtype, t.x, t.q, true, t.to))) return s;
     if (!packed(a) || !(out || lse || dk || dv)) return DPB_OK;
     g.lse = lse;
     return launched(dpb::launch_attention_clear(g, dtype == DPB_BF16, (hipStream_t)stream));
@@ -208,11 +213,11 @@ dpb_status dpb_attention_bwd(const dpb_attn* a, dpb_dtype dtype, const dpb_heads
     if (!dtype_ok(dtype)) return DPB_EINVAL;
     AttnArgs g;
     fill_args(a, &g);
-    const struct { const dpb_heads* x; bool q; AttnRows* to; } all[8] = {
-        {grad_out, true, &g.go}, {q, true, &g.q}, {k, false, &g.k}, {v, false, &g.v}, {out, true, &g.o},
-        {dq, true, &g.gq}, {dk, false, &g.gk}, {dv, false, &g.gv}};
+    const struct { const dpb_heads* x; bool q, written; AttnRows* to; } all[8] = {
+        {grad_out, true, false, &g.go}, {q, true, false, &g.q}, {k, false, false, &g.k}, {v, false, false, &g.v},
+        {out, true, false, &g.o}, {dq, true, true, &g.gq}, {dk, false, true, &g.gk}, {dv, false, true, &g.gv}};
     for (const auto& t : all)
-        if ((s = take(a, dtype, t.x, t.q, t.to))) return s;
+        if ((s = take(a, dtype, t.x, t.q, t.written, t.to))) return s;
     if (a->batch == 0 || (g.q_rows == 0 && g.k_rows == 0)) return DPB_OK;
     const size_t need = dpb_attention_bwd_workspace_bytes(a);
     if (g.q_rows > 0 && (!lse || !aligned16(lse))) return DPB_EINVAL;
