@@ -445,7 +445,10 @@ size_t dpb_attention_bwd_workspace_bytes(const dpb_attn* a);
  * same 128 that a causal mask hides it from.
  * DPB_EINVAL: a bad size, pointer, stride, scale or workspace; DPB_EUNSUPPORTED:
  * head_dim over 128 or not a multiple of 8, a token stride of 16 MiB or more,
- * more than 2^31 rows or workgroups. */
+ * more than 2^31 - 256 rows or keys of a sequence (rows times the heads that share a key
+ * head) or in all packed ones, or a launch of 2^32 threads (256 for 128 query rows
+ * or, in the backward, 128 keys of a sequence and key head; for 32 rows and a part of the
+ * keys where rows are few). */
 dpb_status dpb_attention(const dpb_attn* a, dpb_dtype dtype, const dpb_heads* q, const dpb_heads* k,
                          const dpb_heads* v, const dpb_heads* out, float* lse, void* workspace, size_t ws_bytes,
                          void* stream);

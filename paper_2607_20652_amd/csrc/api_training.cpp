@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 #include <memory>
 #include <new>
 
@@ -18,7 +19,8 @@ namespace {
 using dpb::AttnArgs;
 using dpb::AttnRows;
 
-constexpr int64_t kMaxRows = ((int64_t)1 << 31) - 256;   // rows and workgroups are counted in 32 bits
+constexpr int64_t kMaxRows = ((int64_t)1 << 31) - 256;   // rows are counted in 32 bits
+constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 1;  // and so are a launch's threads
 constexpr int64_t kMaxTokenBytes = (int64_t)1 << 24;     // the rows of a tile stay within a 32-bit offset
 constexpr int kMaxDim = 128;
 
@@ -46,10 +48,58 @@ dpb_status check_sizes(const dpb_attn* a)
     const int64_t group = a->heads / a->kv_heads;
     if (a->batch > kMaxRows || a->q_len > kMaxRows / group || a->k_len > kMaxRows) return DPB_EUNSUPPORTED;
     if (a->q_starts && (a->q_rows > kMaxRows || a->k_rows > kMaxRows)) return DPB_EUNSUPPORTED;
-    // workgroups: at most 64 per 32 rows and key head, and per 128 keys and key head
-    const int64_t tiles = std::max((a->q_len * group + 31) / 32, (a->k_len + 127) / 128) * 64;
-    if (a->batch > 0 && tiles > 0 && (a->kv_heads > kMaxRows / a->batch || a->kv_heads * a->batch > kMaxRows / tiles))
-        return DPB_EUNSUPPORTED;
+    return DPB_OK;
+}
+
+// A launch of as many workgroups of 256 threads as the product of these counts is possible.
+bool launchable(std::initializer_list<int64_t> counts)
+{
+    int64_t threads = 256;
+    for (const int64_t n : counts) {
+        if (n == 0) return true;
+        if (n > kMaxThreads / threads) return false;
+        threads *= n;
+    }
+    return true;
+}
+
+int64_t tiles_of(int64_t n, int64_t each) { return (n + each - 1) / each; }
+
+// The sizes, and the grids of the launches that they lead to; the parts that those have.
+dpb_status check_forward(const dpb_attn* a, int* splits)
+{
+    *splits = 1;
+    const dpb_status s = check_sizes(a);
+    if (s || a->batch == 0 || a->q_len == 0) return s;
+    if (!launchable({a->batch, a->kv_heads})) return DPB_EUNSUPPORTED;
+    const int64_t rows = a->q_len * (a->heads / a->kv_heads);
+    *splits = dpb::attention_splits((int)a->batch, (int)a->q_len, (int)a->k_len, a->heads, a->kv_heads);
+    if (!launchable({a->batch, a->kv_heads, tiles_of(rows, *splits ? 32 : 128), std::max(*splits, 1)})) return DPB_EUNSUPPORTED;
+    if (*splits > 1 && !launchable({tiles_of(a->batch * a->kv_heads * rows, 4)})) return DPB_EUNSUPPORTED;
+    return DPB_OK;
+}
+
+// (The backward's of both types: the size of a workspace does not know the type.)
+struct Parts {
+    int q, k;
+};
+dpb_status check_backward(const dpb_attn* a, Parts (&parts)[2])
+{
+    parts[0] = parts[1] = {1, 1};
+    const dpb_status s = check_sizes(a);
+    if (s || a->batch == 0) return s;
+    if ((a->q_len || a->k_len) && !launchable({a->batch, a->kv_heads})) return DPB_EUNSUPPORTED;
+    const int64_t rows = a->q_len * (a->heads / a->kv_heads), quads = a->head_dim / 4;
+    for (const int bf16 : {0, 1}) {
+        Parts& p = parts[bf16];
+        dpb::attention_parts((int)a->batch, (int)a->q_len, (int)a->k_len, a->heads, a->kv_heads, a->head_dim, a->causal != 0,
+                             bf16, &p.q, &p.k);
+        if (!launchable({a->batch, a->kv_heads, tiles_of(rows, 128), p.q}) ||
+            !launchable({a->batch, a->kv_heads, tiles_of(a->k_len, 128), p.k}) ||
+            (p.q > 1 && !launchable({a->batch, tiles_of(rows * a->kv_heads * quads, 256)})) ||
+            (p.k > 1 && !launchable({a->batch, tiles_of(a->k_len * a->kv_heads * quads, 256)})))
+            return DPB_EUNSUPPORTED;
+    }
     return DPB_OK;
 }
 
@@ -118,6 +168,17 @@ bool races(Span* s, size_t n)
 // One float per query row and head (the backward has two arrays of them, before its parts).
 size_t row_bytes(const dpb_attn* a) { return ((size_t)rows_of(a, true) * a->heads * 4 + 15) / 16 * 16; }
 
+// Those arrays, and the parts of dQ or of dK and dV: as many as the type with more has.
+size_t bwd_bytes(const dpb_attn* a, const Parts (&parts)[2])
+{
+    size_t rows = 0;
+    for (const Parts& p : parts) {
+        if (p.q > 1) rows = std::max(rows, (size_t)p.q * rows_of(a, true) * a->heads);
+        if (p.k > 1) rows = std::max(rows, (size_t)p.k * rows_of(a, false) * a->kv_heads * 2);
+    }
+    return 2 * row_bytes(a) + rows * a->head_dim * 4;
+}
+
 void fill_args(const dpb_attn* a, AttnArgs* g)
 {
     std::memset((void*)g, 0, sizeof *g);
@@ -144,33 +205,26 @@ extern "C" {
 
 size_t dpb_attention_workspace_bytes(const dpb_attn* a)
 {
-    if (check_sizes(a) || a->batch == 0 || a->q_len == 0) return 0;
-    const int splits = dpb::attention_splits((int)a->batch, (int)a->q_len, (int)a->k_len, a->heads, a->kv_heads);
+    int splits;
+    if (check_forward(a, &splits) || a->batch == 0 || a->q_len == 0) return 0;
     return dpb::attention_part_floats(rows_of(a, true), a->heads, a->head_dim, splits) * 4;
 }
 
 size_t dpb_attention_bwd_workspace_bytes(const dpb_attn* a)
 {
-    if (check_sizes(a)) return 0;
-    size_t rows = 0;   // of the parts; the same answer for either type
-    for (const bool bf16 : {false, true}) {
-        int q_parts, k_parts;
-        dpb::attention_parts((int)a->batch, (int)a->q_len, (int)a->k_len, a->heads, a->kv_heads, a->head_dim, a->causal != 0,
-                             bf16, &q_parts, &k_parts);
-        if (q_parts > 1) rows = std::max(rows, (size_t)q_parts * rows_of(a, true) * a->heads);
-        if (k_parts > 1) rows = std::max(rows, (size_t)k_parts * rows_of(a, false) * a->kv_heads * 2);
-    }
-    return 2 * row_bytes(a) + rows * a->head_dim * 4;
+    Parts parts[2];
+    return check_backward(a, parts) ? 0 : bwd_bytes(a, parts);
 }
 
 dpb_status dpb_attention(const dpb_attn* a, dpb_dtype dtype, const dpb_heads* q, const dpb_heads* k,
                          const dpb_heads* v, const dpb_heads* out, float* lse, void* workspace, size_t ws_bytes,
                          void* stream)
 {
-    dpb_status s = check_sizes(a);
+    AttnArgs g;
+    int splits;
+    dpb_status s = check_forward(a, &splits);
     if (s) return s;
     if (!dtype_ok(dtype)) return DPB_EINVAL;
-    AttnArgs g;
     fill_args(a, &g);
     const struct { const dpb_heads* x; bool q, written; AttnRows* to; } all[4] = {
         {q, true, false, &g.q}, {k, false, false, &g.k}, {v, false, false, &g.v}, {out, true, true, &g.o}};
@@ -179,7 +233,7 @@ dpb_status dpb_attention(const dpb_attn* a, dpb_dtype dtype, const dpb_heads* q,
     if (a->batch == 0 || a->q_len == 0 || g.q_rows == 0) return DPB_OK;
     if (!lse || !aligned16(lse)) return DPB_EINVAL;
     g.lse = lse;
-    g.splits = dpb::attention_splits(g.batch, g.q_len, g.k_len, g.heads, g.kv_heads);
+    g.splits = splits;
     const size_t need = dpb::attention_part_floats(g.q_rows, g.heads, g.dim, g.splits) * 4;
     if (need && (!workspace || !aligned16(workspace) || ws_bytes < need)) return DPB_EINVAL;
     if (overlap<1, 3>({g.o.p}, {g.q.p, g.k.p, g.v.p})) return DPB_EINVAL;
@@ -208,10 +262,11 @@ dpb_status dpb_attention_bwd(const dpb_attn* a, dpb_dtype dtype, const dpb_heads
                              const dpb_heads* dq, const dpb_heads* dk, const dpb_heads* dv, void* workspace,
                              size_t ws_bytes, void* stream)
 {
-    dpb_status s = check_sizes(a);
+    AttnArgs g;
+    Parts parts[2];
+    dpb_status s = check_backward(a, parts);
     if (s) return s;
     if (!dtype_ok(dtype)) return DPB_EINVAL;
-    AttnArgs g;
     fill_args(a, &g);
     const struct { const dpb_heads* x; bool q, written; AttnRows* to; } all[8] = {
         {grad_out, true, false, &g.go}, {q, true, false, &g.q}, {k, false, false, &g.k}, {v, false, false, &g.v},
@@ -219,7 +274,7 @@ dpb_status dpb_attention_bwd(const dpb_attn* a, dpb_dtype dtype, const dpb_heads
     for (const auto& t : all)
         if ((s = take(a, dtype, t.x, t.q, t.written, t.to))) return s;
     if (a->batch == 0 || (g.q_rows == 0 && g.k_rows == 0)) return DPB_OK;
-    const size_t need = dpb_attention_bwd_workspace_bytes(a);
+    const size_t need = bwd_bytes(a, parts);
     if (g.q_rows > 0 && (!lse || !aligned16(lse))) return DPB_EINVAL;
     if (need && (!workspace || !aligned16(workspace) || ws_bytes < need)) return DPB_EINVAL;
     if (overlap<3, 5>({g.gq.p, g.gk.p, g.gv.p}, {g.go.p, g.q.p, g.k.p, g.v.p, g.o.p})) return DPB_EINVAL;
@@ -227,8 +282,8 @@ dpb_status dpb_attention_bwd(const dpb_attn* a, dpb_dtype dtype, const dpb_heads
     g.row_lse2 = (float*)workspace;
     g.row_delta = (float*)((char*)workspace + row_bytes(a));
     g.part = (float*)((char*)workspace + 2 * row_bytes(a));
-    dpb::attention_parts(g.batch, g.q_len, g.k_len, g.heads, g.kv_heads, g.dim, g.causal != 0, dtype == DPB_BF16, &g.q_parts,
-                         &g.k_parts);
+    g.q_parts = parts[dtype == DPB_BF16].q;
+    g.k_parts = parts[dtype == DPB_BF16].k;
     return launched(dpb::launch_attention_bwd(g, dtype == DPB_BF16, (hipStream_t)stream));
 }
 
