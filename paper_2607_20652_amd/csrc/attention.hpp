@@ -107,7 +107,7 @@ __device__ __forceinline__ char* head_base(const AttnRows& t, bool packed, int b
 __device__ __forceinline__ int visible_keys(const AttnArgs& a, const Sequence& s, int token)
 {
     if (token >= s.qn) return 0;
-    return a.causal ? min(max(token + 1 + s.kn - s.qn, 0), s.kn) : s.kn;
+    return a.causal ? min(max(token + 1 + (s.kn - s.qn), 0), s.kn) : s.kn;   // (both terms fit 32 bits, token + kn need not)
 }
 
 // Workgroups are numbered with the heads innermost and the longest work first: ids
