@@ -84,6 +84,12 @@ def load():
     return lib
 
 
+def _need(met: bool, what: str = "arguments of shapes or types that do not fit the call"):
+    """A condition of a call, checked under python -O too: what it guards are raw pointers."""
+    if not met:
+        raise AssertionError(what)
+
+
 def _check(fn: str, status: int):
     if status != 0:
         raise DPBError(fn, status)
@@ -214,7 +220,7 @@ def encode(plan: Plan, x: torch.Tensor, idx: torch.Tensor | None = None, coef: t
     standardized scores when stats is given.  A workspace is allocated when the
     plan needs one (wide hierarchies) and none is given."""
     T = x.shape[0]
-    assert x.dim() == 2 and x.shape[1] == plan.d
+    _need(x.dim() == 2 and x.shape[1] == plan.d)
     if idx is None:
         idx = torch.empty((T, plan.k_tot), dtype=torch.int32, device=x.device)
     if coef is None:
@@ -238,7 +244,7 @@ def encode_noalloc(plan: Plan, x: torch.Tensor, idx: torch.Tensor, coef: torch.T
     """encode (stats None) or encode_std into the given idx, coef [T, k_tot]
     through the library's allocation-free entry point (no workspace)."""
     T = x.shape[0]
-    assert x.dim() == 2 and x.shape[1] == plan.d and idx.shape == coef.shape == (T, plan.k_tot)
+    _need(x.dim() == 2 and x.shape[1] == plan.d and idx.shape == coef.shape == (T, plan.k_tot))
     _check("dpb_encode_noalloc", load().dpb_encode_noalloc(plan._handle, _dev(x, "x"), _dtype_code(x), T,
                                                            _opt(stats, "stats"), _dev(idx, "idx"),
                                                            _dev(coef, "coef"), _stream(x)))
@@ -252,7 +258,7 @@ def forward(plan: Plan, x: torch.Tensor, idx: torch.Tensor | None = None, coef: 
     given) and decode in one library call (dpb_forward); y [T, d] in out_dtype
     (default: the type of x)."""
     T = x.shape[0]
-    assert x.dim() == 2 and x.shape[1] == plan.d
+    _need(x.dim() == 2 and x.shape[1] == plan.d)
     if idx is None:
         idx = torch.empty((T, plan.k_tot), dtype=torch.int32, device=x.device)
     if coef is None:
@@ -272,8 +278,8 @@ def decode(plan: Plan, idx: torch.Tensor, coef: torch.Tensor, out_dtype: torch.d
            y: torch.Tensor | None = None):
     """(idx, coef) [T, k_tot] -> y [T, d] in out_dtype (fp32 or bf16)."""
     T = idx.shape[0]
-    assert idx.dtype == torch.int32 and coef.dtype == torch.float32 and idx.shape == coef.shape
-    assert idx.shape[1] == plan.k_tot
+    _need(idx.dtype == torch.int32 and coef.dtype == torch.float32 and idx.shape == coef.shape)
+    _need(idx.shape[1] == plan.k_tot)
     if y is None:
         y = torch.empty((T, plan.d), dtype=out_dtype, device=idx.device)
     _check("dpb_decode", load().dpb_decode(plan._handle, _dev(idx, "idx"), _dev(coef, "coef"), T, _dev(y, "y"),
@@ -285,7 +291,7 @@ def decode_bwd(plan: Plan, idx: torch.Tensor, grad_y: torch.Tensor, gx_dtype: to
                grad_coef: torch.Tensor | None = None, grad_x: torch.Tensor | None = None):
     """(idx [T, k_tot], grad_y [T, d]) -> (grad_coef [T, k_tot] fp32, grad_x [T, d])."""
     T = idx.shape[0]
-    assert idx.dtype == torch.int32 and idx.shape[1] == plan.k_tot and grad_y.shape == (T, plan.d)
+    _need(idx.dtype == torch.int32 and idx.shape[1] == plan.k_tot and grad_y.shape == (T, plan.d))
     if grad_coef is None:
         grad_coef = torch.empty((T, plan.k_tot), dtype=torch.float32, device=idx.device)
     if grad_x is None:
@@ -309,15 +315,15 @@ def decode_bwd_ex(plan: Plan, idx: torch.Tensor, grad_y: torch.Tensor, add_grad_
     statistics when given (else 1); add_grad_x is in grad_x's dtype and may
     be grad_x itself."""
     T = idx.shape[0]
-    assert idx.dtype == torch.int32 and idx.shape[1] == plan.k_tot and grad_y.shape == (T, plan.d)
+    _need(idx.dtype == torch.int32 and idx.shape[1] == plan.k_tot and grad_y.shape == (T, plan.d))
     if grad_coef is None:
         grad_coef = torch.empty((T, plan.k_tot), dtype=torch.float32, device=idx.device)
     if grad_x is None:
         grad_x = torch.empty((T, plan.d), dtype=gx_dtype or grad_y.dtype, device=idx.device)
     if add_grad_coef is not None:
-        assert add_grad_coef.dtype == torch.float32 and add_grad_coef.shape == (T, plan.k_tot)
+        _need(add_grad_coef.dtype == torch.float32 and add_grad_coef.shape == (T, plan.k_tot))
     if add_grad_x is not None:
-        assert add_grad_x.dtype == grad_x.dtype and add_grad_x.shape == (T, plan.d)
+        _need(add_grad_x.dtype == grad_x.dtype and add_grad_x.shape == (T, plan.d))
     _check("dpb_decode_bwd_ex", load().dpb_decode_bwd_ex(
         plan._handle, _dev(idx, "idx"), _dev(grad_y, "grad_y"), _dtype_code(grad_y), T,
         _opt(add_grad_coef, "add_grad_coef"), _opt(add_grad_x, "add_grad_x"), _opt(stats, "stats"),
@@ -330,11 +336,11 @@ def normalize(plan: Plan, u: torch.Tensor, ref: torch.Tensor, ref_rows: torch.Te
     """y = u ||ref_r|| / ||u|| per row (r = ref_rows[t] or t); optionally the
     (||ref_r||, ||u||) pairs [T, 2]."""
     T = u.shape[0]
-    assert u.shape == (T, plan.d) and ref.dim() == 2 and ref.shape[1] == plan.d
+    _need(u.shape == (T, plan.d) and ref.dim() == 2 and ref.shape[1] == plan.d)
     if ref_rows is not None:
-        assert ref_rows.dtype == torch.int32 and ref_rows.shape == (T,)
+        _need(ref_rows.dtype == torch.int32 and ref_rows.shape == (T,))
     else:
-        assert ref.shape[0] == T
+        _need(ref.shape[0] == T)
     if y is None:
         y = torch.empty((T, plan.d), dtype=out_dtype or u.dtype, device=u.device)
     norms = torch.empty((T, 2), dtype=torch.float32, device=u.device) if with_norms else None
@@ -350,10 +356,10 @@ def normalize_bwd(plan: Plan, g: torch.Tensor, u: torch.Tensor, ref: torch.Tenso
     """(grad_u, grad_ref) of normalize for upstream g; grad_ref is added to
     the given buffer when accumulate is True."""
     T = u.shape[0]
-    assert g.shape == u.shape == ref.shape == (T, plan.d)
+    _need(g.shape == u.shape == ref.shape == (T, plan.d))
     grad_u = torch.empty((T, plan.d), dtype=gu_dtype or g.dtype, device=u.device)
     if grad_ref is None:
-        assert not accumulate
+        _need(not accumulate)
         grad_ref = torch.empty((T, plan.d), dtype=gr_dtype or ref.dtype, device=u.device)
     _check("dpb_normalize_bwd", load().dpb_normalize_bwd(
         plan._handle, _dev(g, "g"), _dtype_code(g), _dev(u, "u"), _dtype_code(u), _dev(ref, "ref"),
@@ -367,9 +373,9 @@ def edit_codes(plan: Plan, idx: torch.Tensor, coef: torch.Tensor, rows: torch.Te
     """One edited copy of source row rows[e] per edit (slot slots[e], op
     ops[e]: EDIT_ZERO, EDIT_REPLACE, EDIT_RESCALE, EDIT_NONE) -> (idx, coef) [E, k_tot]."""
     T, E = idx.shape[0], rows.shape[0]
-    assert idx.shape == coef.shape == (T, plan.k_tot) and idx.dtype == torch.int32 and coef.dtype == torch.float32
+    _need(idx.shape == coef.shape == (T, plan.k_tot) and idx.dtype == torch.int32 and coef.dtype == torch.float32)
     for t in (rows, slots, ops):
-        assert t.dtype == torch.int32 and t.shape == (E,)
+        _need(t.dtype == torch.int32 and t.shape == (E,))
     out_idx = torch.empty((E, plan.k_tot), dtype=torch.int32, device=idx.device)
     out_coef = torch.empty((E, plan.k_tot), dtype=torch.float32, device=idx.device)
     _check("dpb_edit_codes", load().dpb_edit_codes(
@@ -394,7 +400,7 @@ def variance_loss(plan: Plan, idx: torch.Tensor, coef: torch.Tensor, n_min: int,
     [T, k_tot] fp32 or None); grad_coef is multiplied by the device scalar
     grad_scale when given."""
     T = idx.shape[0]
-    assert idx.shape == coef.shape == (T, plan.k_tot) and idx.dtype == torch.int32 and coef.dtype == torch.float32
+    _need(idx.shape == coef.shape == (T, plan.k_tot) and idx.dtype == torch.int32 and coef.dtype == torch.float32)
     if workspace is None:
         workspace = variance_workspace(plan, T, idx.device)
     loss = torch.empty((), dtype=torch.float32, device=idx.device)
@@ -436,7 +442,7 @@ def std_state(plan: Plan, device=None):
 def encode_std(plan: Plan, x: torch.Tensor, stats: torch.Tensor, idx: torch.Tensor | None = None,
                coef: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
     """Encoder on standardized scores z = (s - mu) r -> (idx, coef = z)."""
-    assert stats.dtype == torch.float32 and stats.shape == (1 << plan.level_bits[-1], 2)
+    _need(stats.dtype == torch.float32 and stats.shape == (1 << plan.level_bits[-1], 2))
     return encode(plan, x, idx, coef, stats=stats, workspace=workspace)
 
 
@@ -449,7 +455,7 @@ def std_update(plan: Plan, x: torch.Tensor, idx: torch.Tensor, stats: torch.Tens
                momentum: float, eps: float = 1e-6, workspace: torch.Tensor | None = None):
     """EMA update of (stats, m2) in place from the batch x and its code idx."""
     T = x.shape[0]
-    assert idx.shape == (T, plan.k_tot) and idx.dtype == torch.int32
+    _need(idx.shape == (T, plan.k_tot) and idx.dtype == torch.int32)
     if workspace is None:
         workspace = std_workspace(plan, x.device)
     _check("dpb_std_update", load().dpb_std_update(
@@ -502,7 +508,8 @@ def _index(t: torch.Tensor | None, n: int, name: str, device: int) -> int:
     """Address of an int32 device array of n entries, or 0."""
     if t is None:
         return 0
-    assert t.dtype == torch.int32 and t.shape == (n,), f"{name}: int32 [{n}]"
+    if t.dtype != torch.int32 or t.shape != (n,):
+        raise AssertionError(f"{name}: int32 [{n}]")
     return _dev(t, name, device).value or 0
 
 
@@ -510,16 +517,16 @@ def _attn(q, k, v, causal, scale, q_lens, k_lens, q_starts, k_starts, max_q, max
     """The description of an attention call, its arguments checked."""
     qs, ks, device = q.shape, k.shape, q.get_device()
     packed = q_starts is not None
-    assert packed == (k_starts is not None), "packed sequences need q_starts and k_starts"
-    assert len(qs) == len(ks) == (3 if packed else 4) and v.shape == ks and ks[-1] == qs[-1]
-    assert q.dtype == k.dtype == v.dtype
+    _need(packed == (k_starts is not None), "packed sequences need q_starts and k_starts")
+    _need(len(qs) == len(ks) == (3 if packed else 4) and v.shape == ks and ks[-1] == qs[-1])
+    _need(q.dtype == k.dtype == v.dtype)
     if packed:
-        assert q_lens is None and k_lens is None and max_q is not None and max_k is not None
+        _need(q_lens is None and k_lens is None and max_q is not None and max_k is not None)
         batch, q_len, k_len, q_rows, k_rows = len(q_starts) - 1, int(max_q), int(max_k), qs[0], ks[0]
-        assert batch >= 0
+        _need(batch >= 0)
     else:
         batch, q_len, k_len, q_rows, k_rows = qs[0], qs[1], ks[1], 0, 0
-        assert ks[0] == batch
+        _need(ks[0] == batch)
     return _ATTN.pack(batch, q_len, k_len, q_rows, k_rows, qs[-2], ks[-2], qs[-1], int(bool(causal)),
                       qs[-1] ** -0.5 if scale is None else scale, _index(q_lens, batch, "q_lens", device),
                       _index(k_lens, batch, "k_lens", device), _index(q_starts, batch + 1, "q_starts", device),
@@ -546,8 +553,8 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = 
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if lse is None:
         lse = q.new_empty(q.shape[:-1], dtype=torch.float32)
-    assert out.shape == q.shape and out.dtype == q.dtype
-    assert lse.shape == q.shape[:-1] and lse.dtype == torch.float32
+    _need(out.shape == q.shape and out.dtype == q.dtype)
+    _need(lse.shape == q.shape[:-1] and lse.dtype == torch.float32)
     lib = load()
     device, here = _device_of(q, "q")
     with here:
@@ -578,13 +585,13 @@ def attention_bwd(grad_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: t
     other arguments as in the forward call.  Packed rows of no sequence are 0 in
     gradients made here and left as they are in those that are given."""
     a = _attn(q, k, v, causal, scale, q_lens, k_lens, q_starts, k_starts, max_q, max_k)
-    assert grad_out.shape == out.shape == q.shape and grad_out.dtype == out.dtype == q.dtype
-    assert lse.shape == q.shape[:-1] and lse.dtype == torch.float32
+    _need(grad_out.shape == out.shape == q.shape and grad_out.dtype == out.dtype == q.dtype)
+    _need(lse.shape == q.shape[:-1] and lse.dtype == torch.float32)
     new_q, new_k, new_v, given = dq is None, dk is None, dv is None, (dq, dk, dv)
     grads = []
     for x, g in ((q, dq), (k, dk), (v, dv)):
         grads.append(torch.empty_like(x, memory_format=torch.contiguous_format) if g is None else g)
-        assert grads[-1].shape == x.shape and grads[-1].dtype == x.dtype
+        _need(grads[-1].shape == x.shape and grads[-1].dtype == x.dtype)
     lib = load()
     dq, dk, dv = grads
     device, here = _device_of(q, "q")
@@ -657,13 +664,13 @@ def _adamw(params, grads, m, v, scales, master, step, lr, betas, eps, weight_dec
     arguments (which holds the tensors' addresses: the caller keeps them alive).  A step over
     tensors of several types thus checks all before it writes any."""
     n = len(params)
-    assert len(grads) == n
+    _need(len(grads) == n)
     if n == 0:
         return lambda: None
     sizes = list(map(torch.Tensor.numel, params))
-    assert list(map(torch.Tensor.numel, grads)) == sizes
+    _need(list(map(torch.Tensor.numel, grads)) == sizes)
     for tensors in (params, grads):
-        assert len(set(map(_DTYPE, tensors))) == 1
+        _need(len(set(map(_DTYPE, tensors))) == 1)
         if set(map(torch.Tensor.get_device, tensors)) != {m.get_device()} or not m.is_cuda:
             raise ValueError("params and grads must be device tensors, on the states' device")
         if not all(map(torch.Tensor.is_contiguous, tensors)):
@@ -672,12 +679,12 @@ def _adamw(params, grads, m, v, scales, master, step, lr, betas, eps, weight_dec
     lib = load()
     elems = lib.dpb_adamw_blocks(size_arr, n) * ADAMW_BLOCK
     state = torch.float32 if scales is None else torch.float8_e4m3fn
-    assert m.dtype == v.dtype == state and m.numel() >= elems and v.numel() >= elems
-    assert scales is None or (scales.dtype == torch.float32 and scales.numel() >= elems // (ADAMW_BLOCK // 2))
-    assert master is None or (master.dtype == torch.float32 and master.numel() >= elems)
-    assert grad_scale is None or (grad_scale.dtype == torch.float32 and grad_scale.numel() == 1)
+    _need(m.dtype == v.dtype == state and m.numel() >= elems and v.numel() >= elems)
+    _need(scales is None or (scales.dtype == torch.float32 and scales.numel() >= elems // (ADAMW_BLOCK // 2)))
+    _need(master is None or (master.dtype == torch.float32 and master.numel() >= elems))
+    _need(grad_scale is None or (grad_scale.dtype == torch.float32 and grad_scale.numel() == 1))
     decay = [weight_decay] * n if isinstance(weight_decay, (int, float)) else weight_decay
-    assert len(decay) == n
+    _need(len(decay) == n)
     pointers = struct.Struct(f"={n}Q")
     o = _AdamW(lr, betas[0], betas[1], eps, step, seed & 0xFFFFFFFF)
     device, here = _device_of(m, "m")
