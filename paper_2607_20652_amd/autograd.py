@@ -144,8 +144,9 @@ class AttentionLayer(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, grad: torch.Tensor):
         q, k, v, out, lse, q_lens, k_lens = ctx.saved_tensors
-        if grad.stride() != out.stride():   # an expanded gradient, say
-            grad = grad.contiguous()
+        # an expanded gradient, say, or one behind a single number in a tensor they were joined to
+        if grad.stride() != out.stride() or grad.data_ptr() % 16:
+            grad = grad.clone(memory_format=torch.contiguous_format)
         dq, dk, dv = B.attention_bwd(grad, q, k, v, out, lse, ctx.causal, ctx.scale, q_lens, k_lens)
         return dq, dk, dv, None, None, None, None
 

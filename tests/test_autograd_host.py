@@ -65,3 +65,22 @@ def test_a_second_derivative_through_the_bottleneck_is_an_error(monkeypatch):
     assert torch.allclose(first, 8 * x + 3 * x ** 2)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         first.sum().backward()
+
+
+def test_gradients_that_start_anywhere_reach_the_library_aligned(plain, monkeypatch):
+    """The result joined to a single number: its gradient is contiguous, four bytes into the whole's."""
+    seen, bwd = [], B.attention_bwd
+
+    def note(grad, *args):
+        seen.append((grad.data_ptr() % 16, grad.is_contiguous()))
+        return bwd(grad, *args)
+
+    monkeypatch.setattr(B, "attention_bwd", note)
+    w = torch.randn(1 + 2 * 5 * 4 * 8)
+    q, k, v = qkv(torch.float32)
+    (torch.cat([q.sum()[None], A.attention_layer(q, k, v, True).flatten()]) * w).sum().backward()
+    x = [t.detach().clone().requires_grad_() for t in (q, k, v)]
+    ((A.attention_layer(*x, True).flatten() * w[1:].clone()).sum() + x[0].sum() * w[0]).backward()
+    assert seen == [(0, True)] * 2
+    for a, b in zip((q, k, v), x):
+        assert torch.allclose(a.grad, b.grad)
