@@ -195,6 +195,7 @@ class CausalAttention(torch.nn.Module):
         q, k, v = x.split((self.heads, self.kv_heads, self.kv_heads), dim=2)   # views of one tensor
         if cache is not None:
             k, v = cache.append(k, v)
+            q = q.to(k.dtype)   # (under autocast the projection's type is not the cache's)
         y = AttentionLayer.apply(q, k, v, True)
         return h + self.out(y.flatten(-2))
 

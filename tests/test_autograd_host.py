@@ -84,3 +84,27 @@ def test_gradients_that_start_anywhere_reach_the_library_aligned(plain, monkeypa
     assert seen == [(0, True)] * 2
     for a, b in zip((q, k, v), x):
         assert torch.allclose(a.grad, b.grad)
+
+
+@pytest.mark.parametrize("cached", [False, True], ids=["", "cache"])
+def test_sublayer_under_autocast(monkeypatch, cached):
+    """The projection is bf16 there and the cache fp32, as the weights are."""
+    def calls(q, k, v, *args):
+        assert q.dtype == k.dtype == v.dtype
+        out, lse = plain_attention(q, k, v, *args)
+        return out, lse.float()
+
+    monkeypatch.setattr(B, "attention", calls)
+    torch.manual_seed(0)
+    layer = A.CausalAttention(32, 4, 2)
+    h = torch.randn(2, 6, 32)
+    with torch.no_grad():
+        want = layer(h)
+        with torch.autocast("cpu", torch.bfloat16):
+            if cached:
+                cache = layer.cache(2, 6)
+                got = torch.cat([layer(h[:, :4], cache), layer(h[:, 4:5], cache), layer(h[:, 5:], cache)], 1)
+            else:
+                got = layer(h)
+    # three roundings to bf16 of values of about 1
+    assert (got.float() - want).abs().max() < 3 * 2.0 ** -8 * want.abs().max()
