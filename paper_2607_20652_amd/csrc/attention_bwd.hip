@@ -356,7 +356,8 @@ void attention_parts(int batch, int q_len, int k_len, int heads, int kv_heads, i
     // dV 97 us as 660 workgroups, 64 as 240.)
     const int64_t cus = device_cus(), pairs = std::max<int64_t>(1, (int64_t)batch * kv_heads), group = heads / kv_heads;
     const int64_t qt = std::max<int64_t>(1, (q_len * group + 127) / 128), kt = std::max<int64_t>(1, ((int64_t)k_len + 127) / 128);
-    // the kernels' workgroups a compute unit holds, by their registers and LDS
+    // the kernels' workgroups a compute unit holds, by their registers and LDS (bf16 dQ of width
+    // 32 has room for four and is counted like width 64; fp32 dQ of width 96 misses two by one register)
     const int64_t q_slots = cus * (bf16 ? dim <= 64 ? 3 : 2 : dim <= 32 ? 4 : dim <= 64 ? 2 : 1);
     const int64_t k_slots = cus * (bf16 ? dim <= 64 ? 3 : 2 : dim <= 64 ? 2 : 1);
     auto parts = [&](int64_t slots, int64_t units, int64_t most) {
