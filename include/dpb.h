@@ -440,9 +440,9 @@ size_t dpb_attention_bwd_workspace_bytes(const dpb_attn* a);
  * bf16 as operands of the product with V.  The forms: tiles of query rows against
  * the keys; for few rows (one new token over a cache) the keys are split and the
  * parts joined.  Either is deterministic.
- * A NaN or an infinity in a row of q reaches that row's results only; in a row of
- * k or v that takes part it reaches the rows that see it and may reach rows of the
- * same 128 that a causal mask hides it from.
+ * A NaN or an infinity in a row of q reaches that row's results only, in a row of k
+ * the rows that see it; in a row of v it may also reach rows that a causal mask
+ * hides it from, up to 95 tokens before the first that sees it (0 times it is no 0).
  * DPB_EINVAL: a bad size, pointer, stride, scale or workspace; DPB_EUNSUPPORTED:
  * head_dim over 128 or not a multiple of 8, a token stride of 16 MiB or more,
  * more than 2^31 - 256 rows or keys of a sequence (rows times the heads that share a key
@@ -459,8 +459,9 @@ dpb_status dpb_attention(const dpb_attn* a, dpb_dtype dtype, const dpb_heads* q,
  *   dV = P^T dO,  dQ = scale dS K,  dK = scale dS^T Q
  * dk and dv of a shared key head are the sums over the query heads that read it.
  * Rows that take no part get gradients of 0 (padded).  No atomics: the same
- * inputs give the same bits.  What is not finite spreads as in the forward, and
- * from a row of grad_out to the keys of its tiles.
+ * inputs give the same bits.  What is not finite in a row of k or v spreads in dq as
+ * that of v in the forward; in a row of q, grad_out, out or lse it reaches its row of dq and
+ * dk and dv of the keys that the row sees, and may reach up to 62 keys behind them.
  *   dq like q, dk and dv like k and v (written; their own strides; must not
  *   overlap each other or the inputs) */
 dpb_status dpb_attention_bwd(const dpb_attn* a, dpb_dtype dtype, const dpb_heads* grad_out, const dpb_heads* q,
