@@ -435,7 +435,8 @@ size_t dpb_attention_bwd_workspace_bytes(const dpb_attn* a);
  *   dtype   : of q, k, v and out (DPB_F32 or DPB_BF16)
  *   q, out  : heads heads;  k, v: kv_heads heads (out is written; must not
  *             overlap the inputs)
- *   lse     : device fp32 [rows of q, heads] (padded: [batch, q_len, heads])
+ *   lse     : device fp32 [rows of q, heads] (padded: [batch, q_len, heads]), 16-byte
+ *             aligned
  * Scores, softmax and sums are fp32; with bf16 the probabilities are rounded to
  * bf16 as operands of the product with V.  The forms: tiles of query rows against
  * the keys; for few rows (one new token over a cache) the keys are split and the
@@ -444,11 +445,11 @@ size_t dpb_attention_bwd_workspace_bytes(const dpb_attn* a);
  * the rows that see it; in a row of v it may also reach rows that a causal mask
  * hides it from, up to 95 tokens before the first that sees it (0 times it is no 0).
  * DPB_EINVAL: a bad size, pointer, stride, scale or workspace; DPB_EUNSUPPORTED:
- * head_dim over 128 or not a multiple of 8, a token stride of 16 MiB or more,
- * more than 2^31 - 256 rows or keys of a sequence (rows times the heads that share a key
- * head) or in all packed ones, or a launch of 2^32 threads (256 for 128 query rows
- * or, in the backward, 128 keys of a sequence and key head; for 32 rows and a part of the
- * keys where rows are few). */
+ * head_dim over 128 or not a multiple of 8, a token stride of 16 MiB or more, a
+ * sequence of more than 2^31 - 256 keys or rows (queries times the heads that share a
+ * key head), as many packed rows, or a launch of 2^32 threads: 256 are taken for each
+ * sequence, key head and 128 rows (32 and a part of the keys where rows are few), in
+ * the backward also for each 128 keys. */
 dpb_status dpb_attention(const dpb_attn* a, dpb_dtype dtype, const dpb_heads* q, const dpb_heads* k,
                          const dpb_heads* v, const dpb_heads* out, float* lse, void* workspace, size_t ws_bytes,
                          void* stream);

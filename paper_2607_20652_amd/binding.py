@@ -546,7 +546,8 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = 
     max_q / max_k.  scale defaults to 1 / sqrt(D); causal: query i sees the keys
     j <= i + k_len - q_len.  A query that sees none gets 0 and lse -inf, and so do packed
     rows of no sequence in outputs made here; in an out or lse that is given those
-    rows are left as they are."""
+    rows are left as they are.  Tensors start on 16 bytes and their strides are multiples of 16
+    bytes (0 too, for inputs)."""
     a = _attn(q, k, v, causal, scale, q_lens, k_lens, q_starts, k_starts, max_q, max_k)
     new_out, new_lse, given = out is None, lse is None, (out, lse)
     if out is None:

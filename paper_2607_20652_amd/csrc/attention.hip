@@ -12,9 +12,9 @@
 // two stages of them.  Width 64: bound by vector issue (an exponential is two slots,
 // and a maximum, a product, a sum and half a conversion go with each score; 0.75 of
 // the slots are used), 16 x 1024 tokens, 16 heads: 58 us, 0.59 PFLOP/s of visible
-// products.  Width 128: the matrix cores are busy 57% of the cycles at the 1.6 to 1.9
-// GHz that the power allows then, 16,384 tokens, 16 heads over 4: 1.02 ms, 1.08
-// PFLOP/s (a large matrix product: 1.45).  Computing the next tile's scores under the
+// products (62 us a call whose inputs are in no cache).  Width 128: the matrix cores are busy 57% of the cycles at the 1.6 to 1.9
+// GHz that the power allows then, 16,384 tokens, 16 heads over 4: 1.02 to 1.06 ms, 1.04 to
+// 1.08 PFLOP/s (a large matrix product: 1.45).  Computing the next tile's scores under the
 // softmax, 256 rows with one barrier per 128 keys, three or four stages, wave
 // priorities: no faster, each within 2%.
 //
@@ -383,8 +383,9 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a)
 
 // Rows of a packed call that belong to no sequence: before the first, behind the last, and
 // where a sequence is longer than the longest.  A workgroup takes whole sequences' rows,
-// and all share the rows at the two ends.  Nothing but the starts is read where
-// every row has a sequence: the launch is what it costs.
+// and all share the rows at the two ends.  Bound by memory where there are many (200,000
+// rows of 16 heads of 64: 86 us, 4.9 TB/s written); where every row has a sequence nothing
+// but the starts is read and the launch is what it costs (37 documents: 4 us).
 constexpr int kClearBlocks = 1024;
 
 template <typename F>
@@ -424,7 +425,8 @@ __global__ __launch_bounds__(256) void attention_clear_kernel(AttnArgs a, int ch
     });
 }
 
-// W: waves per SIMD that the registers are to allow.
+// W: waves per SIMD that the registers are to allow, or more (bf16, width 64: 122 registers,
+// four waves where three are asked for).
 template <typename T, int DP, int KT, int W>
 hipError_t launch_tiles(const AttnArgs& a, hipStream_t stream)
 {

@@ -14,7 +14,7 @@
 // -delta, so dS is one product.
 //
 // Measured, with the operations executed: 2 x 8192 tokens, 16 heads of 128 over 4,
-// causal: dQ 0.69 ms (1.19 PFLOP/s), dK and dV 1.01 ms (1.09), their parts' sum 25 us; a
+// causal: dQ 0.69 to 0.72 ms (1.19 PFLOP/s), dK and dV 1.01 to 1.05 ms (1.09), their parts' sum 25 us; a
 // large matrix product reaches 1.45, and the clock falls to 1.6 to 1.9 GHz under
 // either.  16 x 1024 tokens, 16 heads of 64: dQ 85 us, dK and dV 90 us (0.6 and 0.76
 // PFLOP/s), bound by vector issue and reading and writing the tensors (67 MB each way).

@@ -3,7 +3,7 @@
 `AdamW(params).step()` updates all parameters of one type in one call of
 dpb_adamw_step: fp32 or 8-bit states, optional fp32 masters of bf16
 parameters, and decay of matrices only if asked for.  It keeps torch's
-step / zero_grad / state_dict manner.
+step / zero_grad / state_dict manner, but is no torch.optim.Optimizer: a schedule sets .lr.
 """
 from __future__ import annotations
 
