@@ -14,8 +14,9 @@ import torch
 from . import binding as B
 
 
-def _versions(tensors) -> list:
-    return [None if t.is_inference() else t._version for t in tensors]
+def _versions(tensors, master) -> list | None:
+    """The parameters' versions, where masters go by them."""
+    return None if master is None else [None if t.is_inference() else t._version for t in tensors]
 
 
 class AdamW:
@@ -46,7 +47,7 @@ class AdamW:
                 keep = dtype == torch.bfloat16 if master is None else master
                 m, v, scales, weights = B.adamw_state(tensors, bits, keep)
                 self.groups.append(dict(params=tensors, decay=[float(wd) for _, wd in mine], m=m, v=v, scales=scales,
-                                        master=weights, versions=_versions(tensors)))
+                                        master=weights, versions=_versions(tensors, weights)))
         if sum(len(g["params"]) for g in self.groups) != len(pairs):
             raise TypeError("parameters have to be float32 or bfloat16")
 
@@ -64,10 +65,10 @@ class AdamW:
                           g["decay"], grad_scale, self.seed + 2 * steps + i)
                  for i, (g, mine) in enumerate(zip(self.groups, grads))]
         for g, call in zip(self.groups, calls):
-            if g["master"] is not None and _versions(g["params"]) != g["versions"]:
+            if _versions(g["params"], g["master"]) != g["versions"]:
                 self._take(g)
             call()
-            g["versions"] = _versions(g["params"])
+            g["versions"] = _versions(g["params"], g["master"])
         self.steps = steps
 
     def take_parameters(self):
@@ -85,7 +86,7 @@ class AdamW:
             mine, p = g["master"][at:at + n], p.reshape(-1)
             mine.copy_(torch.where(mine.to(p.dtype) == p, mine, p.float()))
             at += -(-n // B.ADAMW_BLOCK) * B.ADAMW_BLOCK
-        g["versions"] = _versions(g["params"])
+        g["versions"] = _versions(g["params"], g["master"])
 
     def zero_grad(self):
         for g in self.groups:
