@@ -526,6 +526,93 @@ dpb_status dpb_adamw_step(const dpb_adamw* settings, int count, void* const* par
                           dpb_dtype grad_dtype, int state_bits, void* m, void* v, float* scales, float* master,
                           const float* grad_scale, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * OPERATORS AROUND THE BLOCKS: from tokens to the first block, between its
+ * sublayers, and from the last block to the loss.  They need no plan and run on the
+ * current device.  dtype is that of all activations, tables and their gradients of a
+ * call (DPB_F32 or DPB_BF16); sums and statistics are fp32.  Everything is
+ * deterministic: no atomics on results.  index_bits: 32 or 64, the width of the
+ * integers in `tokens` and `targets` (device, contiguous, aligned to their width).
+ * Strides are in ELEMENTS between rows, the elements of a row contiguous; dim is any
+ * size from 1 on.  An output may not overlap anything else of its call, unless it says so. */
+
+/* EMBEDDING: out[t] = scale * table[tokens[t]] (out contiguous [count, dim]).  A token outside
+ * [0, vocab) gives a row of zeros.  Rows of the table start on 16 bytes and are that
+ * many apart for full speed; any element-aligned table is read. */
+dpb_status dpb_embedding(dpb_dtype dtype, const void* table, int64_t table_stride, int64_t vocab, int dim,
+                         const void* tokens, int index_bits, int64_t count, float scale, void* out, void* stream);
+
+/* EMBEDDING BACKWARD: grad_table[v] = scale * sum of grad_out[t] over the t with tokens[t] = v,
+ * all of the contiguous [vocab, dim] written (zeros for rows that no token names).
+ * The tokens are sorted by their rows, keeping their order, and each row's
+ * gradients are added up in it.  count < 2^31 and vocab < 2^31 - 2^16. */
+size_t dpb_embedding_bwd_workspace_bytes(int64_t vocab, int dim, int64_t count);
+dpb_status dpb_embedding_bwd(dpb_dtype dtype, const void* grad_out, int64_t grad_stride, const void* tokens, int index_bits,
+                             int64_t count, int64_t vocab, int dim, float scale, void* grad_table, void* workspace,
+                             size_t ws_bytes, void* stream);
+
+/* RMS NORM with the residual's addition, for `rows` rows of dim:
+ *   total = x + residual (rounded to dtype; the sum that the norm, and the next layers, see)
+ *   rstd  = 1 / sqrt(mean(total^2) + eps),   out = total * rstd * weight
+ *   residual : or NULL: total is x, and the argument total is ignored
+ *   weight   : [dim] of weight_dtype, or NULL for ones
+ *   out, total : contiguous [rows, dim]; either may be the very tensor of an input (x or
+ *              residual, if that is contiguous), and total may not be out
+ *   rstd     : device fp32 [rows], or NULL where no gradient is wanted
+ * eps >= 0.  A row that is all zeros with eps = 0 gives NaN. */
+dpb_status dpb_rms_norm(dpb_dtype dtype, const void* x, int64_t x_stride, const void* residual, int64_t residual_stride,
+                        const void* weight, dpb_dtype weight_dtype, int64_t rows, int dim, float eps, void* out, void* total,
+                        float* rstd, void* stream);
+
+/* RMS NORM BACKWARD for the gradient grad_out of out, and grad_total of total (NULL for none):
+ *   u = grad_out * weight,  n = total * rstd
+ *   grad_x = rstd (u - n mean(u n)) + grad_total  (the gradient of x and of residual alike)
+ *   grad_weight = sum over rows of grad_out * n
+ *   grad_x      : contiguous [rows, dim], or NULL; may be the very tensor of grad_out or
+ *                 grad_total, if that is contiguous
+ *   grad_weight : [dim] of weight_dtype, or NULL (then no workspace is needed) */
+size_t dpb_rms_norm_bwd_workspace_bytes(int64_t rows, int dim);
+dpb_status dpb_rms_norm_bwd(dpb_dtype dtype, const void* grad_out, int64_t grad_stride, const void* grad_total,
+                            int64_t grad_total_stride, const void* total, int64_t total_stride, const void* weight,
+                            dpb_dtype weight_dtype, const float* rstd, int64_t rows, int dim, void* grad_x,
+                            void* grad_weight, void* workspace, size_t ws_bytes, void* stream);
+
+/* Hidden rows and the vocabulary's matrix whose products are the logits
+ *   logits = scale * hidden [rows, dim] * weight [vocab, dim]^T,   scale > 0.
+ * Both start on 16 bytes; strides of their rows are any (under 8 MiB): rows that do not
+ * start on 16 bytes are copied into the workspace first. */
+typedef struct {
+    const void *hidden, *weight;
+    int64_t hidden_stride, weight_stride;
+    int64_t rows, vocab;
+    int dim;
+    float scale;
+} dpb_logits;
+
+/* CROSS ENTROPY, the logits never in memory:
+ *   lse[t]  = log sum_v exp logits[t, v]
+ *   loss[t] = lse[t] - logits[t, targets[t]],  0 for a target outside [0, vocab)
+ * loss, lse: device fp32 [rows].  A row whose logits are not all finite gets values that are
+ * not; it does not reach other rows' results.  The workspace sizes go by sizes and strides
+ * alone (0 for a description that the call refuses). */
+size_t dpb_cross_entropy_workspace_bytes(const dpb_logits* a, dpb_dtype dtype);
+dpb_status dpb_cross_entropy(const dpb_logits* a, dpb_dtype dtype, const void* targets, int index_bits, float* loss,
+                             float* lse, void* workspace, size_t ws_bytes, void* stream);
+
+/* CROSS ENTROPY BACKWARD for the gradients grad_loss and grad_lse (device fp32 [rows], NULL for
+ * zeros; grad_lse is that of a penalty on lse, say) from the forward's lse:
+ *   D = softmax(logits) (a + grad_lse) - a onehot(targets),   a = grad_loss where the target counts, else 0
+ *   grad_hidden = scale D weight,   grad_weight = scale D^T hidden
+ * grad_hidden [rows, dim], grad_weight [vocab, dim]: contiguous, 16-byte aligned, either may
+ * be NULL.  The logits are computed once more, over pieces of the vocabulary such that a piece's
+ * D takes 1 GiB of the workspace or less (or 1,024 entries).  With bf16 D is rounded to bf16 as
+ * operand of the products.  What is not finite in a row of hidden reaches all of
+ * grad_weight, in one of weight all of grad_hidden (0 times it is no 0). */
+size_t dpb_cross_entropy_bwd_workspace_bytes(const dpb_logits* a, dpb_dtype dtype);
+dpb_status dpb_cross_entropy_bwd(const dpb_logits* a, dpb_dtype dtype, const void* targets, int index_bits,
+                                 const float* grad_loss, const float* grad_lse, const float* lse, void* grad_hidden,
+                                 void* grad_weight, void* workspace, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -73,6 +73,16 @@ def load():
         "dpb_attention": (i32, [P, i32] + [P] * 6 + [ctypes.c_size_t, P]),
         "dpb_attention_bwd": (i32, [P, i32] + [P] * 10 + [ctypes.c_size_t, P]),
         "dpb_attention_clear": (i32, [P, i32] + [P] * 5),
+        "dpb_embedding": (i32, [i32, P, i64, i64, i32, P, i32, i64, ctypes.c_float, P, P]),
+        "dpb_embedding_bwd_workspace_bytes": (ctypes.c_size_t, [i64, i32, i64]),
+        "dpb_embedding_bwd": (i32, [i32, P, i64, P, i32, i64, i64, i32, ctypes.c_float, P, P, ctypes.c_size_t, P]),
+        "dpb_rms_norm": (i32, [i32, P, i64, P, i64, P, i32, i64, i32, ctypes.c_float, P, P, P, P]),
+        "dpb_rms_norm_bwd_workspace_bytes": (ctypes.c_size_t, [i64, i32]),
+        "dpb_rms_norm_bwd": (i32, [i32, P, i64, P, i64, P, i64, P, i32, P, i64, i32, P, P, P, ctypes.c_size_t, P]),
+        "dpb_cross_entropy_workspace_bytes": (ctypes.c_size_t, [P, i32]),
+        "dpb_cross_entropy": (i32, [P, i32, P, i32, P, P, P, ctypes.c_size_t, P]),
+        "dpb_cross_entropy_bwd_workspace_bytes": (ctypes.c_size_t, [P, i32]),
+        "dpb_cross_entropy_bwd": (i32, [P, i32, P, i32] + [P] * 6 + [ctypes.c_size_t, P]),
         "dpb_adamw_blocks": (i64, [P, i32]),
         "dpb_adamw_step": (i32, [P, i32, P, P, P, P, i32, i32, i32, P, P, P, P, P, P]),
     }
@@ -700,3 +710,257 @@ def _adamw(params, grads, m, v, scales, master, step, lr, betas, eps, weight_dec
         _written([*params, m, v, scales, master])
 
     return call
+
+
+# ---- operators around the blocks: embedding, norm, loss over the vocabulary
+
+_LOGITS = struct.Struct("=QQqqqqif")
+
+
+def _place(t: torch.Tensor | None, name: str, device: int) -> int | None:
+    """Address of a tensor on this device, contiguous or not."""
+    if t is None:
+        return None
+    if t.get_device() != device:
+        _elsewhere(t, name, device)
+    return t.data_ptr()
+
+
+def _whole(t: torch.Tensor | None, name: str, device: int) -> int | None:
+    return None if t is None else _dev(t, name, device).value
+
+
+def _rows(t: torch.Tensor, name: str):
+    """(rows, stride between them) of [..., dim] as rows of dim elements, contiguous each."""
+    shape, st = t.shape, t.stride()
+    if len(shape) == 0:
+        raise ValueError(f"{name} has no rows")
+    if shape[-1] > 1 and st[-1] != 1:
+        raise ValueError(f"{name} must be contiguous along its last dimension")
+    if t.is_contiguous():
+        return t.numel() // shape[-1] if shape[-1] else 0, shape[-1]
+    # the other dimensions have to be one, in the order of memory
+    n, stride = 1, shape[-1]
+    for size, step in zip(reversed(shape[:-1]), reversed(st[:-1])):
+        if size == 1:
+            continue
+        if n == 1:
+            stride = step
+        elif step != n * stride:
+            raise ValueError(f"{name}: its rows must be evenly apart")
+        n *= size
+    return n, stride
+
+
+def _integers(t: torch.Tensor, name: str, device: int):
+    """(address, bits) of a contiguous tensor of tokens."""
+    if t.dtype not in (torch.int64, torch.int32):
+        raise TypeError(f"{name}: int64 or int32, not {t.dtype}")
+    return _dev(t, name, device).value, 64 if t.dtype == torch.int64 else 32
+
+
+def _space(workspace: torch.Tensor | None, need: int, like: torch.Tensor):
+    """A workspace of at least `need` bytes (the caller's, if given) and its size."""
+    if workspace is None:
+        if not need:
+            return None, 0
+        workspace = torch.empty((need + 15) // 16 * 4, dtype=torch.float32, device=like.device)
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def embedding(tokens: torch.Tensor, table: torch.Tensor, scale: float = 1.0, out: torch.Tensor | None = None):
+    """scale * table[tokens] -> [*tokens.shape, dim] of the table's type; table [vocab, dim]
+    with any stride of its rows.  A token outside [0, vocab) gives a row of zeros."""
+    _need(table.dim() == 2)
+    vocab, dim = table.shape
+    if out is None:
+        out = table.new_empty((*tokens.shape, dim))
+        given = None
+    else:
+        _need(out.shape == (*tokens.shape, dim) and out.dtype == table.dtype)
+        given = out
+    _need(dim >= 1, "a table of no columns")
+    device, here = _device_of(table, "table")
+    with here:
+        at, bits = _integers(tokens, "tokens", device)
+        _, stride = _rows(table, "table")
+        _check("dpb_embedding", load().dpb_embedding(
+            _dtype_code(table), table.data_ptr(), stride, vocab, dim, at, bits, tokens.numel(), scale,
+            _whole(out, "out", device), _stream(table)))
+    if given is not None:
+        _written([given])
+    return out
+
+
+def embedding_bwd(grad_out: torch.Tensor, tokens: torch.Tensor, vocab: int, scale: float = 1.0,
+                  dweight: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """Gradient [vocab, dim] of the table for grad_out [*tokens.shape, dim] of embedding:
+    scale times the sum of each row's tokens' gradients, added up in their order."""
+    _need(grad_out.dim() >= 1 and grad_out.shape[:-1] == tokens.shape and grad_out.shape[-1] >= 1)
+    dim, vocab, given = grad_out.shape[-1], int(vocab), dweight
+    _need(vocab >= 0)
+    if dweight is None:
+        dweight = grad_out.new_empty((vocab, dim))
+    _need(dweight.shape == (vocab, dim) and dweight.dtype == grad_out.dtype)
+    lib = load()
+    device, here = _device_of(grad_out, "grad_out")
+    with here:
+        at, bits = _integers(tokens, "tokens", device)
+        n, stride = _rows(grad_out, "grad_out")
+        workspace, size = _space(workspace, lib.dpb_embedding_bwd_workspace_bytes(vocab, dim, n), grad_out)
+        _check("dpb_embedding_bwd", lib.dpb_embedding_bwd(
+            _dtype_code(grad_out), grad_out.data_ptr(), stride, at, bits, n, vocab, dim, scale,
+            _whole(dweight, "dweight", device), _whole(workspace, "workspace", device), size, _stream(grad_out)))
+    if given is not None:
+        _written([given])
+    return dweight
+
+
+def rms_norm(x: torch.Tensor, weight: torch.Tensor | None, residual: torch.Tensor | None = None, eps: float = 1e-6,
+             out: torch.Tensor | None = None, total: torch.Tensor | None = None, rstd: torch.Tensor | None = None):
+    """(out, total, rstd): total = x + residual in their type (x itself without a residual),
+    rstd = (mean(total^2) + eps)^-1/2 over the last dimension (fp32), out = total rstd weight.
+
+    x, residual: [..., dim], rows evenly apart; weight [dim], fp32 or bf16, or None.  out and
+    total may be x or residual themselves, if those are contiguous."""
+    shape = x.shape
+    _need(len(shape) >= 1 and shape[-1] >= 1)
+    dim = shape[-1]
+    _need(residual is None or (residual.shape == shape and residual.dtype == x.dtype))
+    _need(weight is None or weight.shape == (dim,))
+    _need(residual is not None or total is None, "without a residual the sum is x")
+    given = [out, total, rstd]
+    if out is None:
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+    if residual is not None and total is None:
+        total = torch.empty_like(x, memory_format=torch.contiguous_format)
+    if rstd is None:
+        rstd = x.new_empty(shape[:-1], dtype=torch.float32)
+    _need(out.shape == shape and out.dtype == x.dtype and rstd.shape == shape[:-1] and rstd.dtype == torch.float32)
+    _need(total is None or (total.shape == shape and total.dtype == x.dtype))
+    device, here = _device_of(x, "x")
+    with here:
+        n, stride = _rows(x, "x")
+        r_stride = 0 if residual is None else _rows(residual, "residual")[1]
+        _check("dpb_rms_norm", load().dpb_rms_norm(
+            _dtype_code(x), x.data_ptr(), stride, _place(residual, "residual", device), r_stride,
+            _whole(weight, "weight", device), DPB_F32 if weight is None else _dtype_code(weight), n, dim, eps,
+            _whole(out, "out", device), _whole(total, "total", device), _whole(rstd, "rstd", device), _stream(x)))
+    if any(t is not None for t in given):
+        _written(given)
+    return out, x if residual is None else total, rstd
+
+
+def rms_norm_bwd(grad_out: torch.Tensor, total: torch.Tensor, weight: torch.Tensor | None, rstd: torch.Tensor,
+                 grad_total: torch.Tensor | None = None, dx: torch.Tensor | None = None,
+                 dweight: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """Gradients (dx, dweight) of rms_norm for grad_out of out and grad_total of total, from its
+    total and rstd: dx is the gradient of x and of residual alike; dweight in the weight's type
+    (None without one).  dx may be grad_out or grad_total itself, if that is contiguous."""
+    shape = total.shape
+    _need(len(shape) >= 1 and shape[-1] >= 1)
+    dim = shape[-1]
+    _need(grad_out.shape == shape and grad_out.dtype == total.dtype)
+    _need(grad_total is None or (grad_total.shape == shape and grad_total.dtype == total.dtype))
+    _need(rstd.shape == shape[:-1] and rstd.dtype == torch.float32)
+    _need(weight is None or weight.shape == (dim,))
+    _need(weight is not None or dweight is None)
+    given = [dx, dweight]
+    if dx is None:
+        dx = torch.empty_like(total, memory_format=torch.contiguous_format)
+    if weight is not None and dweight is None:
+        dweight = torch.empty_like(weight)
+    _need(dx.shape == shape and dx.dtype == total.dtype)
+    _need(dweight is None or (dweight.shape == (dim,) and dweight.dtype == weight.dtype))
+    lib = load()
+    device, here = _device_of(total, "total")
+    with here:
+        n, stride = _rows(total, "total")
+        g_stride = _rows(grad_out, "grad_out")[1]
+        t_stride = 0 if grad_total is None else _rows(grad_total, "grad_total")[1]
+        need = 0 if dweight is None else lib.dpb_rms_norm_bwd_workspace_bytes(n, dim)
+        workspace, size = _space(workspace, need, total)
+        _check("dpb_rms_norm_bwd", lib.dpb_rms_norm_bwd(
+            _dtype_code(total), _place(grad_out, "grad_out", device), g_stride, _place(grad_total, "grad_total", device),
+            t_stride, total.data_ptr(), stride, _whole(weight, "weight", device),
+            DPB_F32 if weight is None else _dtype_code(weight), _whole(rstd, "rstd", device), n, dim,
+            _whole(dx, "dx", device), _whole(dweight, "dweight", device), _whole(workspace, "workspace", device), size,
+            _stream(total)))
+    if any(t is not None for t in given):
+        _written(given)
+    return dx, dweight
+
+
+def _logits(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, scale: float) -> tuple[bytes, int]:
+    """The description of a call's logits, and its rows."""
+    _need(hidden.dim() >= 1 and weight.dim() == 2 and hidden.shape[-1] == weight.shape[1] >= 1)
+    _need(hidden.dtype == weight.dtype and targets.shape == hidden.shape[:-1])
+    n, stride = _rows(hidden, "hidden")
+    w_stride = _rows(weight, "weight")[1]
+    return _LOGITS.pack(hidden.data_ptr(), weight.data_ptr(), stride, w_stride, n, weight.shape[0], weight.shape[1], scale), n
+
+
+def cross_entropy(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, scale: float = 1.0,
+                  loss: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                  workspace: torch.Tensor | None = None):
+    """(loss, lse), fp32 of the targets' shape: lse = log sum_v exp(scale <hidden, weight_v>),
+    loss = lse - scale <hidden, weight_target>, 0 for a target outside [0, vocab).
+
+    hidden [..., dim] and weight [vocab, dim] of one type, rows evenly apart; the logits are never in memory."""
+    a, n = _logits(hidden, weight, targets, scale)
+    given = [loss, lse]
+    if loss is None:
+        loss = hidden.new_empty(targets.shape, dtype=torch.float32)
+    if lse is None:
+        lse = hidden.new_empty(targets.shape, dtype=torch.float32)
+    _need(loss.shape == lse.shape == targets.shape and loss.dtype == lse.dtype == torch.float32)
+    lib, dtype = load(), _dtype_code(hidden)
+    device, here = _device_of(hidden, "hidden")
+    with here:
+        _place(weight, "weight", device)
+        at, bits = _integers(targets, "targets", device)
+        workspace, size = _space(workspace, lib.dpb_cross_entropy_workspace_bytes(a, dtype), hidden)
+        _check("dpb_cross_entropy", lib.dpb_cross_entropy(
+            a, dtype, at, bits, _whole(loss, "loss", device), _whole(lse, "lse", device),
+            _whole(workspace, "workspace", device), size, _stream(hidden)))
+    if any(t is not None for t in given):
+        _written(given)
+    return loss, lse
+
+
+def cross_entropy_bwd(grad_loss: torch.Tensor | None, hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor,
+                      lse: torch.Tensor, scale: float = 1.0, grad_lse: torch.Tensor | None = None,
+                      dhidden: torch.Tensor | None = None, dweight: torch.Tensor | None = None,
+                      workspace: torch.Tensor | None = None, hidden_grad: bool = True, weight_grad: bool = True):
+    """Gradients (dhidden, dweight) of cross_entropy for grad_loss and grad_lse (fp32 of the
+    targets' shape, or None for zeros) from the forward's lse.  hidden_grad, weight_grad: which of
+    the two are wanted (None in the place of the other)."""
+    a, n = _logits(hidden, weight, targets, scale)
+    _need(lse.shape == targets.shape and lse.dtype == torch.float32)
+    for g in (grad_loss, grad_lse):
+        _need(g is None or (g.shape == targets.shape and g.dtype == torch.float32))
+    given = [dhidden, dweight]
+    if hidden_grad and dhidden is None:
+        dhidden = torch.empty_like(hidden, memory_format=torch.contiguous_format)
+    if weight_grad and dweight is None:
+        dweight = torch.empty_like(weight, memory_format=torch.contiguous_format)
+    _need((dhidden is None) != bool(hidden_grad) and (dweight is None) != bool(weight_grad))
+    _need(dhidden is None or (dhidden.shape == hidden.shape and dhidden.dtype == hidden.dtype))
+    _need(dweight is None or (dweight.shape == weight.shape and dweight.dtype == weight.dtype))
+    lib, dtype = load(), _dtype_code(hidden)
+    device, here = _device_of(hidden, "hidden")
+    with here:
+        _place(weight, "weight", device)
+        at, bits = _integers(targets, "targets", device)
+        outs = _whole(dhidden, "dhidden", device), _whole(dweight, "dweight", device)
+        if n == 0:
+            if dweight is not None:
+                dweight.zero_()
+        else:
+            workspace, size = _space(workspace, lib.dpb_cross_entropy_bwd_workspace_bytes(a, dtype), hidden)
+            _check("dpb_cross_entropy_bwd", lib.dpb_cross_entropy_bwd(
+                a, dtype, at, bits, _whole(grad_loss, "grad_loss", device), _whole(grad_lse, "grad_lse", device),
+                _whole(lse, "lse", device), *outs, _whole(workspace, "workspace", device), size, _stream(hidden)))
+    if any(t is not None for t in given):
+        _written(given)
+    return dhidden, dweight

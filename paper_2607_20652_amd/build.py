@@ -16,18 +16,20 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdpb.so")
 OBJ_DIR = os.path.join(os.path.dirname(HERE), "_build")
-SOURCES = ["api.cpp", "api_training.cpp", "tables.cpp", "adamw.hip", "attention.hip", "attention_bwd.hip",
-           "encode_general.hip", "codes.hip", "columns.hip", "columns_bwd.hip", "encode.hip", "extras.hip",
-           "standardize.hip"]
+SOURCES = ["api.cpp", "api_around.cpp", "api_training.cpp", "tables.cpp", "adamw.hip", "attention.hip",
+           "attention_bwd.hip", "cross_entropy.hip", "encode_general.hip", "embedding.hip", "codes.hip", "columns.hip",
+           "columns_bwd.hip", "encode.hip", "extras.hip", "rms_norm.hip", "standardize.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # keep the compiler from forming packed fp32 instructions
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-    # matrix-core results in ordinary VGPRs (no accumulator-register copies)
-    "-mllvm", "-amdgpu-mfma-vgpr-form",
     "-Wall", "-Wno-unused-result",
 ]
+# matrix-core results in ordinary VGPRs (no accumulator-register copies); not where they fill all 256
+# accumulator registers and leave the ordinary ones to the operands
+VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
+ACCUMULATORS = {"cross_entropy.hip"}
 _NOISE = ("is not a recognized feature for this target", "argument unused during compilation")
 
 
@@ -41,7 +43,8 @@ def build(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     os.makedirs(OBJ_DIR, exist_ok=True)
     objs = [os.path.join(OBJ_DIR, os.path.splitext(s)[0] + ".o") for s in SOURCES]
-    cmds = [[hipcc, *HIPCC_FLAGS, "-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(SOURCES, objs)]
+    cmds = [[hipcc, *HIPCC_FLAGS, *([] if s in ACCUMULATORS else VGPR_FORM), "-c", os.path.join(CSRC, s), "-o", o]
+            for s, o in zip(SOURCES, objs)]
     jobs = max(1, min(len(cmds), int(os.environ.get("MAX_JOBS", os.cpu_count() or 1))))
     with ThreadPoolExecutor(jobs) as ex:
         results = list(ex.map(_run, cmds))

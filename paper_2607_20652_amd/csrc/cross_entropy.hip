@@ -1,0 +1,550 @@
+// Softmax cross entropy of hidden rows over a vocabulary's matrix, and its gradients:
+//     l = scale H W^T,   lse_t = log sum_v exp l_tv,   loss_t = lse_t - l_t,target
+//     D = exp(l - lse) (a + e) - a onehot(target)      (a, e: gradients of loss and lse)
+//     dH = scale D W,   dW = scale D^T H.
+//
+// The logits stay on the chip: a tile of them (vocabulary entries as rows, a token a lane)
+// leaves its maximum and its sum of exponentials per token, which a second kernel
+// joins.  The backward takes the vocabulary in pieces: it computes a piece's logits once
+// more, leaves its D in the operands' type, and D is an operand of two products.
+#include <algorithm>
+#include <cmath>
+
+#include "cross_entropy.hpp"
+#include "product.hpp"
+
+namespace dpb {
+namespace {
+
+// Workgroup `id` of `mt` x `nt` tiles.  Ids go round the eight XCDs in turn: each gets
+// one stretch of an order in which 32 neighbours, what its compute units run together, are a
+// block of 4 x 8 tiles that share their panels in its L2.
+__device__ __forceinline__ void tile_of(unsigned id, unsigned mt, unsigned nt, int& m, int& n)
+{
+    const unsigned total = mt * nt, each = total / 8, rest = total % 8, xcd = id % 8;
+    const unsigned at = xcd * each + min(xcd, rest) + id / 8;
+    const unsigned band = at / (mt * 8), first = band * 8, width = min(8u, nt - first), in = at - band * mt * 8;
+    m = (int)(in / width);
+    n = (int)(first + in % width);
+}
+
+__device__ __forceinline__ int64_t target_of(const LossArgs& a, int64_t row)
+{
+    if (row >= a.rows) return -1;
+    const int64_t t = a.wide_targets ? ((const int64_t*)a.targets)[row] : ((const int32_t*)a.targets)[row];
+    return t >= 0 && t < a.vocab ? t : -1;
+}
+
+// Row `from` of the wave's N as an index into what its lane half holds of them (-1: not among
+// those): rows 8 g + 4 h + {0..3} are those of half h, counted here without the 4 h.
+template <int N>
+__device__ __forceinline__ int place_in(int64_t from)
+{
+    const int h = (threadIdx.x & 63) >> 5, at = (int)from;
+    return from >= 0 && from < N && (at >> 2 & 1) == h ? at - 4 * h : -1;
+}
+
+// Keeps the compiler from forming all comparisons with v before it uses the first.
+__device__ __forceinline__ int one_by_one(int& v)
+{
+    __asm__ volatile("" : "+v"(v));
+    return v;
+}
+
+template <int FM, int FN>
+__device__ __forceinline__ void clear(f32x16 (&c)[FM][FN])
+{
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) c[i][j][r] = 0.f;
+}
+
+// Column j of a wave's fragments in ordinary registers (the products' results are not: only
+// one column of them at a time is brought over).
+template <int FM, int FN>
+__device__ __forceinline__ void take_out(const f32x16 (&c)[FM][FN], int j, f32x16 (&v)[FM])
+{
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+        v[i] = c[i][j];
+        __asm__ volatile("" : "+v"(v[i]));
+    }
+}
+
+// What a tile leaves of its token: sum_v 2^(l_v log2(e) - base), where base is the largest of those
+// exponents, rounded.  (It is subtracted in the fma that forms the exponent, so base + log2(sum) holds
+// no error of its rounding.)
+struct Part {
+    float base, sum;
+};
+
+__device__ __forceinline__ void join(Part& x, const Part& y)
+{
+    const float base = fmaxf(x.base, y.base), from = base == -INFINITY ? 0.f : base;
+    x.sum = x.sum * __builtin_amdgcn_exp2f(x.base - from) + y.sum * __builtin_amdgcn_exp2f(y.base - from);
+    x.base = base;
+}
+
+template <typename T, int BM, int BN>
+__global__ __launch_bounds__(256, 1) void loss_part_kernel(LossArgs a, int mt, int nt, Part* parts, float* own)
+{
+    typedef Product<T, false, false, BM, BN> P;
+    constexpr int FM = P::FM, FN = P::FN;
+    int mi, ni;
+    tile_of(blockIdx.x, mt, nt, mi, ni);
+    const int64_t m0 = (int64_t)mi * BM, n0 = (int64_t)ni * BN;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
+    const int h = lane >> 5;
+
+    f32x16 c[FM][FN];
+    clear(c);
+    P::run(Side{(const char*)a.weight, a.weight_stride, a.vocab}, Side{(const char*)a.hidden, a.hidden_stride, a.rows}, m0, n0,
+           0, a.dim, c);
+
+    const float cs = a.scale * kLog2e;
+    const int64_t v0 = m0 + wm * (BM / 2);   // the wave's first vocabulary entry
+    const int left = (int)min(max(a.vocab - v0, (int64_t)0), (int64_t)BM);   // entries from there on
+    Part* const lds = (Part*)stage_lds<P::kStage, 0>();   // [2][BN]
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        const int col = wn * (BN / 2) + 32 * j + (lane & 31);
+        f32x16 v[FM];
+        take_out(c, j, v);
+        int at = place_in<BM / 2>(target_of(a, n0 + col) - v0);
+        if (__any(at >= 0)) {
+            float l = 0.f;
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) l = one_by_one(at) == 32 * i + 8 * (r >> 2) + (r & 3) ? v[i][r] : l;
+            if (at >= 0) own[n0 + col] = l;
+        }
+        if (left < BM / 2) {
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) v[i][r] = 32 * i + 8 * (r >> 2) + (r & 3) + 4 * h < left ? apart(v[i][r]) : -INFINITY;
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, v[i][r]);
+        top = fmaxf(top, other_half(top));
+        const float base = top == -INFINITY ? 0.f : top * cs;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(fmaf(v[i][r], cs, -base));
+        sum += other_half(sum);
+        if (h == 0) lds[wm * BN + col] = Part{top == -INFINITY ? top : base, sum};
+    }
+    __syncthreads();
+    for (int col = threadIdx.x; col < BN; col += 256) {
+        if (n0 + col >= a.rows) break;
+        Part x = lds[col];
+        join(x, lds[BN + col]);
+        parts[(int64_t)mi * a.rows + n0 + col] = x;
+    }
+}
+
+// Joins the parts of 16 tokens, 64 threads each of a share of the parts.
+__global__ __launch_bounds__(1024) void loss_join_kernel(LossArgs a, int mt, const Part* parts, const float* own)
+{
+    __shared__ Part lds[64][17];
+    const int col = threadIdx.x & 15, share = threadIdx.x >> 4;
+    const int64_t row = (int64_t)blockIdx.x * 16 + col;
+    Part p{-INFINITY, 0.f};
+    if (row < a.rows) {
+#pragma unroll 4
+        for (int i = share; i < mt; i += 64) join(p, parts[(int64_t)i * a.rows + row]);
+    }
+    lds[share][col] = p;
+    __syncthreads();
+    if (share >= 4) return;
+    for (int i = share + 4; i < 64; i += 4) join(p, lds[i][col]);
+    // the four are lanes of one wave
+    wave_sync();
+    lds[share][col] = p;
+    wave_sync();
+    if (share || row >= a.rows) return;
+    for (int i = 1; i < 4; ++i) join(p, lds[i][col]);
+    const float rest = logf(p.sum);
+    a.lse[row] = fmaf(p.base, kLn2, rest);
+    // (the rounding of 1 + what is left of a sure target's sum may fall below 0; NaN stays)
+    const float loss = fmaf(fmaf(-own[row], a.scale * kLog2e, p.base), kLn2, rest);
+    a.loss[row] = target_of(a, row) < 0 || loss < 0.f ? 0.f : loss;
+}
+
+// D of vocabulary entries [first, first + width): `out` has rows of out_stride bytes.
+template <typename T, int BM, int BN>
+__global__ __launch_bounds__(256, 1) void loss_grad_kernel(LossArgs a, int mt, int nt, int64_t first, int64_t width, char* out,
+                                                           int64_t out_stride)
+{
+    typedef Product<T, false, false, BM, BN> P;
+    constexpr int FM = P::FM, FN = P::FN;
+    int mi, ni;
+    tile_of(blockIdx.x, mt, nt, mi, ni);
+    const int64_t m0 = (int64_t)mi * BM, n0 = (int64_t)ni * BN;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
+    const int h = lane >> 5;
+
+    f32x16 c[FM][FN];
+    clear(c);
+    P::run(Side{(const char*)a.weight + first * a.weight_stride, a.weight_stride, width},
+           Side{(const char*)a.hidden, a.hidden_stride, a.rows}, m0, n0, 0, a.dim, c);
+
+    const float cs = a.scale * kLog2e;
+    const int64_t v0 = m0 + wm * (BM / 2);
+    const int left = (int)min(max(width - v0, (int64_t)0), (int64_t)BM);   // entries of the piece
+    char* const lds = stage_lds<P::kStage, 0>() + wave * (P::kStage / kWaves);
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        f32x16 v[FM];
+        take_out(c, j, v);
+        const int64_t row = n0 + wn * (BN / 2) + 32 * j + (lane & 31);
+        const int64_t target = target_of(a, row);
+        float ga = 0.f, ge = 0.f, lse2 = 0.f;
+        if (row < a.rows) {
+            if (a.grad_loss && target >= 0) ga = a.grad_loss[row];
+            if (a.grad_lse) ge = a.grad_lse[row];
+            lse2 = a.lse[row] * kLog2e;
+        }
+        const bool live = ga != 0.f || ge != 0.f;
+        const float both = ga + ge;
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(v[i][r], cs, -lse2)) * both;
+                v[i][r] = live ? p : 0.f;
+            }
+        int at = place_in<BM / 2>(target - first - v0);
+        if (__any(at >= 0)) {
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) v[i][r] -= one_by_one(at) == 32 * i + 8 * (r >> 2) + (r & 3) ? ga : 0.f;
+        }
+        if (left < BM / 2) {
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) v[i][r] = 32 * i + 8 * (r >> 2) + (r & 3) + 4 * h < left ? apart(v[i][r]) : 0.f;
+        }
+        // 32 tokens of BM / 2 entries, through LDS into whole lines
+        constexpr int kRow = BM / 2 * (int)sizeof(T), kChunks = kRow / 16;
+        static_assert(32 * kRow <= P::kStage / kWaves, "a wave's share of a stage holds 32 rows");
+        wave_sync();
+        const int r32 = lane & 31;
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int byte = (32 * i + 8 * g + 4 * h) * (int)sizeof(T), chunk = byte >> 4;
+                char* to = lds + r32 * kRow + (((chunk & ~3) | ((chunk ^ r32) & 3)) << 4) + (byte & 15);
+                store4<T>(to, 0, v[i][4 * g], v[i][4 * g + 1], v[i][4 * g + 2], v[i][4 * g + 3]);
+            }
+        wave_sync();
+        const int bytes = (left * (int)sizeof(T) + 15) / 16 * 16;
+#pragma unroll
+        for (int k = 0; k < kChunks / 2; ++k) {
+            const int r = k * (64 / kChunks) + lane / kChunks, chunk = lane % kChunks;
+            const int64_t t = n0 + wn * (BN / 2) + 32 * j + r;
+            if (t < a.rows && chunk * 16 < bytes)
+                *(u32x4*)(out + t * out_stride + v0 * (int)sizeof(T) + chunk * 16) =
+                    *(const u32x4*)(lds + r * kRow + (((chunk & ~3) | ((chunk ^ r) & 3)) << 4));
+        }
+    }
+}
+
+struct OutArgs {
+    Side a, b;          // the result's contiguous index (transposed), and its rows
+    int64_t k;          // contraction
+    int parts;
+    float* part;        // [parts][rows][dim] fp32, or null: the result itself
+    int add;            // to what the parts hold
+    void* out;
+    int64_t dim;        // of a result's row
+    float scale;
+};
+
+// out[n][m] = scale sum_k a[k][m] b[n][k] (b plain) or b[k][n] (transposed).
+template <typename T, bool TB, int BM, int BN>
+__global__ __launch_bounds__(256, 1) void loss_out_kernel(OutArgs o, int mt, int nt)
+{
+    typedef Product<T, true, TB, BM, BN> P;
+    constexpr int FM = P::FM, FN = P::FN;
+    int mi, ni;
+    const unsigned tiles = (unsigned)mt * nt, part = blockIdx.x / tiles;
+    tile_of(blockIdx.x % tiles, mt, nt, mi, ni);
+    const int64_t m0 = (int64_t)mi * BM, n0 = (int64_t)ni * BN;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
+    const int h = lane >> 5;
+    const int64_t steps = (o.k + P::kK - 1) / P::kK;
+    const int64_t begin = steps * part / o.parts * P::kK, end = min(steps * (part + 1) / o.parts * P::kK, o.k);
+
+    f32x16 c[FM][FN];
+    clear(c);
+    P::run(o.a, o.b, m0, n0, begin, end, c);
+
+    char* const lds = stage_lds<P::kStage, 0>() + wave * (P::kStage / kWaves);
+    constexpr int kRow = BM / 2 * 4, kChunks = kRow / 16;
+    static_assert(32 * kRow <= P::kStage / kWaves, "a wave's share of a stage holds 32 rows");
+    const bool whole = o.dim % 4 == 0;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        f32x16 v[FM];
+        take_out(c, j, v);
+        wave_sync();
+        const int r32 = lane & 31;
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int chunk = 8 * i + 2 * g + h;
+                *(f32x4*)(lds + r32 * kRow + ((chunk ^ (r32 & 7)) << 4)) =
+                    (f32x4){v[i][4 * g], v[i][4 * g + 1], v[i][4 * g + 2], v[i][4 * g + 3]};
+            }
+        wave_sync();
+#pragma unroll 4
+        for (int k = 0; k < kChunks / 2; ++k) {
+            const int r = k * (64 / kChunks) + lane / kChunks, chunk = lane % kChunks;
+            const int64_t n = n0 + wn * (BN / 2) + 32 * j + r, m = m0 + wm * (BM / 2) + chunk * 4;
+            if (n >= o.b.rows || m >= o.dim) continue;
+            f32x4 w = *(const f32x4*)(lds + r * kRow + ((chunk ^ (r & 7)) << 4));
+            if (o.part) {
+                float* to = o.part + (part * o.b.rows + n) * o.dim + m;
+                if (whole) {
+                    if (o.add) w += *(const f32x4*)to;
+                    *(f32x4*)to = w;
+                } else {
+                    for (int e = 0; e < 4 && m + e < o.dim; ++e) to[e] = o.add ? to[e] + w[e] : w[e];
+                }
+            } else if (whole) {
+                store4<T>((char*)o.out + (n * o.dim + m) * (int)sizeof(T), 0, w[0] * o.scale, w[1] * o.scale, w[2] * o.scale, w[3] * o.scale);
+            } else {
+                for (int e = 0; e < 4 && m + e < o.dim; ++e) store_act<sizeof(T) == 2>(o.out, n * o.dim + m + e, w[e] * o.scale);
+            }
+        }
+    }
+}
+
+// The parts' sum in their order, times scale: four values a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void loss_sum_kernel(const float* part, int parts, int64_t n, float scale, void* out)
+{
+    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (at >= n) return;
+    if (n % 4 == 0) {
+        f32x4 v = *(const f32x4*)(part + at);
+        for (int p = 1; p < parts; ++p) v += *(const f32x4*)(part + p * n + at);
+        store4<T>((char*)out + at * (int)sizeof(T), 0, v[0] * scale, v[1] * scale, v[2] * scale, v[3] * scale);
+    } else {
+        for (int64_t e = at; e < min(at + 4, n); ++e) {
+            float v = part[e];
+            for (int p = 1; p < parts; ++p) v += part[p * n + e];
+            store_act<sizeof(T) == 2>(out, e, v * scale);
+        }
+    }
+}
+
+template <typename W>   // uint16_t or uint32_t
+__global__ __launch_bounds__(256) void lay_out_kernel(const char* from, int64_t stride, int64_t rows, int64_t dim, int64_t padded, W* to)
+{
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, row = at / padded, col = at % padded;
+    if (row < rows) to[at] = col < dim ? ((const W*)(from + row * stride))[col] : (W)0;
+}
+
+// ---- sizes of the launches
+
+int64_t tiles(int64_t n, int each) { return (n + each - 1) / each; }
+
+// Edge of a product's tiles, and the parts its contraction is split into.
+struct Cut {
+    int edge, parts;
+};
+
+// The cut whose rounds of workgroups cost least.
+Cut cut(int64_t m, int64_t n, int64_t k, bool bf16, bool may_split)
+{
+    Cut best{bf16 ? 256 : 128, 1};
+    double least = 1e300;
+    const int64_t cus = device_cus(), steps = tiles(k, bf16 ? 64 : 32);
+    for (const int edge : {256, 128, 64}) {
+        if (edge == 256 && !bf16) continue;
+        // workgroups of a compute unit, and cycles of a step with that many (measured)
+        const int each = edge == 256 ? 1 : edge == 128 ? 2 : 4;
+        const double step = bf16 ? (edge == 256 ? 2600. : edge == 128 ? 1700. : 1500.) : (edge == 128 ? 4500. : 2600.);
+        for (int parts = 1; parts <= (may_split ? 64 : 1) && parts <= std::max<int64_t>(1, steps / 4); ++parts) {
+            const int64_t groups = tiles(m, edge) * tiles(n, edge) * parts;
+            const double t = tiles(groups, (int)(cus * each)) * (tiles(steps, parts) * step + 6000.) + (parts > 1 ? 5000. + parts * m * n / 2000. : 0.);
+            if (t < least) least = t, best = Cut{edge, parts};
+        }
+    }
+    return best;
+}
+
+// The backward's pieces of the vocabulary: at most 1 GiB of D.
+constexpr int64_t kPieceBytes = (int64_t)1 << 30;
+struct Backward {
+    int64_t piece;       // vocabulary entries of a piece (the last one may have fewer)
+    int64_t stride;      // bytes of a row of D
+    int pieces;
+    Cut grad, dh, dw;
+    int64_t h_parts, w_parts;   // floats of the parts (0: none)
+    size_t d_bytes;
+};
+
+Backward backward(int64_t rows, int64_t vocab, int64_t dim, bool bf16)
+{
+    Backward b;
+    const int64_t each = bf16 ? 2 : 4;
+    const int64_t most = std::max<int64_t>(1024, kPieceBytes / each / std::max<int64_t>(rows, 1) / 256 * 256);
+    b.pieces = (int)std::max<int64_t>(1, tiles(vocab, (int)std::min<int64_t>(most, 1 << 30)));
+    b.piece = tiles(tiles(vocab, b.pieces), 256) * 256;
+    b.pieces = (int)tiles(vocab, (int)b.piece);
+    b.stride = std::min(b.piece, (vocab + 7) / 8 * 8) * each;
+    b.d_bytes = (size_t)rows * b.stride;
+    const int64_t width = std::min(b.piece, vocab);
+    b.grad = cut(width, rows, dim, bf16, false);
+    b.dh = cut(dim, rows, width, bf16, true);
+    b.dw = cut(dim, width, rows, bf16, true);
+    b.h_parts = b.dh.parts > 1 || b.pieces > 1 ? b.dh.parts * rows * dim : 0;
+    b.w_parts = b.dw.parts > 1 ? b.dw.parts * width * dim : 0;
+    return b;
+}
+
+size_t round16(size_t n) { return (n + 15) / 16 * 16; }
+
+template <typename T, int E>
+hipError_t forward(const LossArgs& a, hipStream_t stream)
+{
+    const int mt = (int)tiles(a.vocab, E), nt = (int)tiles(a.rows, E);
+    Part* parts = (Part*)a.ws;
+    float* own = (float*)(parts + (int64_t)mt * a.rows);
+    loss_part_kernel<T, E, E><<<dim3((unsigned)(mt * nt)), 256, 0, stream>>>(a, mt, nt, parts, own);
+    loss_join_kernel<<<dim3((unsigned)tiles(a.rows, 16)), 1024, 0, stream>>>(a, mt, parts, own);
+    return hipGetLastError();
+}
+
+template <typename T, int E>
+void grad_piece(const LossArgs& a, int64_t first, int64_t width, char* d, int64_t stride, hipStream_t stream)
+{
+    const int mt = (int)tiles(width, E), nt = (int)tiles(a.rows, E);
+    loss_grad_kernel<T, E, E><<<dim3((unsigned)(mt * nt)), 256, 0, stream>>>(a, mt, nt, first, width, d, stride);
+}
+
+template <typename T, bool TB, int E>
+void out_piece(const OutArgs& o, hipStream_t stream)
+{
+    const int mt = (int)tiles(o.dim, E), nt = (int)tiles(o.b.rows, E);
+    loss_out_kernel<T, TB, E, E><<<dim3((unsigned)((int64_t)mt * nt * o.parts)), 256, 0, stream>>>(o, mt, nt);
+}
+
+template <typename T, bool TB>
+void out_of(const OutArgs& o, int edge, hipStream_t stream)
+{
+    if constexpr (sizeof(T) == 2)
+        if (edge == 256) return out_piece<T, TB, 256>(o, stream);
+    edge == 128 ? out_piece<T, TB, 128>(o, stream) : out_piece<T, TB, 64>(o, stream);
+}
+
+template <typename T>
+void sum_of(const float* part, int parts, int64_t n, float scale, void* out, hipStream_t stream)
+{
+    loss_sum_kernel<T><<<dim3((unsigned)tiles(n, 1024)), 256, 0, stream>>>(part, parts, n, scale, out);
+}
+
+template <typename T>
+hipError_t back(const LossArgs& a, hipStream_t stream)
+{
+    constexpr bool kBf16 = sizeof(T) == 2;
+    const Backward b = backward(a.rows, a.vocab, a.out_dim, kBf16);
+    char* const d = a.ws;
+    float* const hp = (float*)(a.ws + round16(b.d_bytes));
+    float* const wp = hp + (b.h_parts + 3) / 4 * 4;
+    for (int i = 0; i < b.pieces; ++i) {
+        const int64_t first = i * b.piece, width = std::min(b.piece, a.vocab - first);
+        if (kBf16 && b.grad.edge == 256) {
+            if constexpr (kBf16) grad_piece<T, 256>(a, first, width, d, b.stride, stream);
+        } else if (b.grad.edge == 128) {
+            grad_piece<T, 128>(a, first, width, d, b.stride, stream);
+        } else {
+            grad_piece<T, 64>(a, first, width, d, b.stride, stream);
+        }
+        if (a.grad_hidden) {
+            const OutArgs o{Side{(const char*)a.weight + first * a.weight_stride, a.weight_stride, a.dim}, Side{d, b.stride, a.rows}, width,
+                            b.dh.parts, b.h_parts ? hp : nullptr, i > 0, a.grad_hidden, a.out_dim, a.scale};
+            out_of<T, false>(o, b.dh.edge, stream);
+        }
+        if (a.grad_weight) {
+            void* const to = (char*)a.grad_weight + first * a.out_dim * (int)sizeof(T);
+            const OutArgs o{Side{(const char*)a.hidden, a.hidden_stride, a.dim}, Side{d, b.stride, width}, a.rows,
+                            b.dw.parts, b.w_parts ? wp : nullptr, 0, to, a.out_dim, a.scale};
+            out_of<T, true>(o, b.dw.edge, stream);
+            if (b.w_parts) sum_of<T>(wp, b.dw.parts, width * a.out_dim, a.scale, to, stream);
+        }
+    }
+    if (a.grad_hidden && b.h_parts) sum_of<T>(hp, b.dh.parts, a.rows * a.out_dim, a.scale, a.grad_hidden, stream);
+    return hipGetLastError();
+}
+
+bool threads_fit(double groups) { return groups * 256. < 4294967296.; }
+
+}  // namespace
+
+size_t loss_ws_bytes(int64_t rows, int64_t vocab, int64_t dim, bool bf16)
+{
+    const Cut c = cut(vocab, rows, dim, bf16, false);
+    return (size_t)tiles(vocab, c.edge) * rows * sizeof(Part) + (size_t)rows * 4;
+}
+
+size_t loss_bwd_ws_bytes(int64_t rows, int64_t vocab, int64_t dim, bool bf16)
+{
+    const Backward b = backward(rows, vocab, dim, bf16);
+    return round16(b.d_bytes) + (size_t)((b.h_parts + 3) / 4 * 4 + (b.w_parts + 3) / 4 * 4) * 4;
+}
+
+bool loss_launchable(int64_t rows, int64_t vocab, int64_t dim, bool bf16, bool back)
+{
+    // (doubles: the products may pass 64 bits)
+    const double r = (double)rows, v = (double)vocab, d = (double)dim;
+    auto count = [](double n, int edge) { return std::floor(n / edge) + 1; };
+    if (!threads_fit(count(v, 64) * count(r, 64)) || !threads_fit(count(r, 4))) return false;
+    if (!back) return true;
+    return threads_fit(count(d, 64) * count(r, 64) * 64) && threads_fit(count(d, 64) * count(v, 64) * 64) &&
+           threads_fit(r * d / 1024 + 1) && threads_fit(v * d / 1024 + 1) && r * v < 1e18 && (void(bf16), true);
+}
+
+hipError_t launch_loss(const LossArgs& a, bool bf16, hipStream_t stream)
+{
+    const Cut c = cut(a.vocab, a.rows, a.out_dim, bf16, false);
+    if (bf16)
+        return c.edge == 256 ? forward<__bf16, 256>(a, stream) : c.edge == 128 ? forward<__bf16, 128>(a, stream) : forward<__bf16, 64>(a, stream);
+    return c.edge == 128 ? forward<float, 128>(a, stream) : forward<float, 64>(a, stream);
+}
+
+hipError_t launch_loss_bwd(const LossArgs& a, bool bf16, hipStream_t stream)
+{
+    return bf16 ? back<__bf16>(a, stream) : back<float>(a, stream);
+}
+
+hipError_t launch_lay_out(const void* from, int64_t from_stride, int64_t rows, int64_t dim, int64_t padded, void* to, bool bf16,
+                          hipStream_t stream)
+{
+    const dim3 grid((unsigned)tiles(rows * padded, 256));
+    if (bf16) lay_out_kernel<uint16_t><<<grid, 256, 0, stream>>>((const char*)from, from_stride, rows, dim, padded, (uint16_t*)to);
+    else lay_out_kernel<uint32_t><<<grid, 256, 0, stream>>>((const char*)from, from_stride, rows, dim, padded, (uint32_t*)to);
+    return hipGetLastError();
+}
+
+}  // namespace dpb
