@@ -26,6 +26,11 @@ torch layers; everything of the DPB itself runs in libdpb.so.
 attention as a differentiable function (dpb_attention, dpb_attention_bwd);
 `CausalAttention` the sublayer around it, with a key-value cache for generation,
 and `ParityBlock` the two sublayers of one transformer block.
+
+`EmbeddingLayer`, `RMSNormLayer` and `CrossEntropyLayer` are what stands around the
+blocks as differentiable functions: the lookup of a table's rows, the residual's
+addition with the norm of the sum, and the loss over a vocabulary; `ParityTransformer`
+is the whole model from them (§3.1).
 """
 from __future__ import annotations
 
@@ -119,12 +124,15 @@ class DPBMLP(torch.nn.Module):
 
     def forward(self, h: torch.Tensor):
         shape = h.shape
-        z = self.norm(h).reshape(-1, shape[-1])
+        out, loss_var = self.feed(self.norm(h).reshape(-1, shape[-1]))
+        return h + out.reshape(shape), loss_var
+
+    def feed(self, z: torch.Tensor):
+        """The sublayer without its norm and residual, for rows z [T, d]: (W2 gelu(W1 DPB(z)), loss_var)."""
         if self.std is not None:
             self.std.training = self.training
         y, loss_var = DPBLayer.apply(z, self.plan, self.normalized, self.n_min, self.std)
-        out = h + self.fc2(torch.nn.functional.gelu(self.fc1(y))).reshape(shape)
-        return out, loss_var
+        return self.fc2(torch.nn.functional.gelu(self.fc1(y))), loss_var
 
 
 class AttentionLayer(torch.autograd.Function):
@@ -191,13 +199,17 @@ class CausalAttention(torch.nn.Module):
         self.out = torch.nn.Linear(d, d, bias=False, dtype=dtype, device=device)
 
     def forward(self, h: torch.Tensor, cache: KeyValueCache | None = None):
-        x = self.qkv(self.norm(h)).unflatten(-1, (-1, self.head_dim))
+        return h + self.mix(self.norm(h), cache)
+
+    def mix(self, z: torch.Tensor, cache: KeyValueCache | None = None):
+        """The sublayer without its norm and residual: W_o attention(z)."""
+        x = self.qkv(z).unflatten(-1, (-1, self.head_dim))
         q, k, v = x.split((self.heads, self.kv_heads, self.kv_heads), dim=2)   # views of one tensor
         if cache is not None:
             k, v = cache.append(k, v)
             q = q.to(k.dtype)   # (under autocast the projection's type is not the cache's)
         y = AttentionLayer.apply(q, k, v, True)
-        return h + self.out(y.flatten(-2))
+        return self.out(y.flatten(-2))
 
     def cache(self, batch: int, length: int) -> KeyValueCache:
         w = self.qkv.weight
@@ -216,3 +228,161 @@ class ParityBlock(torch.nn.Module):
 
     def forward(self, h: torch.Tensor, cache: KeyValueCache | None = None):
         return self.mlp(self.attention(h, cache))
+
+
+def _even(t: torch.Tensor) -> torch.Tensor:
+    """t, or a copy whose rows are evenly apart and start on 16 bytes."""
+    try:
+        B._rows(t, "rows")
+    except ValueError:
+        return t.contiguous()
+    return t.clone(memory_format=torch.contiguous_format) if t.data_ptr() % 16 else t
+
+
+class EmbeddingLayer(torch.autograd.Function):
+    """scale * table[tokens]; tokens outside the table give zeros and no gradient."""
+
+    @staticmethod
+    def forward(ctx, tokens: torch.Tensor, table: torch.Tensor, scale: float = 1.0):
+        tokens = tokens.contiguous()
+        ctx.save_for_backward(tokens)
+        ctx.vocab, ctx.scale = table.shape[0], scale
+        return B.embedding(tokens, table, scale)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad: torch.Tensor):
+        tokens, = ctx.saved_tensors
+        return None, B.embedding_bwd(_even(grad), tokens, ctx.vocab, ctx.scale), None
+
+
+def embedding_layer(tokens: torch.Tensor, table: torch.Tensor, scale: float = 1.0):
+    """Functional form of EmbeddingLayer."""
+    return EmbeddingLayer.apply(tokens, table, scale)
+
+
+class RMSNormLayer(torch.autograd.Function):
+    """(norm of the sum, the sum) for x and residual of one type; without a residual the sum
+    is x, and (norm, None) comes back."""
+
+    @staticmethod
+    def forward(ctx, x: torch.Tensor, weight: torch.Tensor | None, residual: torch.Tensor | None = None, eps: float = 1e-6):
+        x = _even(x)
+        out, total, rstd = B.rms_norm(x, weight, None if residual is None else _even(residual), eps)
+        ctx.save_for_backward(total, weight, rstd)
+        ctx.set_materialize_grads(False)
+        return out, None if residual is None else total
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad: torch.Tensor | None, grad_total: torch.Tensor | None):
+        total, weight, rstd = ctx.saved_tensors
+        if grad is None:         # the norm itself was not used
+            return grad_total, None, grad_total if ctx.needs_input_grad[2] else None, None
+        dx, dw = B.rms_norm_bwd(_even(grad), total, weight, rstd, None if grad_total is None else _even(grad_total))
+        return dx, dw, dx if ctx.needs_input_grad[2] else None, None
+
+
+def rms_norm_layer(x: torch.Tensor, weight: torch.Tensor | None, residual: torch.Tensor | None = None, eps: float = 1e-6):
+    """Functional form of RMSNormLayer."""
+    return RMSNormLayer.apply(x, weight, residual, eps)
+
+
+class CrossEntropyLayer(torch.autograd.Function):
+    """(loss, lse) of hidden rows over a vocabulary's matrix, fp32 of the targets' shape, both
+    differentiable (a penalty on lse, say); the backward computes the logits once more."""
+
+    @staticmethod
+    def forward(ctx, hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, scale: float = 1.0):
+        hidden, weight, targets = _even(hidden), _even(weight), targets.contiguous()
+        loss, lse = B.cross_entropy(hidden, weight, targets, scale)
+        ctx.save_for_backward(hidden, weight, targets, lse)
+        ctx.scale = scale
+        ctx.set_materialize_grads(False)
+        return loss, lse
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad_loss: torch.Tensor | None, grad_lse: torch.Tensor | None):
+        hidden, weight, targets, lse = ctx.saved_tensors
+        if grad_loss is None and grad_lse is None:
+            return None, None, None, None
+        grads = [None if g is None else g.contiguous() for g in (grad_loss, grad_lse)]
+        dh, dw = B.cross_entropy_bwd(grads[0], hidden, weight, targets, lse, ctx.scale, grad_lse=grads[1],
+                                     hidden_grad=ctx.needs_input_grad[0], weight_grad=ctx.needs_input_grad[1])
+        return dh, dw, None, None
+
+
+def cross_entropy_layer(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, scale: float = 1.0):
+    """Functional form of CrossEntropyLayer: (loss, lse)."""
+    return CrossEntropyLayer.apply(hidden, weight, targets, scale)
+
+
+class ParityTransformer(torch.nn.Module):
+    """Tied token embeddings, learned positions and RMSNorm around ParityBlocks (§3.1).
+
+    The residual stream is carried as its two last terms, so that each addition is
+    part of the next norm; the blocks' own modules and parameters are used as they
+    are.  forward gives logits; loss the mean loss of the tokens that count, without
+    logits in memory."""
+
+    def __init__(self, plan: B.Plan, vocab: int, length: int, layers: int, heads: int, d_ff: int, kv_heads: int | None = None,
+                 dtype: torch.dtype = torch.float32, device=None, std: float = 0.02, **mlp):
+        super().__init__()
+        self.embed = torch.nn.Embedding(vocab, plan.d, dtype=dtype, device=device)
+        self.position = torch.nn.Embedding(length, plan.d, dtype=dtype, device=device)
+        torch.nn.init.normal_(self.embed.weight, std=std)
+        torch.nn.init.normal_(self.position.weight, std=std)
+        self.blocks = torch.nn.ModuleList(
+            ParityBlock(plan, heads, d_ff, kv_heads, dtype=dtype, device=device, **mlp) for _ in range(layers))
+        self.norm = torch.nn.RMSNorm(plan.d, dtype=dtype, device=device)
+
+    @staticmethod
+    def _norm(norm: torch.nn.RMSNorm, x: torch.Tensor, residual: torch.Tensor):
+        # (torch.nn.RMSNorm's own default, in bf16 too)
+        eps = torch.finfo(torch.float32).eps if norm.eps is None else norm.eps
+        # (under autocast a sublayer's output has not the stream's type)
+        return RMSNormLayer.apply(x.to(residual.dtype), norm.weight, residual, eps)
+
+    def hidden(self, tokens: torch.Tensor, caches=None, start: int = 0):
+        """(rows behind the last norm, the blocks' summed variance loss); with caches, tokens are
+        those from place `start` on."""
+        if start < 0 or start + tokens.shape[1] > self.position.num_embeddings:
+            raise ValueError(f"tokens {start} to {start + tokens.shape[1]}: the model has {self.position.num_embeddings} places")
+        at = torch.arange(start, start + tokens.shape[1], device=tokens.device).expand_as(tokens)
+        x, h = EmbeddingLayer.apply(tokens, self.embed.weight), EmbeddingLayer.apply(at, self.position.weight)
+        loss_var = 0.0
+        for i, block in enumerate(self.blocks):
+            z, h = self._norm(block.attention.norm, x, h)
+            x = block.attention.mix(z, None if caches is None else caches[i])
+            z, h = self._norm(block.mlp.norm, x, h)
+            x, loss = block.mlp.feed(z.flatten(0, 1))
+            x, loss_var = x.view(z.shape), loss_var + loss
+        return self._norm(self.norm, x, h)[0], loss_var
+
+    def forward(self, tokens: torch.Tensor, caches=None, start: int = 0):
+        return torch.nn.functional.linear(self.hidden(tokens, caches, start)[0], self.embed.weight)
+
+    def loss(self, tokens: torch.Tensor, targets: torch.Tensor):
+        """(mean loss over the targets that are in the vocabulary, the blocks' variance loss)."""
+        z, loss_var = self.hidden(tokens)
+        weight = self.embed.weight
+        if torch.is_autocast_enabled("cuda") and torch.get_autocast_dtype("cuda") == torch.bfloat16:
+            z, weight = z.bfloat16(), weight.bfloat16()
+        loss, _ = CrossEntropyLayer.apply(z, weight, targets)
+        counted = ((targets >= 0) & (targets < weight.shape[0])).sum()
+        return loss.sum() / counted, loss_var
+
+    def caches(self, batch: int, length: int) -> list[KeyValueCache]:
+        return [b.attention.cache(batch, length) for b in self.blocks]
+
+    @torch.no_grad()
+    def generate(self, prompt: torch.Tensor, tokens: int):
+        """`tokens` more tokens, each the likeliest: one pass over the prompt, then one token at a time."""
+        caches = self.caches(prompt.shape[0], prompt.shape[1] + tokens)
+        z, out = self.hidden(prompt, caches)[0][:, -1], [prompt]
+        for i in range(tokens):
+            out.append(torch.nn.functional.linear(z, self.embed.weight).argmax(-1, keepdim=True))
+            if i + 1 < tokens:
+                z = self.hidden(out[-1], caches, prompt.shape[1] + i)[0][:, -1]
+        return torch.cat(out, 1)

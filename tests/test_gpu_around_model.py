@@ -1,0 +1,178 @@
+"""Embedding, norm, attention, bottleneck and loss together, as a model runs them: against the same model from
+torch's own modules, replayed from graphs, on other streams, in a training step."""
+import pytest
+import torch
+
+from paper_2607_20652_amd import autograd as A
+from paper_2607_20652_amd import binding as dpb
+from paper_2607_20652_amd.optim import AdamW
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    dpb.load()
+
+
+def model_of(dtype=torch.float32, layers=2, **kw):
+    torch.manual_seed(0)
+    plan = dpb.Plan(64, 12, 3, 16, 16, 32, 0)
+    return A.ParityTransformer(plan, 501, 40, layers, 4, 96, kv_heads=2, dtype=dtype, device=DEV, std=0.3, **kw)
+
+
+def plain_loss(model, tokens, targets):
+    """The same parameters through torch's embedding, additions, norms and loss (the blocks' own forward)."""
+    F = torch.nn.functional
+    h = F.embedding(tokens, model.embed.weight) + model.position.weight[:tokens.shape[1]]
+    for block in model.blocks:
+        h, _ = block(h)
+    logits = F.linear(model.norm(h), model.embed.weight)
+    return F.cross_entropy(logits.flatten(0, 1).float(), targets.flatten(), ignore_index=-100), logits
+
+
+def grads_of(model):
+    return {n: p.grad.clone() for n, p in model.named_parameters()}
+
+
+def test_model_is_what_torch_makes_of_it():
+    model = model_of()
+    g = torch.Generator().manual_seed(1)
+    tokens, targets = torch.randint(501, (3, 37), generator=g).to(DEV), torch.randint(501, (3, 37), generator=g).to(DEV)
+    targets[:, :5] = -100
+    want, logits = plain_loss(model, tokens, targets)
+    want.backward()
+    wanted = grads_of(model)
+    model.zero_grad()
+    loss, _ = model.loss(tokens, targets)
+    loss.backward()
+    # fp32 sums of up to 501 terms, in two orders, through two blocks of six products each
+    assert abs(float(loss.detach() - want.detach())) < 1e-5 * float(want.detach())
+    assert (model(tokens) - logits).abs().max() < 2e-5 * logits.abs().max()
+    for n, got in grads_of(model).items():
+        assert (got - wanted[n]).abs().max() < 5e-5 * wanted[n].abs().max() + 1e-8, n
+
+
+def test_under_autocast():
+    model = model_of()
+    tokens = torch.randint(501, (2, 30), device=DEV)
+    with torch.no_grad():
+        want, _ = model.loss(tokens, tokens)
+    with torch.autocast("cuda", torch.bfloat16):
+        loss, _ = model.loss(tokens, tokens)
+    loss.backward()
+    # hidden rows and table rounded to bf16 (2^-8 each) in a score of size up to about 8, and what four
+    # products of bf16 operands before it leave
+    assert abs(float(loss.detach() - want)) < 6 * 2.0 ** -8 * 8
+    assert all(p.grad is not None and torch.isfinite(p.grad).all() for p in model.parameters())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_a_cache_gives_what_the_whole_sequence_gives(dtype):
+    model = model_of(dtype, layers=1)
+    tokens = torch.randint(501, (2, 20), device=DEV)
+    with torch.no_grad():
+        whole = model(tokens)
+        caches = model.caches(2, 20)
+        parts = [model(tokens[:, :9], caches)] + [model(tokens[:, i:i + 1], caches, i) for i in range(9, 20)]
+    off = (torch.cat(parts, 1) - whole).abs().amax(-1) / whole.abs().max()
+    # a bottleneck that keeps other features on a tie within rounding is off by more: at most one token in ten
+    near = 1e-5 if dtype == torch.float32 else 8 * 2.0 ** -8
+    assert (off < near).double().mean() >= (1.0 if dtype == torch.float32 else 0.9)
+
+
+def test_a_training_step():
+    """Every parameter gets a gradient, and the optimizer moves each."""
+    model = model_of(torch.bfloat16)
+    tokens = torch.randint(501, (4, 32), device=DEV)
+    model.loss(tokens, tokens)[0].backward()
+    assert all(torch.isfinite(p.grad).all() and p.grad.any() for p in model.parameters())
+    before = [p.detach().clone() for p in model.parameters()]
+    AdamW(model.parameters(), lr=1e-2).step()
+    assert all(not torch.equal(p, q) for p, q in zip(model.parameters(), before))
+
+
+def calls(s):
+    """One pass through all six calls."""
+    x = dpb.embedding(s["tokens"], s["table"], 1.5)
+    out, total, rstd = dpb.rms_norm(x, s["w"], s["res"])
+    loss, lse = dpb.cross_entropy(out, s["table"], s["targets"])
+    dh, dt = dpb.cross_entropy_bwd(s["ga"], out, s["table"], s["targets"], lse)
+    dx, dw = dpb.rms_norm_bwd(dh, total, s["w"], rstd, total)
+    de = dpb.embedding_bwd(dx, s["tokens"], s["table"].shape[0], 1.5)
+    return loss, lse, dh, dt, dx, dw, de
+
+
+def state(seed, rows=700, dim=128, vocab=2000, dtype=torch.bfloat16):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    randn = lambda *s: torch.randn(*s, device=DEV, generator=g)  # noqa: E731
+    return {"tokens": torch.randint(-1, vocab, (rows,), device=DEV, generator=g), "targets": torch.randint(-1, vocab, (rows,), device=DEV, generator=g),
+            "table": randn(vocab, dim).to(dtype), "w": randn(dim).to(dtype), "res": randn(rows, dim).to(dtype), "ga": randn(rows)}
+
+
+def test_a_captured_pass_replays():
+    s = state(0)
+    calls(s)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = calls(s)
+    for seed in (1, 2, 3, 0):
+        for k, v in state(seed).items():
+            s[k].copy_(v)
+        graph.replay()
+        got = [o.clone() for o in outs]
+        torch.cuda.synchronize()
+        for a, b in zip(got, calls(s)):
+            assert torch.equal(a, b)
+
+
+def test_two_graphs_of_one_pool_and_of_their_own():
+    """Workspaces are the allocator's: two graphs that may share its memory still give each its own results."""
+    one, two = state(4), state(5, rows=300, vocab=900)
+    calls(one), calls(two)
+    torch.cuda.synchronize()
+    a, b = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(a):
+        first = calls(one)
+    with torch.cuda.graph(b):
+        second = calls(two)
+    for _ in range(3):
+        a.replay()
+        b.replay()
+    torch.cuda.synchronize()
+    for got, want in zip((*first, *second), (*calls(one), *calls(two))):
+        assert torch.equal(got, want)
+
+
+def test_on_two_streams_at_once():
+    states = [state(6), state(7, rows=1500)]
+    want = [calls(s) for s in states]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in states]
+    got = []
+    for _ in range(4):
+        for s, stream in zip(states, streams):
+            with torch.cuda.stream(stream):
+                got.append(calls(s))
+    torch.cuda.synchronize()
+    for i, outs in enumerate(got):
+        for x, y in zip(outs, want[i % 2]):
+            assert torch.equal(x, y)
+
+
+def test_layers_give_the_calls_results():
+    s = state(8, dtype=torch.float32)
+    leaves = {k: s[k].clone().requires_grad_() for k in ("table", "w", "res")}
+    x = A.embedding_layer(s["tokens"], leaves["table"], 1.5)
+    out, total = A.rms_norm_layer(x, leaves["w"], leaves["res"])
+    loss, lse = A.cross_entropy_layer(out, leaves["table"], s["targets"])
+    ((loss * s["ga"]).sum() + 0.5 * total.square().sum()).backward()
+    want = calls(s)
+    assert torch.equal(loss, want[0]) and torch.equal(lse, want[1])
+    assert torch.equal(leaves["res"].grad, want[4]) and torch.equal(leaves["w"].grad, want[5])
+    assert torch.allclose(leaves["table"].grad, want[3] + want[6], rtol=1e-6, atol=1e-6)
