@@ -28,11 +28,17 @@ __device__ __forceinline__ void tile_of(unsigned id, unsigned mt, unsigned nt, i
     n = (int)(first + in % width);
 }
 
-__device__ __forceinline__ int64_t target_of(const LossArgs& a, int64_t row)
+__device__ __forceinline__ int target_of(const LossArgs& a, int64_t row)
 {
-    if (row >= a.rows) return -1;
     const int64_t t = a.wide_targets ? ((const int64_t*)a.targets)[row] : ((const int32_t*)a.targets)[row];
-    return t >= 0 && t < a.vocab ? t : -1;
+    return t >= 0 && t < a.vocab ? (int)t : -1;
+}
+
+// The token a lane holds in column j of a tile's fragments, or one that is there (of rows past the end nothing
+// is kept).
+__device__ __forceinline__ int64_t row_of(const LossArgs& a, int64_t n0, int j)
+{
+    return min(n0 + 32 * j + (threadIdx.x & 31), a.rows - 1);
 }
 
 // Row `from` of the wave's N as an index into what its lane half holds of them (-1: not among
@@ -51,28 +57,46 @@ __device__ __forceinline__ int one_by_one(int& v)
     return v;
 }
 
-template <int FM, int FN>
-__device__ __forceinline__ void clear(f32x16 (&c)[FM][FN])
+template <int F>
+__device__ __forceinline__ void clear(f32x16 (&c)[F][F])
 {
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
+    for (int i = 0; i < F; ++i)
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
+        for (int j = 0; j < F; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) c[i][j][r] = 0.f;
 }
 
-// Column j of a wave's fragments in ordinary registers (the products' results are not: only
-// one column of them at a time is brought over).
-template <int FM, int FN>
-__device__ __forceinline__ void take_out(const f32x16 (&c)[FM][FN], int j, f32x16 (&v)[FM])
+// Column j of a wave's fragments in ordinary registers.  The results of large tiles fill the
+// accumulator registers; moved by the compiler, all would be where the products end, into registers that
+// are not there.  (run() has waited for the last products.)
+template <int F>
+__device__ __forceinline__ void take_out(const f32x16 (&c)[F][F], int j, f32x16 (&v)[F])
 {
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-        v[i] = c[i][j];
-        __asm__ volatile("" : "+v"(v[i]));
-    }
+    for (int i = 0; i < F; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            float x;
+            __asm__ volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(c[i][j][r]));
+            v[i][r] = x;
+        }
+}
+
+// The lane, formed anew: what a tile's end derives from it is not kept in registers through the next
+// tile's products.
+__device__ __forceinline__ int fresh_lane()
+{
+    int lane = threadIdx.x & 63;
+    __asm__ volatile("" : "+v"(lane));
+    return lane;
+}
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(void* p, int64_t bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(p, 0, (int)bytes, 0x00027000);
 }
 
 // What a tile leaves of its token: sum_v 2^(l_v log2(e) - base), where base is the largest of those
@@ -89,69 +113,88 @@ __device__ __forceinline__ void join(Part& x, const Part& y)
     x.base = base;
 }
 
-template <typename T, int BM, int BN>
+template <typename T, int E>
 __global__ __launch_bounds__(256, 1) void loss_part_kernel(LossArgs a, int mt, int nt, Part* parts, float* own)
 {
-    typedef Product<T, false, false, BM, BN> P;
-    constexpr int FM = P::FM, FN = P::FN;
-    int mi, ni;
-    tile_of(blockIdx.x, mt, nt, mi, ni);
-    const int64_t m0 = (int64_t)mi * BM, n0 = (int64_t)ni * BN;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
-    const int h = lane >> 5;
-
-    f32x16 c[FM][FN];
-    clear(c);
-    P::run(Side{(const char*)a.weight, a.weight_stride, a.vocab}, Side{(const char*)a.hidden, a.hidden_stride, a.rows}, m0, n0,
-           0, a.dim, c);
-
+    typedef Product<T, false, false, E> P;
+    constexpr int F = P::F;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
     const float cs = a.scale * kLog2e;
-    const int64_t v0 = m0 + wm * (BM / 2);   // the wave's first vocabulary entry
-    const int left = (int)min(max(a.vocab - v0, (int64_t)0), (int64_t)BM);   // entries from there on
-    Part* const lds = (Part*)stage_lds<P::kStage, 0>();   // [2][BN]
-    __syncthreads();
+    const Side weight{(const char*)a.weight, a.weight_stride, a.vocab}, hidden{(const char*)a.hidden, a.hidden_stride, a.rows};
+    int mi, ni;
+    auto job = [&](unsigned id) {
+        const bool some = id < (unsigned)mt * nt;
+        tile_of(some ? id : 0, mt, nt, mi, ni);
+        return Job{(int64_t)mi * E, (int64_t)ni * E, 0, some ? a.dim : 0};
+    };
+    P prod(wave);
+    prod.start(weight, hidden, job(blockIdx.x));
+    prod.send_all();
+    int next[F];   // the next tile's targets
+    auto fetch = [&]() {
 #pragma unroll
-    for (int j = 0; j < FN; ++j) {
-        const int col = wn * (BN / 2) + 32 * j + (lane & 31);
-        f32x16 v[FM];
-        take_out(c, j, v);
-        int at = place_in<BM / 2>(target_of(a, n0 + col) - v0);
-        if (__any(at >= 0)) {
-            float l = 0.f;
+        for (int j = 0; j < F; ++j) next[j] = target_of(a, row_of(a, (int64_t)ni * E + wn * (E / 2), j));
+    };
+    fetch();
+    for (unsigned id = blockIdx.x; id < (unsigned)mt * nt; id += gridDim.x) {
+        const int tile = mi;
+        const int64_t n0 = (int64_t)ni * E, v0 = (int64_t)mi * E + wm * (E / 2);   // v0: the wave's first vocabulary entry
+        const int left = (int)min(max(a.vocab - v0, (int64_t)0), (int64_t)E);     // entries from there on
+        f32x16 c[F][F];
+        clear(c);
+        prod.run(c);
+        int target[F];
 #pragma unroll
-            for (int i = 0; i < FM; ++i)
+        for (int j = 0; j < F; ++j) target[j] = place_in<E / 2>(next[j] - v0);
+        // (past the last tile: loads of nothing)
+        prod.start(weight, hidden, job(id + gridDim.x));
+        fetch();
+
+        Part* const lds = (Part*)stage_lds<P::kStage, P::kStages - 1>();   // [2][E]
 #pragma unroll
-                for (int r = 0; r < 16; ++r) l = one_by_one(at) == 32 * i + 8 * (r >> 2) + (r & 3) ? v[i][r] : l;
-            if (at >= 0) own[n0 + col] = l;
+        for (int j = 0; j < F; ++j) {
+            f32x16 v[F];
+            take_out(c, j, v);
+            prod.send_beside(j);
+            const int lane = fresh_lane(), h = lane >> 5, col = wn * (E / 2) + 32 * j + (lane & 31);
+            if (__any(target[j] >= 0)) {
+                float l = 0.f;
+#pragma unroll
+                for (int i = 0; i < F; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) l = one_by_one(target[j]) == 32 * i + 8 * (r >> 2) + (r & 3) ? v[i][r] : l;
+                if (target[j] >= 0 && n0 + col < a.rows) own[n0 + col] = l;
+            }
+            if (left < E / 2) {
+#pragma unroll
+                for (int i = 0; i < F; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) v[i][r] = 32 * i + 8 * (r >> 2) + (r & 3) < left - 4 * h ? v[i][r] : -INFINITY;
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < F; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) top = fmaxf(top, v[i][r]);
+            top = fmaxf(top, other_half(top));
+            const float base = top == -INFINITY ? 0.f : top * cs;
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < F; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(fmaf(v[i][r], cs, -base));
+            sum += other_half(sum);
+            if (h == 0) lds[wm * E + col] = Part{top == -INFINITY ? top : base, sum};
         }
-        if (left < BM / 2) {
-#pragma unroll
-            for (int i = 0; i < FM; ++i)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) v[i][r] = 32 * i + 8 * (r >> 2) + (r & 3) + 4 * h < left ? apart(v[i][r]) : -INFINITY;
+        __syncthreads();
+        for (int col = threadIdx.x; col < E; col += 256) {
+            if (n0 + col >= a.rows) break;
+            Part x = lds[col];
+            join(x, lds[E + col]);
+            parts[(int64_t)tile * a.rows + n0 + col] = x;
         }
-        float top = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < FM; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) top = fmaxf(top, v[i][r]);
-        top = fmaxf(top, other_half(top));
-        const float base = top == -INFINITY ? 0.f : top * cs;
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < FM; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(fmaf(v[i][r], cs, -base));
-        sum += other_half(sum);
-        if (h == 0) lds[wm * BN + col] = Part{top == -INFINITY ? top : base, sum};
     }
-    __syncthreads();
-    for (int col = threadIdx.x; col < BN; col += 256) {
-        if (n0 + col >= a.rows) break;
-        Part x = lds[col];
-        join(x, lds[BN + col]);
-        parts[(int64_t)mi * a.rows + n0 + col] = x;
-    }
+    wait_loads<0>();   // none into LDS is under way when another workgroup gets it
 }
 
 // Joins the parts of 16 tokens, 64 threads each of a share of the parts.
@@ -183,86 +226,118 @@ __global__ __launch_bounds__(1024) void loss_join_kernel(LossArgs a, int mt, con
 }
 
 // D of vocabulary entries [first, first + width): `out` has rows of out_stride bytes.
-template <typename T, int BM, int BN>
+template <typename T, int E>
 __global__ __launch_bounds__(256, 1) void loss_grad_kernel(LossArgs a, int mt, int nt, int64_t first, int64_t width, char* out,
                                                            int64_t out_stride)
 {
-    typedef Product<T, false, false, BM, BN> P;
-    constexpr int FM = P::FM, FN = P::FN;
-    int mi, ni;
-    tile_of(blockIdx.x, mt, nt, mi, ni);
-    const int64_t m0 = (int64_t)mi * BM, n0 = (int64_t)ni * BN;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
-    const int h = lane >> 5;
-
-    f32x16 c[FM][FN];
-    clear(c);
-    P::run(Side{(const char*)a.weight + first * a.weight_stride, a.weight_stride, width},
-           Side{(const char*)a.hidden, a.hidden_stride, a.rows}, m0, n0, 0, a.dim, c);
-
+    typedef Product<T, false, false, E> P;
+    constexpr int F = P::F;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
     const float cs = a.scale * kLog2e;
-    const int64_t v0 = m0 + wm * (BM / 2);
-    const int left = (int)min(max(width - v0, (int64_t)0), (int64_t)BM);   // entries of the piece
-    char* const lds = stage_lds<P::kStage, 0>() + wave * (P::kStage / kWaves);
-    __syncthreads();
+    const Side weight{(const char*)a.weight + first * a.weight_stride, a.weight_stride, width};
+    const Side hidden{(const char*)a.hidden, a.hidden_stride, a.rows};
+    int mi, ni;
+    auto job = [&](unsigned id) {
+        const bool some = id < (unsigned)mt * nt;
+        tile_of(some ? id : 0, mt, nt, mi, ni);
+        return Job{(int64_t)mi * E, (int64_t)ni * E, 0, some ? a.dim : 0};
+    };
+    P prod(wave);
+    prod.start(weight, hidden, job(blockIdx.x));
+    prod.send_all();
+    // the next tile's rows: target, gradients of loss and lse, lse
+    int target[F];
+    float ga[F], ge[F], lse[F];
+    auto fetch = [&]() {
 #pragma unroll
-    for (int j = 0; j < FN; ++j) {
-        f32x16 v[FM];
-        take_out(c, j, v);
-        const int64_t row = n0 + wn * (BN / 2) + 32 * j + (lane & 31);
-        const int64_t target = target_of(a, row);
-        float ga = 0.f, ge = 0.f, lse2 = 0.f;
-        if (row < a.rows) {
-            if (a.grad_loss && target >= 0) ga = a.grad_loss[row];
-            if (a.grad_lse) ge = a.grad_lse[row];
-            lse2 = a.lse[row] * kLog2e;
+        for (int j = 0; j < F; ++j) {
+            const int64_t row = row_of(a, (int64_t)ni * E + wn * (E / 2), j);
+            target[j] = target_of(a, row);
+            ga[j] = a.grad_loss ? a.grad_loss[row] : 0.f;
+            ge[j] = a.grad_lse ? a.grad_lse[row] : 0.f;
+            lse[j] = a.lse[row];
         }
-        const bool live = ga != 0.f || ge != 0.f;
-        const float both = ga + ge;
+    };
+    fetch();
+    for (unsigned id = blockIdx.x; id < (unsigned)mt * nt; id += gridDim.x) {
+        const int64_t n0 = (int64_t)ni * E + wn * (E / 2), v0 = (int64_t)mi * E + wm * (E / 2);   // the wave's part of the tile
+        const int left = (int)min(max(width - v0, (int64_t)0), (int64_t)E);                      // entries of the piece from there on
+        f32x16 c[F][F];
+        clear(c);
+        prod.run(c);
+        float own[F], both[F], base[F];
+        int at[F];
 #pragma unroll
-        for (int i = 0; i < FM; ++i)
+        for (int j = 0; j < F; ++j) {
+            own[j] = target[j] >= 0 ? ga[j] : 0.f;
+            both[j] = own[j] + ge[j];
+            base[j] = -lse[j] * kLog2e;
+            at[j] = place_in<E / 2>(target[j] - first - v0);
+        }
+        prod.start(weight, hidden, job(id + gridDim.x));
+        fetch();
+
+        char* const lds = prod.scratch();
+        const int rows = (int)min(a.rows - n0, (int64_t)(E / 2)), bytes = (min(left, E / 2) * (int)sizeof(T) + 15) & ~15;
+        const __amdgpu_buffer_rsrc_t to = buffer(out + n0 * out_stride + v0 * (int)sizeof(T), rows > 0 && left > 0 ? (rows - 1) * out_stride + bytes : 0);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(v[i][r], cs, -lse2)) * both;
-                v[i][r] = live ? p : 0.f;
+        for (int j = 0; j < F; ++j) {
+            f32x16 v[F];
+            take_out(c, j, v);
+            prod.send_beside(j);
+            const int lane = fresh_lane(), h = lane >> 5, r32 = lane & 31;
+            if (__all(both[j] >= 0.f)) {
+                // the gradient's factor in the exponent
+                const float b = base[j] + __builtin_amdgcn_logf(both[j]);
+#pragma unroll
+                for (int i = 0; i < F; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) v[i][r] = __builtin_amdgcn_exp2f(fmaf(v[i][r], cs, b));
+            } else {
+#pragma unroll
+                for (int i = 0; i < F; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) v[i][r] = __builtin_amdgcn_exp2f(fmaf(v[i][r], cs, base[j])) * both[j];
             }
-        int at = place_in<BM / 2>(target - first - v0);
-        if (__any(at >= 0)) {
+            if (__any(at[j] >= 0)) {
 #pragma unroll
-            for (int i = 0; i < FM; ++i)
+                for (int i = 0; i < F; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) v[i][r] -= one_by_one(at) == 32 * i + 8 * (r >> 2) + (r & 3) ? ga : 0.f;
-        }
-        if (left < BM / 2) {
-#pragma unroll
-            for (int i = 0; i < FM; ++i)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) v[i][r] = 32 * i + 8 * (r >> 2) + (r & 3) + 4 * h < left ? apart(v[i][r]) : 0.f;
-        }
-        // 32 tokens of BM / 2 entries, through LDS into whole lines
-        constexpr int kRow = BM / 2 * (int)sizeof(T), kChunks = kRow / 16;
-        static_assert(32 * kRow <= P::kStage / kWaves, "a wave's share of a stage holds 32 rows");
-        wave_sync();
-        const int r32 = lane & 31;
-#pragma unroll
-        for (int i = 0; i < FM; ++i)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int byte = (32 * i + 8 * g + 4 * h) * (int)sizeof(T), chunk = byte >> 4;
-                char* to = lds + r32 * kRow + (((chunk & ~3) | ((chunk ^ r32) & 3)) << 4) + (byte & 15);
-                store4<T>(to, 0, v[i][4 * g], v[i][4 * g + 1], v[i][4 * g + 2], v[i][4 * g + 3]);
+                    for (int r = 0; r < 16; ++r) v[i][r] -= one_by_one(at[j]) == 32 * i + 8 * (r >> 2) + (r & 3) ? own[j] : 0.f;
             }
-        wave_sync();
-        const int bytes = (left * (int)sizeof(T) + 15) / 16 * 16;
+            if (left < E / 2 || __any(own[j] == 0.f)) {
+                // entries past the piece, and rows without a gradient, whatever their scores and lse
+                const int some = own[j] == 0.f && both[j] == 0.f ? 0 : left - 4 * h;
 #pragma unroll
-        for (int k = 0; k < kChunks / 2; ++k) {
-            const int r = k * (64 / kChunks) + lane / kChunks, chunk = lane % kChunks;
-            const int64_t t = n0 + wn * (BN / 2) + 32 * j + r;
-            if (t < a.rows && chunk * 16 < bytes)
-                *(u32x4*)(out + t * out_stride + v0 * (int)sizeof(T) + chunk * 16) =
-                    *(const u32x4*)(lds + r * kRow + (((chunk & ~3) | ((chunk ^ r) & 3)) << 4));
+                for (int i = 0; i < F; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) v[i][r] = 32 * i + 8 * (r >> 2) + (r & 3) < some ? v[i][r] : 0.f;
+            }
+            // 32 tokens of E / 2 entries, through LDS into whole lines
+            constexpr int kRow = E / 2 * (int)sizeof(T), kChunks = kRow / 16;
+            static_assert(32 * kRow <= P::kScratch, "a wave's share of a stage holds 32 rows");
+            wave_sync();
+#pragma unroll
+            for (int i = 0; i < F; ++i)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int byte = (32 * i + 8 * g + 4 * h) * (int)sizeof(T), chunk = byte >> 4;
+                    char* at = lds + r32 * kRow + (((chunk & ~3) | ((chunk ^ r32) & 3)) << 4) + (byte & 15);
+                    store4<T>(at, 0, v[i][4 * g], v[i][4 * g + 1], v[i][4 * g + 2], v[i][4 * g + 3]);
+                }
+            wave_sync();
+            // (past the piece's entries out of the buffer's range: not stored)
+            const int chunk = lane % kChunks, r0 = lane / kChunks, stride = (int)out_stride;
+            const uint32_t from = chunk * 16 < bytes ? (uint32_t)((32 * j + r0) * stride + chunk * 16) : 0x80000000u;
+#pragma unroll
+            for (int k = 0; k < kChunks / 2; ++k) {
+                const int r = k * (64 / kChunks) + r0;
+                __builtin_amdgcn_raw_buffer_store_b128(*(const u32x4*)(lds + r * kRow + (((chunk & ~3) | ((chunk ^ r) & 3)) << 4)), to,
+                                                       (int)(from + (uint32_t)(k * (64 / kChunks) * stride)), 0, 0);
+            }
         }
     }
+    wait_loads<0>();   // none into LDS is under way when another workgroup gets it
 }
 
 struct OutArgs {
@@ -277,65 +352,97 @@ struct OutArgs {
 };
 
 // out[n][m] = scale sum_k a[k][m] b[n][k] (b plain) or b[k][n] (transposed).
-template <typename T, bool TB, int BM, int BN>
+template <typename T, bool TB, int E>
 __global__ __launch_bounds__(256, 1) void loss_out_kernel(OutArgs o, int mt, int nt)
 {
-    typedef Product<T, true, TB, BM, BN> P;
-    constexpr int FM = P::FM, FN = P::FN;
-    int mi, ni;
-    const unsigned tiles = (unsigned)mt * nt, part = blockIdx.x / tiles;
-    tile_of(blockIdx.x % tiles, mt, nt, mi, ni);
-    const int64_t m0 = (int64_t)mi * BM, n0 = (int64_t)ni * BN;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
-    const int h = lane >> 5;
+    typedef Product<T, true, TB, E> P;
+    constexpr int F = P::F;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
+    const unsigned tiles = (unsigned)mt * nt, all = tiles * o.parts;
     const int64_t steps = (o.k + P::kK - 1) / P::kK;
-    const int64_t begin = steps * part / o.parts * P::kK, end = min(steps * (part + 1) / o.parts * P::kK, o.k);
-
-    f32x16 c[FM][FN];
-    clear(c);
-    P::run(o.a, o.b, m0, n0, begin, end, c);
-
-    char* const lds = stage_lds<P::kStage, 0>() + wave * (P::kStage / kWaves);
-    constexpr int kRow = BM / 2 * 4, kChunks = kRow / 16;
-    static_assert(32 * kRow <= P::kStage / kWaves, "a wave's share of a stage holds 32 rows");
     const bool whole = o.dim % 4 == 0;
-    __syncthreads();
+    int mi, ni;
+    int64_t part;
+    auto job = [&](unsigned id) {
+        const bool some = id < all;
+        if (!some) id = 0;
+        part = id / tiles;
+        tile_of(id % tiles, mt, nt, mi, ni);
+        const int64_t begin = steps * part / o.parts * P::kK;
+        return Job{(int64_t)mi * E, (int64_t)ni * E, begin, some ? min(steps * (part + 1) / o.parts * P::kK, o.k) : begin};
+    };
+    P prod(wave);
+    prod.start(o.a, o.b, job(blockIdx.x));
+    prod.send_all();
+    for (unsigned id = blockIdx.x; id < all; id += gridDim.x) {
+        const int64_t m0 = (int64_t)mi * E + wm * (E / 2), n0 = (int64_t)ni * E + wn * (E / 2), p0 = part * o.b.rows;
+        f32x16 c[F][F];
+        clear(c);
+        prod.run(c);
+        prod.start(o.a, o.b, job(id + gridDim.x));   // (past the last tile: loads of nothing)
+
+        char* const lds = prod.scratch();
+        const int size = o.part ? 4 : (int)sizeof(T), row = (int)o.dim * size, rows = (int)min(o.b.rows - n0, (int64_t)(E / 2));
+        char* const base = (o.part ? (char*)o.part + (p0 + n0) * row : (char*)o.out + n0 * row) + m0 * size;
+        const __amdgpu_buffer_rsrc_t to = buffer(base, rows > 0 && m0 < o.dim ? (rows - 1) * (int64_t)row + min((int64_t)(E / 2), o.dim - m0) * size : 0);
+        // 32 rows, so many fragments at a time as the wave's share of a stage holds
+        constexpr int kFit = P::kScratch / (32 * 128), G = kFit < F ? kFit : F, kRow = G * 128, kChunks = kRow / 16;
+        static_assert(G >= 1 && F % G == 0, "fragments through LDS");
 #pragma unroll
-    for (int j = 0; j < FN; ++j) {
-        f32x16 v[FM];
-        take_out(c, j, v);
-        wave_sync();
-        const int r32 = lane & 31;
+        for (int j = 0; j < F; ++j) {
+            f32x16 v[F];
+            take_out(c, j, v);
+            prod.send_beside(j);
+            const int lane = fresh_lane(), h = lane >> 5, r32 = lane & 31;
 #pragma unroll
-        for (int i = 0; i < FM; ++i)
+            for (int q = 0; q < F; q += G) {
+                wave_sync();
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int chunk = 8 * i + 2 * g + h;
-                *(f32x4*)(lds + r32 * kRow + ((chunk ^ (r32 & 7)) << 4)) =
-                    (f32x4){v[i][4 * g], v[i][4 * g + 1], v[i][4 * g + 2], v[i][4 * g + 3]};
-            }
-        wave_sync();
-#pragma unroll 4
-        for (int k = 0; k < kChunks / 2; ++k) {
-            const int r = k * (64 / kChunks) + lane / kChunks, chunk = lane % kChunks;
-            const int64_t n = n0 + wn * (BN / 2) + 32 * j + r, m = m0 + wm * (BM / 2) + chunk * 4;
-            if (n >= o.b.rows || m >= o.dim) continue;
-            f32x4 w = *(const f32x4*)(lds + r * kRow + ((chunk ^ (r & 7)) << 4));
-            if (o.part) {
-                float* to = o.part + (part * o.b.rows + n) * o.dim + m;
+                for (int i = 0; i < G; ++i)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const int chunk = 8 * i + 2 * g + h;
+                        *(f32x4*)(lds + r32 * kRow + ((chunk ^ (r32 & 7)) << 4)) =
+                            (f32x4){v[q + i][4 * g], v[q + i][4 * g + 1], v[q + i][4 * g + 2], v[q + i][4 * g + 3]};
+                    }
+                wave_sync();
+                const int chunk = lane % kChunks, r0 = lane / kChunks, m = 32 * q + chunk * 4;
                 if (whole) {
-                    if (o.add) w += *(const f32x4*)to;
-                    *(f32x4*)to = w;
+                    // (rows and columns past the result's lie out of the buffer's range: not read, not stored)
+                    const uint32_t from = m0 + m < o.dim ? (uint32_t)((32 * j + r0) * row + m * size) : 0x80000000u;
+#pragma unroll 4
+                    for (int k = 0; k < kChunks / 2; ++k) {
+                        const int r = k * (64 / kChunks) + r0;
+                        const uint32_t at = from + (uint32_t)(k * (64 / kChunks) * row);
+                        f32x4 w = *(const f32x4*)(lds + r * kRow + ((chunk ^ (r & 7)) << 4));
+                        if (o.part) {
+                            if (o.add) w += __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(to, (int)at, 0, 0));
+                            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, w), to, (int)at, 0, 0);
+                        } else {
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) w[x] *= o.scale;
+                            if constexpr (sizeof(T) == 2)
+                                __builtin_amdgcn_raw_buffer_store_b64((u32x2){pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3])}, to, (int)at, 0, 0);
+                            else
+                                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, w), to, (int)at, 0, 0);
+                        }
+                    }
                 } else {
-                    for (int e = 0; e < 4 && m + e < o.dim; ++e) to[e] = o.add ? to[e] + w[e] : w[e];
+                    for (int k = 0; k < kChunks / 2; ++k) {
+                        const int r = k * (64 / kChunks) + r0;
+                        const int64_t n = n0 + 32 * j + r;
+                        for (int x = 0; x < 4 && n < o.b.rows && m0 + m + x < o.dim; ++x) {
+                            const float w = *(const float*)(lds + r * kRow + ((chunk ^ (r & 7)) << 4) + 4 * x);
+                            const int64_t at = n * o.dim + m0 + m + x;
+                            if (!o.part) store_act<sizeof(T) == 2>(o.out, at, w * o.scale);
+                            else o.part[p0 * o.dim + at] = o.add ? o.part[p0 * o.dim + at] + w : w;
+                        }
+                    }
                 }
-            } else if (whole) {
-                store4<T>((char*)o.out + (n * o.dim + m) * (int)sizeof(T), 0, w[0] * o.scale, w[1] * o.scale, w[2] * o.scale, w[3] * o.scale);
-            } else {
-                for (int e = 0; e < 4 && m + e < o.dim; ++e) store_act<sizeof(T) == 2>(o.out, n * o.dim + m + e, w[e] * o.scale);
             }
         }
     }
+    wait_loads<0>();   // none into LDS is under way when another workgroup gets it
 }
 
 // The parts' sum in their order, times scale: four values a thread.
@@ -368,6 +475,12 @@ __global__ __launch_bounds__(256) void lay_out_kernel(const char* from, int64_t 
 
 int64_t tiles(int64_t n, int each) { return (n + each - 1) / each; }
 
+// Workgroups of a compute unit, by their LDS (and the large tiles' registers).
+int sharing(int edge) { return edge == 256 ? 1 : edge == 128 ? 2 : 4; }
+
+// As many workgroups as the chip holds, which take the tiles in turn.
+dim3 resident(int64_t groups, int edge) { return dim3((unsigned)std::min<int64_t>(groups, (int64_t)device_cus() * sharing(edge))); }
+
 // Edge of a product's tiles, and the parts its contraction is split into.
 struct Cut {
     int edge, parts;
@@ -382,7 +495,7 @@ Cut cut(int64_t m, int64_t n, int64_t k, bool bf16, bool may_split)
     for (const int edge : {256, 128, 64}) {
         if (edge == 256 && !bf16) continue;
         // workgroups of a compute unit, and cycles of a step with that many (measured)
-        const int each = edge == 256 ? 1 : edge == 128 ? 2 : 4;
+        const int each = sharing(edge);
         const double step = bf16 ? (edge == 256 ? 2600. : edge == 128 ? 1700. : 1500.) : (edge == 128 ? 4500. : 2600.);
         for (int parts = 1; parts <= (may_split ? 64 : 1) && parts <= std::max<int64_t>(1, steps / 4); ++parts) {
             const int64_t groups = tiles(m, edge) * tiles(n, edge) * parts;
@@ -393,8 +506,9 @@ Cut cut(int64_t m, int64_t n, int64_t k, bool bf16, bool may_split)
     return best;
 }
 
-// The backward's pieces of the vocabulary: at most 1 GiB of D.
-constexpr int64_t kPieceBytes = (int64_t)1 << 30;
+// The backward's pieces of the vocabulary: at most 1 GiB of D, and rows of 8 MiB (those of a tile stay
+// within a 31-bit offset).
+constexpr int64_t kPieceBytes = (int64_t)1 << 30, kPieceRow = (int64_t)1 << 23;
 struct Backward {
     int64_t piece;       // vocabulary entries of a piece (the last one may have fewer)
     int64_t stride;      // bytes of a row of D
@@ -408,8 +522,8 @@ Backward backward(int64_t rows, int64_t vocab, int64_t dim, bool bf16)
 {
     Backward b;
     const int64_t each = bf16 ? 2 : 4;
-    const int64_t most = std::max<int64_t>(1024, kPieceBytes / each / std::max<int64_t>(rows, 1) / 256 * 256);
-    b.pieces = (int)std::max<int64_t>(1, tiles(vocab, (int)std::min<int64_t>(most, 1 << 30)));
+    const int64_t most = std::max<int64_t>(1024, std::min(kPieceBytes / std::max<int64_t>(rows, 1), kPieceRow) / each / 256 * 256);
+    b.pieces = (int)std::max<int64_t>(1, tiles(vocab, (int)most));
     b.piece = tiles(tiles(vocab, b.pieces), 256) * 256;
     b.pieces = (int)tiles(vocab, (int)b.piece);
     b.stride = std::min(b.piece, (vocab + 7) / 8 * 8) * each;
@@ -431,7 +545,7 @@ hipError_t forward(const LossArgs& a, hipStream_t stream)
     const int mt = (int)tiles(a.vocab, E), nt = (int)tiles(a.rows, E);
     Part* parts = (Part*)a.ws;
     float* own = (float*)(parts + (int64_t)mt * a.rows);
-    loss_part_kernel<T, E, E><<<dim3((unsigned)(mt * nt)), 256, 0, stream>>>(a, mt, nt, parts, own);
+    loss_part_kernel<T, E><<<resident((int64_t)mt * nt, E), 256, 0, stream>>>(a, mt, nt, parts, own);
     loss_join_kernel<<<dim3((unsigned)tiles(a.rows, 16)), 1024, 0, stream>>>(a, mt, parts, own);
     return hipGetLastError();
 }
@@ -440,14 +554,14 @@ template <typename T, int E>
 void grad_piece(const LossArgs& a, int64_t first, int64_t width, char* d, int64_t stride, hipStream_t stream)
 {
     const int mt = (int)tiles(width, E), nt = (int)tiles(a.rows, E);
-    loss_grad_kernel<T, E, E><<<dim3((unsigned)(mt * nt)), 256, 0, stream>>>(a, mt, nt, first, width, d, stride);
+    loss_grad_kernel<T, E><<<resident((int64_t)mt * nt, E), 256, 0, stream>>>(a, mt, nt, first, width, d, stride);
 }
 
 template <typename T, bool TB, int E>
 void out_piece(const OutArgs& o, hipStream_t stream)
 {
     const int mt = (int)tiles(o.dim, E), nt = (int)tiles(o.b.rows, E);
-    loss_out_kernel<T, TB, E, E><<<dim3((unsigned)((int64_t)mt * nt * o.parts)), 256, 0, stream>>>(o, mt, nt);
+    loss_out_kernel<T, TB, E><<<resident((int64_t)mt * nt * o.parts, E), 256, 0, stream>>>(o, mt, nt);
 }
 
 template <typename T, bool TB>
