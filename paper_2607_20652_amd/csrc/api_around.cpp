@@ -217,7 +217,7 @@ static dpb_status logits_ok(const dpb_logits* a, dpb_dtype dtype, bool backward)
         return DPB_EINVAL;
     const int64_t b = bytes_of(dtype);
     if (a->rows >= kMaxRows || a->vocab >= kMaxRows || round_up(a->dim * b, 16) >= kMaxStride || a->hidden_stride >= kMaxStride / b ||
-        a->weight_stride >= kMaxStride / b || !dpb::loss_launchable(a->rows, a->vocab, a->dim, dtype == DPB_BF16, backward))
+        a->weight_stride >= kMaxStride / b || !dpb::loss_launchable(a->rows, a->vocab, a->dim, backward))
         return DPB_EUNSUPPORTED;
     // copies of rows that do not start on 16 bytes: a thread an element
     if (((double)a->rows + 1) * (a->dim + 8.) / 256 >= kMaxGroups || ((double)a->vocab + 1) * (a->dim + 8.) / 256 >= kMaxGroups)

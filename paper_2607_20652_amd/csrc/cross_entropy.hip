@@ -9,6 +9,7 @@
 // more, leaves its D in the operands' type, and D is an operand of two products.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "cross_entropy.hpp"
 #include "product.hpp"
@@ -116,7 +117,7 @@ __device__ __forceinline__ void join(Part& x, const Part& y)
 template <typename T, int E>
 __global__ __launch_bounds__(256, 1) void loss_part_kernel(LossArgs a, int mt, int nt, Part* parts, float* own)
 {
-    typedef Product<T, false, false, E> P;
+    typedef Product<T, false, false, Lies::rows, E> P;
     constexpr int F = P::F;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
     const float cs = a.scale * kLog2e;
@@ -225,12 +226,12 @@ __global__ __launch_bounds__(1024) void loss_join_kernel(LossArgs a, int mt, con
     a.loss[row] = target_of(a, row) < 0 || loss < 0.f ? 0.f : loss;
 }
 
-// D of vocabulary entries [first, first + width): `out` has rows of out_stride bytes.
+// D of vocabulary entries [first, first + width) in blocks, `group` bytes for 64 tokens.
 template <typename T, int E>
 __global__ __launch_bounds__(256, 1) void loss_grad_kernel(LossArgs a, int mt, int nt, int64_t first, int64_t width, char* out,
-                                                           int64_t out_stride)
+                                                           int64_t group)
 {
-    typedef Product<T, false, false, E> P;
+    typedef Product<T, false, false, Lies::rows, E> P;
     constexpr int F = P::F;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
     const float cs = a.scale * kLog2e;
@@ -269,8 +270,9 @@ __global__ __launch_bounds__(256, 1) void loss_grad_kernel(LossArgs a, int mt, i
         int at[F];
 #pragma unroll
         for (int j = 0; j < F; ++j) {
-            own[j] = target[j] >= 0 ? ga[j] : 0.f;
-            both[j] = own[j] + ge[j];
+            const bool there = n0 + 32 * j + (threadIdx.x & 31) < a.rows;
+            own[j] = there && target[j] >= 0 ? ga[j] : 0.f;
+            both[j] = there ? own[j] + ge[j] : 0.f;
             base[j] = -lse[j] * kLog2e;
             at[j] = place_in<E / 2>(target[j] - first - v0);
         }
@@ -278,8 +280,8 @@ __global__ __launch_bounds__(256, 1) void loss_grad_kernel(LossArgs a, int mt, i
         fetch();
 
         char* const lds = prod.scratch();
-        const int rows = (int)min(a.rows - n0, (int64_t)(E / 2)), bytes = (min(left, E / 2) * (int)sizeof(T) + 15) & ~15;
-        const __amdgpu_buffer_rsrc_t to = buffer(out + n0 * out_stride + v0 * (int)sizeof(T), rows > 0 && left > 0 ? (rows - 1) * out_stride + bytes : 0);
+        constexpr int kEach = 64 / (int)sizeof(T);   // entries of a block
+        const int blocks = (int)min(group / kBlockBytes - v0 / kEach, (int64_t)(E / 2 / kEach));
 #pragma unroll
         for (int j = 0; j < F; ++j) {
             f32x16 v[F];
@@ -306,14 +308,14 @@ __global__ __launch_bounds__(256, 1) void loss_grad_kernel(LossArgs a, int mt, i
                     for (int r = 0; r < 16; ++r) v[i][r] -= one_by_one(at[j]) == 32 * i + 8 * (r >> 2) + (r & 3) ? own[j] : 0.f;
             }
             if (left < E / 2 || __any(own[j] == 0.f)) {
-                // entries past the piece, and rows without a gradient, whatever their scores and lse
+                // entries past the piece, and rows without a gradient (and past the last), whatever their scores and lse
                 const int some = own[j] == 0.f && both[j] == 0.f ? 0 : left - 4 * h;
 #pragma unroll
                 for (int i = 0; i < F; ++i)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) v[i][r] = 32 * i + 8 * (r >> 2) + (r & 3) < some ? v[i][r] : 0.f;
             }
-            // 32 tokens of E / 2 entries, through LDS into whole lines
+            // 32 tokens of E / 2 entries, through LDS into blocks: 1 KB a store
             constexpr int kRow = E / 2 * (int)sizeof(T), kChunks = kRow / 16;
             static_assert(32 * kRow <= P::kScratch, "a wave's share of a stage holds 32 rows");
             wave_sync();
@@ -322,69 +324,107 @@ __global__ __launch_bounds__(256, 1) void loss_grad_kernel(LossArgs a, int mt, i
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
                     const int byte = (32 * i + 8 * g + 4 * h) * (int)sizeof(T), chunk = byte >> 4;
-                    char* at = lds + r32 * kRow + (((chunk & ~3) | ((chunk ^ r32) & 3)) << 4) + (byte & 15);
-                    store4<T>(at, 0, v[i][4 * g], v[i][4 * g + 1], v[i][4 * g + 2], v[i][4 * g + 3]);
+                    store4<T>(lds + r32 * kRow + ((chunk ^ (r32 & (kChunks - 1))) << 4) + (byte & 15), 0, v[i][4 * g], v[i][4 * g + 1],
+                              v[i][4 * g + 2], v[i][4 * g + 3]);
                 }
             wave_sync();
-            // (past the piece's entries out of the buffer's range: not stored)
-            const int chunk = lane % kChunks, r0 = lane / kChunks, stride = (int)out_stride;
-            const uint32_t from = chunk * 16 < bytes ? (uint32_t)((32 * j + r0) * stride + chunk * 16) : 0x80000000u;
+            const int64_t t0 = n0 + 32 * j;
+            char* const to = out + t0 / kBlockRows * group + v0 / kEach * kBlockBytes + t0 % kBlockRows * 64 + lane * 16;
+            // (whole blocks: their last tokens' rows are zeros)
+            if (t0 < (a.rows + kBlockRows - 1) / kBlockRows * kBlockRows)
 #pragma unroll
-            for (int k = 0; k < kChunks / 2; ++k) {
-                const int r = k * (64 / kChunks) + r0;
-                __builtin_amdgcn_raw_buffer_store_b128(*(const u32x4*)(lds + r * kRow + (((chunk & ~3) | ((chunk ^ r) & 3)) << 4)), to,
-                                                       (int)(from + (uint32_t)(k * (64 / kChunks) * stride)), 0, 0);
-            }
+                for (int k = 0; k < 2 * (E / 2 / kEach); ++k) {
+                    const int r = k % 2 * 16 + lane / 4, chunk = k / 2 * 4 + lane % 4;
+                    if (k / 2 < blocks)
+                        *(u32x4*)(to + k / 2 * kBlockBytes + k % 2 * 1024) = *(const u32x4*)(lds + r * kRow + ((chunk ^ (r & (kChunks - 1))) << 4));
+                }
         }
     }
     wait_loads<0>();   // none into LDS is under way when another workgroup gets it
 }
 
+// A product's tiles: `whole` of them with all of their contraction, the `rest` in `parts` parts of it each
+// (1: none), which a second kernel adds up.
+struct Cut {
+    int edge;
+    int whole, rest, parts;
+};
+
 struct OutArgs {
     Side a, b;          // the result's contiguous index (transposed), and its rows
     int64_t k;          // contraction
-    int parts;
-    float* part;        // [parts][rows][dim] fp32, or null: the result itself
-    int add;            // to what the parts hold
+    int mt, nt;         // tiles
+    Cut cut;
+    float* part;        // [parts][rest][edge][edge]
+    float* sum;         // fp32 [rows][dim] of a result that comes in pieces, or null
+    int first, last;    // piece: the first finds nothing in `sum`, the last leaves the result
     void* out;
     int64_t dim;        // of a result's row
     float scale;
 };
 
+// Four values of row n, from column m: what earlier pieces left, and where this one's go.
+template <typename T>
+__device__ __forceinline__ void leave4(const OutArgs& o, int64_t n, int64_t m, f32x4 v)
+{
+    const int64_t at = n * o.dim + m;
+    if (o.dim % 4 == 0) {
+        if (!o.first) v += *(const f32x4*)(o.sum + at);
+        if (o.last) store4<T>((char*)o.out + at * (int)sizeof(T), 0, v[0] * o.scale, v[1] * o.scale, v[2] * o.scale, v[3] * o.scale);
+        else *(f32x4*)(o.sum + at) = v;
+    } else {
+        for (int x = 0; x < 4 && m + x < o.dim; ++x) {
+            const float w = o.first ? v[x] : v[x] + o.sum[at + x];
+            if (o.last) store_act<sizeof(T) == 2>(o.out, at + x, w * o.scale);
+            else o.sum[at + x] = w;
+        }
+    }
+}
+
 // out[n][m] = scale sum_k a[k][m] b[n][k] (b plain) or b[k][n] (transposed).
 template <typename T, bool TB, int E>
-__global__ __launch_bounds__(256, 1) void loss_out_kernel(OutArgs o, int mt, int nt)
+__global__ __launch_bounds__(256, 1) void loss_out_kernel(OutArgs o)
 {
-    typedef Product<T, true, TB, E> P;
+    typedef Product<T, true, TB, Lies::blocks, E> P;
     constexpr int F = P::F;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
-    const unsigned tiles = (unsigned)mt * nt, all = tiles * o.parts;
+    const unsigned whole = (unsigned)o.cut.whole, rest = (unsigned)o.cut.rest, all = whole + rest * o.cut.parts;
     const int64_t steps = (o.k + P::kK - 1) / P::kK;
-    const bool whole = o.dim % 4 == 0;
+    const bool lines = o.dim * (int)sizeof(T) % 16 == 0;
     int mi, ni;
-    int64_t part;
+    int64_t place;   // of a part's tile in the scratch, or -1
     auto job = [&](unsigned id) {
         const bool some = id < all;
         if (!some) id = 0;
-        part = id / tiles;
-        tile_of(id % tiles, mt, nt, mi, ni);
-        const int64_t begin = steps * part / o.parts * P::kK;
-        return Job{(int64_t)mi * E, (int64_t)ni * E, begin, some ? min(steps * (part + 1) / o.parts * P::kK, o.k) : begin};
+        const unsigned x = id - whole, part = id < whole ? 0 : x / rest, of = id < whole ? 1 : o.cut.parts;
+        place = id < whole ? (int64_t)-1 : (int64_t)x;   // (-1 and x have no common type that holds both)
+        tile_of(id < whole ? id : whole + x % rest, o.mt, o.nt, mi, ni);
+        const int64_t begin = steps * part / of * P::kK;
+        return Job{(int64_t)mi * E, (int64_t)ni * E, begin, some ? min(steps * (part + 1) / of * P::kK, o.k) : begin};
     };
     P prod(wave);
     prod.start(o.a, o.b, job(blockIdx.x));
     prod.send_all();
     for (unsigned id = blockIdx.x; id < all; id += gridDim.x) {
-        const int64_t m0 = (int64_t)mi * E + wm * (E / 2), n0 = (int64_t)ni * E + wn * (E / 2), p0 = part * o.b.rows;
+        const int64_t m0 = (int64_t)mi * E + wm * (E / 2), n0 = (int64_t)ni * E + wn * (E / 2);
+        // What the wave stores: its quarter of a part's tile, of the sum so far, or of the result.  Rows and
+        // columns past the result's end are out of the buffer's range.
+        const bool part = place >= 0, fp32 = part || !o.last;
+        const int64_t width = part ? E : o.dim, rows = part ? E / 2 : min(o.b.rows - n0, (int64_t)(E / 2));
+        const int size = fp32 ? 4 : (int)sizeof(T), row = (int)width * size, sum_row = (int)o.dim * 4;
+        const int64_t columns = part ? E / 2 : min(o.dim - m0, (int64_t)(E / 2)), at = n0 * o.dim + m0;
+        const bool some = rows > 0 && columns > 0;
+        char* const base = part ? (char*)(o.part + place * (E * E) + (wn * (E / 2)) * E + wm * (E / 2))
+                                : o.last ? (char*)o.out + at * (int)sizeof(T) : (char*)(o.sum + at);
+        const __amdgpu_buffer_rsrc_t to = buffer(base, some ? (rows - 1) * row + columns * size : 0);
+        const __amdgpu_buffer_rsrc_t sum = buffer(o.sum + at, some && !part && !o.first ? (rows - 1) * sum_row + columns * 4 : 0);
+        const bool add = !part && !o.first;
         f32x16 c[F][F];
         clear(c);
         prod.run(c);
         prod.start(o.a, o.b, job(id + gridDim.x));   // (past the last tile: loads of nothing)
 
         char* const lds = prod.scratch();
-        const int size = o.part ? 4 : (int)sizeof(T), row = (int)o.dim * size, rows = (int)min(o.b.rows - n0, (int64_t)(E / 2));
-        char* const base = (o.part ? (char*)o.part + (p0 + n0) * row : (char*)o.out + n0 * row) + m0 * size;
-        const __amdgpu_buffer_rsrc_t to = buffer(base, rows > 0 && m0 < o.dim ? (rows - 1) * (int64_t)row + min((int64_t)(E / 2), o.dim - m0) * size : 0);
         // 32 rows, so many fragments at a time as the wave's share of a stage holds
         constexpr int kFit = P::kScratch / (32 * 128), G = kFit < F ? kFit : F, kRow = G * 128, kChunks = kRow / 16;
         static_assert(G >= 1 && F % G == 0, "fragments through LDS");
@@ -406,62 +446,68 @@ __global__ __launch_bounds__(256, 1) void loss_out_kernel(OutArgs o, int mt, int
                             (f32x4){v[q + i][4 * g], v[q + i][4 * g + 1], v[q + i][4 * g + 2], v[q + i][4 * g + 3]};
                     }
                 wave_sync();
-                const int chunk = lane % kChunks, r0 = lane / kChunks, m = 32 * q + chunk * 4;
-                if (whole) {
-                    // (rows and columns past the result's lie out of the buffer's range: not read, not stored)
-                    const uint32_t from = m0 + m < o.dim ? (uint32_t)((32 * j + r0) * row + m * size) : 0x80000000u;
-#pragma unroll 4
+                if (!part && !lines) {   // rows that do not start on 16 bytes
+                    const int chunk = lane % kChunks, r0 = lane / kChunks, m = 32 * q + chunk * 4;
                     for (int k = 0; k < kChunks / 2; ++k) {
                         const int r = k * (64 / kChunks) + r0;
-                        const uint32_t at = from + (uint32_t)(k * (64 / kChunks) * row);
-                        f32x4 w = *(const f32x4*)(lds + r * kRow + ((chunk ^ (r & 7)) << 4));
-                        if (o.part) {
-                            if (o.add) w += __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(to, (int)at, 0, 0));
-                            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, w), to, (int)at, 0, 0);
-                        } else {
-#pragma unroll
-                            for (int x = 0; x < 4; ++x) w[x] *= o.scale;
-                            if constexpr (sizeof(T) == 2)
-                                __builtin_amdgcn_raw_buffer_store_b64((u32x2){pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3])}, to, (int)at, 0, 0);
-                            else
-                                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, w), to, (int)at, 0, 0);
-                        }
+                        const f32x4 w = *(const f32x4*)(lds + r * kRow + ((chunk ^ (r & 7)) << 4));
+                        if (n0 + 32 * j + r < o.b.rows && m0 + m < o.dim) leave4<T>(o, n0 + 32 * j + r, m0 + m, w);
                     }
-                } else {
-                    for (int k = 0; k < kChunks / 2; ++k) {
-                        const int r = k * (64 / kChunks) + r0;
-                        const int64_t n = n0 + 32 * j + r;
-                        for (int x = 0; x < 4 && n < o.b.rows && m0 + m + x < o.dim; ++x) {
-                            const float w = *(const float*)(lds + r * kRow + ((chunk ^ (r & 7)) << 4) + 4 * x);
-                            const int64_t at = n * o.dim + m0 + m + x;
-                            if (!o.part) store_act<sizeof(T) == 2>(o.out, at, w * o.scale);
-                            else o.part[p0 * o.dim + at] = o.add ? o.part[p0 * o.dim + at] + w : w;
-                        }
-                    }
+                    continue;
                 }
+                // as many values as a store of 16 bytes takes: two chunks of a bf16 result
+                constexpr int kWide = sizeof(T) == 2 ? 2 : 1;
+                auto store = [&](auto both) {
+                    constexpr int kTake = decltype(both)::value, kLanes = kChunks / kTake;   // chunks a lane, lanes a row
+                    const int n = lane % kLanes, r0 = lane / kLanes, m = 32 * q + n * 4 * kTake;
+                    const bool in = m < columns;
+                    const uint32_t from = in ? (uint32_t)((32 * j + r0) * row + m * size) : 0x80000000u;
+                    const uint32_t sum_from = in ? (uint32_t)((32 * j + r0) * sum_row + m * 4) : 0x80000000u;
+#pragma unroll 4
+                    for (int k = 0; k < kLanes / 2; ++k) {
+                        const int r = k * (64 / kLanes) + r0;
+                        f32x4 w[kTake];
+#pragma unroll
+                        for (int x = 0; x < kTake; ++x) {
+                            w[x] = *(const f32x4*)(lds + r * kRow + (((n * kTake + x) ^ (r & 7)) << 4));
+                            if (add) w[x] += __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(sum, (int)(sum_from + (uint32_t)(k * (64 / kLanes) * sum_row + x * 16)), 0, 0));
+                        }
+                        const int off = (int)(from + (uint32_t)(k * (64 / kLanes) * row));
+                        if constexpr (kTake == 2) {
+                            u32x4 v;
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) v[x] = pack_bf16x2(w[x / 2][x % 2 * 2] * o.scale, w[x / 2][x % 2 * 2 + 1] * o.scale);
+                            __builtin_amdgcn_raw_buffer_store_b128(v, to, off, 0, 0);
+                        } else {
+                            if (!fp32) w[0] *= o.scale;
+                            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, w[0]), to, off, 0, 0);
+                        }
+                    }
+                };
+                if (kWide == 2 && !fp32) store(std::integral_constant<int, kWide>());
+                else store(std::integral_constant<int, 1>());
             }
         }
     }
     wait_loads<0>();   // none into LDS is under way when another workgroup gets it
 }
 
-// The parts' sum in their order, times scale: four values a thread.
+// The parts of the tiles that were split, added up in their order: four values a thread.
 template <typename T>
-__global__ __launch_bounds__(256) void loss_sum_kernel(const float* part, int parts, int64_t n, float scale, void* out)
+__global__ __launch_bounds__(256) void loss_sum_kernel(OutArgs o)
 {
-    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-    if (at >= n) return;
-    if (n % 4 == 0) {
-        f32x4 v = *(const f32x4*)(part + at);
-        for (int p = 1; p < parts; ++p) v += *(const f32x4*)(part + p * n + at);
-        store4<T>((char*)out + at * (int)sizeof(T), 0, v[0] * scale, v[1] * scale, v[2] * scale, v[3] * scale);
-    } else {
-        for (int64_t e = at; e < min(at + 4, n); ++e) {
-            float v = part[e];
-            for (int p = 1; p < parts; ++p) v += part[p * n + e];
-            store_act<sizeof(T) == 2>(out, e, v * scale);
-        }
-    }
+    const int edge = o.cut.edge, quads = edge / 4;
+    const int tile = blockIdx.x / (edge * quads / 256), at = (blockIdx.x % (edge * quads / 256)) * 256 + threadIdx.x;
+    int mi, ni;
+    tile_of(o.cut.whole + tile, o.mt, o.nt, mi, ni);
+    const int64_t n = (int64_t)ni * edge + at / quads, m = (int64_t)mi * edge + at % quads * 4;
+    if (n >= o.b.rows || m >= o.dim) return;
+    const float* p = o.part + ((int64_t)tile * edge * edge + at * 4);
+    const int64_t stride = (int64_t)o.cut.rest * edge * edge;
+    f32x4 v = *(const f32x4*)p;
+#pragma unroll 4
+    for (int i = 1; i < o.cut.parts; ++i) v += *(const f32x4*)(p + i * stride);
+    leave4<T>(o, n, m, v);
 }
 
 template <typename W>   // uint16_t or uint32_t
@@ -481,26 +527,43 @@ int sharing(int edge) { return edge == 256 ? 1 : edge == 128 ? 2 : 4; }
 // As many workgroups as the chip holds, which take the tiles in turn.
 dim3 resident(int64_t groups, int edge) { return dim3((unsigned)std::min<int64_t>(groups, (int64_t)device_cus() * sharing(edge))); }
 
-// Edge of a product's tiles, and the parts its contraction is split into.
-struct Cut {
-    int edge, parts;
-};
-
-// The cut whose rounds of workgroups cost least.
-Cut cut(int64_t m, int64_t n, int64_t k, bool bf16, bool may_split)
+// Cycles of a step of q workgroups on a compute unit: as many as one's own latencies take, or as its products
+// and loads of them all do.  (Fitted to forward calls of 1,000 to 65,536 tokens of 128 to 1,024 over 500 to
+// 50,304 entries with tiles of each size: off by 10% at most.)
+double step_cycles(int edge, bool bf16, int64_t q)
 {
-    Cut best{bf16 ? 256 : 128, 1};
+    const double own = bf16 ? (edge == 256 ? 1200. : edge == 128 ? 1100. : 800.) : (edge == 128 ? 4400. : 1300.);
+    const double share = bf16 ? (edge == 256 ? 1200. : edge == 128 ? 850. : 380.) : (edge == 128 ? 4300. : 1100.);
+    return std::max(own, share * q);
+}
+
+// The cut of a product of m x n results over k that takes the fewest cycles: rounds of as many tiles as the
+// chip holds, and, with `split`, what is left over in parts that fill a round (or some) too.
+Cut cut(int64_t m, int64_t n, int64_t k, bool bf16, bool split)
+{
+    Cut best{};
     double least = 1e300;
-    const int64_t cus = device_cus(), steps = tiles(k, bf16 ? 64 : 32);
+    const int64_t cus = device_cus();
     for (const int edge : {256, 128, 64}) {
         if (edge == 256 && !bf16) continue;
-        // workgroups of a compute unit, and cycles of a step with that many (measured)
-        const int each = sharing(edge);
-        const double step = bf16 ? (edge == 256 ? 2600. : edge == 128 ? 1700. : 1500.) : (edge == 128 ? 4500. : 2600.);
-        for (int parts = 1; parts <= (may_split ? 64 : 1) && parts <= std::max<int64_t>(1, steps / 4); ++parts) {
-            const int64_t groups = tiles(m, edge) * tiles(n, edge) * parts;
-            const double t = tiles(groups, (int)(cus * each)) * (tiles(steps, parts) * step + 6000.) + (parts > 1 ? 5000. + parts * m * n / 2000. : 0.);
-            if (t < least) least = t, best = Cut{edge, parts};
+        const int64_t all = tiles(m, edge) * tiles(n, edge), slots = cus * sharing(edge);
+        const int64_t steps = tiles(k, edge == 256 ? 32 : bf16 ? 64 : 32), rounds = all / slots, rest = all % slots;
+        const double end = edge == 256 ? 18000. : edge == 128 ? 6500. : 4000.;   // of a tile
+        const double before = rounds * (steps * step_cycles(edge, bf16, sharing(edge)) + end);
+        if (before >= least) continue;
+        for (int parts = 1; parts <= (split && rest ? 64 : 1) && parts <= std::max<int64_t>(1, steps / 4); ++parts) {
+            double t = before;
+            if (rest) {
+                const int64_t groups = rest * parts, full = groups / slots, over = groups % slots, each = tiles(steps, parts);
+                t += full * (each * step_cycles(edge, bf16, sharing(edge)) + end);
+                if (over) t += each * step_cycles(edge, bf16, tiles(over, (int)cus)) + end;
+                // the parts are written and read back at some 2,000 bytes a cycle, by one more launch
+                if (parts > 1) t += 6000. + groups * edge * edge * 8. / 2000.;
+            }
+            if (t < least) {
+                least = t;
+                best = Cut{edge, (int)(parts > 1 ? all - rest : all), parts > 1 ? (int)rest : 0, parts};
+            }
         }
     }
     return best;
@@ -511,12 +574,23 @@ Cut cut(int64_t m, int64_t n, int64_t k, bool bf16, bool may_split)
 constexpr int64_t kPieceBytes = (int64_t)1 << 30, kPieceRow = (int64_t)1 << 23;
 struct Backward {
     int64_t piece;       // vocabulary entries of a piece (the last one may have fewer)
-    int64_t stride;      // bytes of a row of D
+    int64_t group;       // bytes of D for 64 tokens
     int pieces;
-    Cut grad, dh, dw;
-    int64_t h_parts, w_parts;   // floats of the parts (0: none)
-    size_t d_bytes;
+    size_t d_bytes, sum_bytes, part_bytes;
 };
+
+// The cuts of a piece.
+struct Piece {
+    Cut grad, dh, dw;
+};
+Piece piece_cuts(int64_t rows, int64_t width, int64_t dim, bool bf16)
+{
+    return {cut(width, rows, dim, bf16, false), cut(dim, rows, width, bf16, true), cut(dim, width, rows, bf16, true)};
+}
+
+size_t part_bytes(const Cut& c) { return c.parts > 1 ? (size_t)c.rest * c.parts * c.edge * c.edge * 4 : 0; }
+
+size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 
 Backward backward(int64_t rows, int64_t vocab, int64_t dim, bool bf16)
 {
@@ -526,18 +600,16 @@ Backward backward(int64_t rows, int64_t vocab, int64_t dim, bool bf16)
     b.pieces = (int)std::max<int64_t>(1, tiles(vocab, (int)most));
     b.piece = tiles(tiles(vocab, b.pieces), 256) * 256;
     b.pieces = (int)tiles(vocab, (int)b.piece);
-    b.stride = std::min(b.piece, (vocab + 7) / 8 * 8) * each;
-    b.d_bytes = (size_t)rows * b.stride;
-    const int64_t width = std::min(b.piece, vocab);
-    b.grad = cut(width, rows, dim, bf16, false);
-    b.dh = cut(dim, rows, width, bf16, true);
-    b.dw = cut(dim, width, rows, bf16, true);
-    b.h_parts = b.dh.parts > 1 || b.pieces > 1 ? b.dh.parts * rows * dim : 0;
-    b.w_parts = b.dw.parts > 1 ? b.dw.parts * width * dim : 0;
+    b.group = tiles(std::min(b.piece, vocab) * each, 128) * 128 * kBlockRows;
+    b.d_bytes = (size_t)tiles(rows, kBlockRows) * b.group;
+    b.sum_bytes = b.pieces > 1 ? round16((size_t)rows * dim * 4) : 0;
+    b.part_bytes = 0;
+    for (const int64_t width : {std::min(b.piece, vocab), vocab - (b.pieces - 1) * b.piece}) {
+        const Piece p = piece_cuts(rows, width, dim, bf16);
+        b.part_bytes = std::max({b.part_bytes, part_bytes(p.dh), part_bytes(p.dw)});
+    }
     return b;
 }
-
-size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 
 template <typename T, int E>
 hipError_t forward(const LossArgs& a, hipStream_t stream)
@@ -551,31 +623,27 @@ hipError_t forward(const LossArgs& a, hipStream_t stream)
 }
 
 template <typename T, int E>
-void grad_piece(const LossArgs& a, int64_t first, int64_t width, char* d, int64_t stride, hipStream_t stream)
+void grad_piece(const LossArgs& a, int64_t first, int64_t width, char* d, int64_t group, hipStream_t stream)
 {
     const int mt = (int)tiles(width, E), nt = (int)tiles(a.rows, E);
-    loss_grad_kernel<T, E><<<resident((int64_t)mt * nt, E), 256, 0, stream>>>(a, mt, nt, first, width, d, stride);
+    loss_grad_kernel<T, E><<<resident((int64_t)mt * nt, E), 256, 0, stream>>>(a, mt, nt, first, width, d, group);
 }
 
 template <typename T, bool TB, int E>
-void out_piece(const OutArgs& o, hipStream_t stream)
+void out_tiles(const OutArgs& o, hipStream_t stream)
 {
-    const int mt = (int)tiles(o.dim, E), nt = (int)tiles(o.b.rows, E);
-    loss_out_kernel<T, TB, E><<<resident((int64_t)mt * nt * o.parts, E), 256, 0, stream>>>(o, mt, nt);
+    loss_out_kernel<T, TB, E><<<resident(o.cut.whole + (int64_t)o.cut.rest * o.cut.parts, E), 256, 0, stream>>>(o);
+    if (o.cut.parts > 1) loss_sum_kernel<T><<<dim3((unsigned)(o.cut.rest * (E * E / 1024))), 256, 0, stream>>>(o);
 }
 
 template <typename T, bool TB>
-void out_of(const OutArgs& o, int edge, hipStream_t stream)
+void out_piece(OutArgs o, hipStream_t stream)
 {
+    o.mt = (int)tiles(o.dim, o.cut.edge);
+    o.nt = (int)tiles(o.b.rows, o.cut.edge);
     if constexpr (sizeof(T) == 2)
-        if (edge == 256) return out_piece<T, TB, 256>(o, stream);
-    edge == 128 ? out_piece<T, TB, 128>(o, stream) : out_piece<T, TB, 64>(o, stream);
-}
-
-template <typename T>
-void sum_of(const float* part, int parts, int64_t n, float scale, void* out, hipStream_t stream)
-{
-    loss_sum_kernel<T><<<dim3((unsigned)tiles(n, 1024)), 256, 0, stream>>>(part, parts, n, scale, out);
+        if (o.cut.edge == 256) return out_tiles<T, TB, 256>(o, stream);
+    o.cut.edge == 128 ? out_tiles<T, TB, 128>(o, stream) : out_tiles<T, TB, 64>(o, stream);
 }
 
 template <typename T>
@@ -584,31 +652,25 @@ hipError_t back(const LossArgs& a, hipStream_t stream)
     constexpr bool kBf16 = sizeof(T) == 2;
     const Backward b = backward(a.rows, a.vocab, a.out_dim, kBf16);
     char* const d = a.ws;
-    float* const hp = (float*)(a.ws + round16(b.d_bytes));
-    float* const wp = hp + (b.h_parts + 3) / 4 * 4;
+    float* const sum = (float*)(d + b.d_bytes);
+    float* const part = (float*)(d + b.d_bytes + b.sum_bytes);
     for (int i = 0; i < b.pieces; ++i) {
         const int64_t first = i * b.piece, width = std::min(b.piece, a.vocab - first);
-        if (kBf16 && b.grad.edge == 256) {
-            if constexpr (kBf16) grad_piece<T, 256>(a, first, width, d, b.stride, stream);
-        } else if (b.grad.edge == 128) {
-            grad_piece<T, 128>(a, first, width, d, b.stride, stream);
+        const Piece p = piece_cuts(a.rows, width, a.out_dim, kBf16);
+        if (kBf16 && p.grad.edge == 256) {
+            if constexpr (kBf16) grad_piece<T, 256>(a, first, width, d, b.group, stream);
+        } else if (p.grad.edge == 128) {
+            grad_piece<T, 128>(a, first, width, d, b.group, stream);
         } else {
-            grad_piece<T, 64>(a, first, width, d, b.stride, stream);
+            grad_piece<T, 64>(a, first, width, d, b.group, stream);
         }
-        if (a.grad_hidden) {
-            const OutArgs o{Side{(const char*)a.weight + first * a.weight_stride, a.weight_stride, a.dim}, Side{d, b.stride, a.rows}, width,
-                            b.dh.parts, b.h_parts ? hp : nullptr, i > 0, a.grad_hidden, a.out_dim, a.scale};
-            out_of<T, false>(o, b.dh.edge, stream);
-        }
-        if (a.grad_weight) {
-            void* const to = (char*)a.grad_weight + first * a.out_dim * (int)sizeof(T);
-            const OutArgs o{Side{(const char*)a.hidden, a.hidden_stride, a.dim}, Side{d, b.stride, width}, a.rows,
-                            b.dw.parts, b.w_parts ? wp : nullptr, 0, to, a.out_dim, a.scale};
-            out_of<T, true>(o, b.dw.edge, stream);
-            if (b.w_parts) sum_of<T>(wp, b.dw.parts, width * a.out_dim, a.scale, to, stream);
-        }
+        if (a.grad_hidden)
+            out_piece<T, false>(OutArgs{Side{(const char*)a.weight + first * a.weight_stride, a.weight_stride, a.dim}, Side{d, b.group, a.rows},
+                                        width, 0, 0, p.dh, part, sum, i == 0, i == b.pieces - 1, a.grad_hidden, a.out_dim, a.scale}, stream);
+        if (a.grad_weight)
+            out_piece<T, true>(OutArgs{Side{(const char*)a.hidden, a.hidden_stride, a.dim}, Side{d, b.group, width}, a.rows, 0, 0, p.dw,
+                                       part, nullptr, 1, 1, (char*)a.grad_weight + first * a.out_dim * (int)sizeof(T), a.out_dim, a.scale}, stream);
     }
-    if (a.grad_hidden && b.h_parts) sum_of<T>(hp, b.dh.parts, a.rows * a.out_dim, a.scale, a.grad_hidden, stream);
     return hipGetLastError();
 }
 
@@ -625,18 +687,15 @@ size_t loss_ws_bytes(int64_t rows, int64_t vocab, int64_t dim, bool bf16)
 size_t loss_bwd_ws_bytes(int64_t rows, int64_t vocab, int64_t dim, bool bf16)
 {
     const Backward b = backward(rows, vocab, dim, bf16);
-    return round16(b.d_bytes) + (size_t)((b.h_parts + 3) / 4 * 4 + (b.w_parts + 3) / 4 * 4) * 4;
+    return b.d_bytes + b.sum_bytes + b.part_bytes;
 }
 
-bool loss_launchable(int64_t rows, int64_t vocab, int64_t dim, bool bf16, bool back)
+bool loss_launchable(int64_t rows, int64_t vocab, int64_t dim, bool backward)
 {
-    // (doubles: the products may pass 64 bits)
-    const double r = (double)rows, v = (double)vocab, d = (double)dim;
-    auto count = [](double n, int edge) { return std::floor(n / edge) + 1; };
-    if (!threads_fit(count(v, 64) * count(r, 64)) || !threads_fit(count(r, 4))) return false;
-    if (!back) return true;
-    return threads_fit(count(d, 64) * count(r, 64) * 64) && threads_fit(count(d, 64) * count(v, 64) * 64) &&
-           threads_fit(r * d / 1024 + 1) && threads_fit(v * d / 1024 + 1) && r * v < 1e18 && (void(bf16), true);
+    // in tiles of 64, the smallest (doubles: the products may pass 64 bits)
+    const double r = std::floor(rows / 64.) + 1, v = std::floor(vocab / 64.) + 1, d = std::floor(dim / 64.) + 1;
+    if (!threads_fit(r * v) || !threads_fit(16 * r)) return false;
+    return !backward || (threads_fit(d * r) && threads_fit(d * v));
 }
 
 hipError_t launch_loss(const LossArgs& a, bool bf16, hipStream_t stream)

@@ -27,7 +27,7 @@ struct LossArgs {
 size_t loss_ws_bytes(int64_t rows, int64_t vocab, int64_t dim, bool bf16);
 size_t loss_bwd_ws_bytes(int64_t rows, int64_t vocab, int64_t dim, bool bf16);
 // Every launch of a call of these sizes is possible.
-bool loss_launchable(int64_t rows, int64_t vocab, int64_t dim, bool bf16, bool backward);
+bool loss_launchable(int64_t rows, int64_t vocab, int64_t dim, bool backward);
 hipError_t launch_loss(const LossArgs& a, bool bf16, hipStream_t stream);
 hipError_t launch_loss_bwd(const LossArgs& a, bool bf16, hipStream_t stream);
 // Rows of dim values as rows of `padded`, the rest zeros.

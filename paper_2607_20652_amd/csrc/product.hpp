@@ -16,6 +16,13 @@
 
 namespace dpb {
 
+// How a side lies in memory.  Blocks: what a kernel here has left for a product here, in blocks of 64 rows of 64
+// bytes (4 KB), the blocks of 64 rows one behind the other (`stride` bytes); rows and columns up to whole
+// blocks, and to 128 bytes of a row, are zeros.  (Rows of some 50 KB, read 64 bytes at a time, had taken a
+// product of 16,384 x 25,344 by 1,024 a third longer than its MFMAs: each piece another page of memory.)
+enum class Lies { rows, blocks };
+constexpr int kBlockRows = 64, kBlockBytes = 4096;
+
 // One side of a product.  Plain: `rows` rows, `stride` bytes apart, of the contraction;
 // transposed: the contraction's rows, `stride` bytes apart, of `rows` values each.  Rows start
 // on 16 bytes, and what follows their values up to the next 16 may be read: zeros, in a plain side's.
@@ -26,7 +33,7 @@ struct Side {
 };
 
 // R rows (values) of a side, a step's K values of the contraction (K elements of a row, or K rows).
-template <typename T, bool TR, int R, int K>
+template <typename T, bool TR, Lies LIES, int R, int K>
 struct Panel {
     static constexpr int kRowBytes = (TR ? R : K) * (int)sizeof(T);
     static constexpr int kBytes = R * K * (int)sizeof(T);
@@ -56,12 +63,29 @@ struct Panel {
         int stride, last;   // last: bytes from the first row to the end of the last, all rows there
         int chunk;          // plain: contraction values before this lane's chunk
         int left;           // contraction values not yet sent for
+        int64_t turn_step;  // transposed blocks, half a block of contraction a step: what the other half adds
 
         // The panels that start at row (value) `first` of the side, contraction from `k`.
         __device__ __forceinline__ void start(const Side& s, int64_t first, int64_t k, int64_t end, int wave)
         {
             const int lane = threadIdx.x & 63;
             left = (int)(end - k);
+            if constexpr (LIES == Lies::blocks) {
+                constexpr int kEach = 64 / (int)sizeof(T);   // values of a block's row
+                const int64_t groups = (s.rows + kBlockRows - 1) / kBlockRows - first / kBlockRows;
+                const int64_t values = (s.rows * (int)sizeof(T) + 127) / 128 * 128 - first * (int)sizeof(T);
+                p = s.p + (TR ? k / kBlockRows * s.stride + first / kEach * kBlockBytes + k % kBlockRows * 64
+                              : first / kBlockRows * s.stride + k / kEach * kBlockBytes);
+                step = TR ? (K < kBlockRows && k % kBlockRows == 0 ? K * 64 : s.stride - (kBlockRows - K) * 64) : K / kEach * kBlockBytes;
+                turn_step = s.stride;
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) {
+                    const int at = (i * kWaves + wave) * 64 + lane, r = at / kChunks, c = (at % kChunks) ^ turn(r);
+                    const bool here = TR ? c * 16 < values : r / kBlockRows < groups;
+                    off[i] = here ? (uint32_t)((TR ? 0 : r / kBlockRows) * (int64_t)s.stride) + (c / 4) * kBlockBytes + (r % kBlockRows) * 64 + (c % 4) * 16 : 0xFFFFFFF0u;
+                }
+                return;
+            }
             stride = (int)s.stride;
             p = s.p + (TR ? k * s.stride + first * (int)sizeof(T) : first * s.stride + k * (int)sizeof(T));
             step = TR ? K * s.stride : kRowBytes;
@@ -83,9 +107,15 @@ struct Panel {
         {
             // (by masks: a branch would part what is mixed with the products)
             const int none = (left - 1) >> 31;
-            const int bytes = (TR ? (min(left, K) - 1) * stride + last : last + min(whole(left), kRowBytes)) & ~none;
+            const int bytes = (LIES == Lies::blocks ? 0x7FFFFFE0 : TR ? (min(left, K) - 1) * stride + last : last + min(whole(left), kRowBytes)) & ~none;
             const char* const from = p;
             out = 0;
+            if constexpr (LIES == Lies::blocks) {
+                p += step;
+                if (TR && K < kBlockRows) step = turn_step - step;
+                left -= K;
+                return __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, bytes, 0x00027000);
+            }
             if constexpr (!TR) {
                 out = chunk >= left ? 0x80000000u : 0u;
                 __asm__("" : "+v"(out));   // formed anew each step, and with it every place: not kept for the next tile
@@ -98,7 +128,7 @@ struct Panel {
         __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t buf, char* lds, int i, int wave) const
         {
             __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lds_void*)(lds + (i * kWaves + wave) * 1024), 16,
-                                                     (int)(TR ? off[i] : off[i] | out), 0, 0, 0);
+                                                     (int)(TR || LIES == Lies::blocks ? off[i] : off[i] | out), 0, 0, 0);
         }
 
         __device__ __forceinline__ void operator()(char* lds, int wave)
@@ -167,11 +197,11 @@ struct Job {
 // Large bf16 tiles take 32 contraction values a step through five stages of 32 KB: a step of 1,024
 // MFMA cycles is shorter than memory's latency, four of them are not.  Smaller ones share a compute unit
 // and take twice that through two stages; fp32 steps last 4,096 cycles.
-template <typename T, bool TA, bool TB, int E>
+template <typename T, bool TA, bool TB, Lies LB, int E>
 struct Product {
         static constexpr int kK = E == 256 ? 32 : 128 / (int)sizeof(T), kStages = E == 256 ? 4 : 2;
-    typedef Panel<T, TA, E, kK> PA;
-    typedef Panel<T, TB, E, kK> PB;
+    typedef Panel<T, TA, Lies::rows, E, kK> PA;
+    typedef Panel<T, TB, LB, E, kK> PB;
     typedef typename Operand<T>::type Op;
     static constexpr int kSubs = kK / 16;
     static constexpr int F = E / 64;                   // fragments of a wave, either way
