@@ -727,18 +727,27 @@ def _place(t: torch.Tensor | None, name: str, device: int) -> int | None:
 
 
 def _whole(t: torch.Tensor | None, name: str, device: int) -> int | None:
-    return None if t is None else _dev(t, name, device).value
+    """Address of a contiguous tensor on this device (_dev without its ctypes object: these calls are short)."""
+    if t is None:
+        return None
+    if t.get_device() != device:
+        _elsewhere(t, name, device)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
 
 
 def _rows(t: torch.Tensor, name: str):
     """(rows, stride between them) of [..., dim] as rows of dim elements, contiguous each."""
-    shape, st = t.shape, t.stride()
+    shape = t.shape
     if len(shape) == 0:
         raise ValueError(f"{name} has no rows")
+    if t.is_contiguous():
+        dim = shape[-1]
+        return t.numel() // dim if dim else 0, dim
+    st = t.stride()
     if shape[-1] > 1 and st[-1] != 1:
         raise ValueError(f"{name} must be contiguous along its last dimension")
-    if t.is_contiguous():
-        return t.numel() // shape[-1] if shape[-1] else 0, shape[-1]
     # the other dimensions have to be one, in the order of memory
     n, stride = 1, shape[-1]
     for size, step in zip(reversed(shape[:-1]), reversed(st[:-1])):
@@ -754,9 +763,10 @@ def _rows(t: torch.Tensor, name: str):
 
 def _integers(t: torch.Tensor, name: str, device: int):
     """(address, bits) of a contiguous tensor of tokens."""
-    if t.dtype not in (torch.int64, torch.int32):
-        raise TypeError(f"{name}: int64 or int32, not {t.dtype}")
-    return _dev(t, name, device).value, 64 if t.dtype == torch.int64 else 32
+    dtype = t.dtype
+    if dtype != torch.int64 and dtype != torch.int32:
+        raise TypeError(f"{name}: int64 or int32, not {dtype}")
+    return _whole(t, name, device), 64 if dtype == torch.int64 else 32
 
 
 def _space(workspace: torch.Tensor | None, need: int, like: torch.Tensor):
@@ -829,15 +839,17 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor | None, residual: torch.Tenso
     _need(residual is None or (residual.shape == shape and residual.dtype == x.dtype))
     _need(weight is None or weight.shape == (dim,))
     _need(residual is not None or total is None, "without a residual the sum is x")
-    given = [out, total, rstd]
-    if out is None:
-        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+    given = None if out is None and total is None and rstd is None else [out, total, rstd]
+    if given is not None:
+        _need(out is None or (out.shape == shape and out.dtype == x.dtype))
+        _need(total is None or (total.shape == shape and total.dtype == x.dtype))
+        _need(rstd is None or (rstd.shape == shape[:-1] and rstd.dtype == torch.float32))
+    if out is None:   # (empty_like without a format is the quickest where it gives the same)
+        out = torch.empty_like(x) if x.is_contiguous() else x.new_empty(shape)
     if residual is not None and total is None:
-        total = torch.empty_like(x, memory_format=torch.contiguous_format)
+        total = torch.empty_like(out)
     if rstd is None:
-        rstd = x.new_empty(shape[:-1], dtype=torch.float32)
-    _need(out.shape == shape and out.dtype == x.dtype and rstd.shape == shape[:-1] and rstd.dtype == torch.float32)
-    _need(total is None or (total.shape == shape and total.dtype == x.dtype))
+        rstd = torch.empty(shape[:-1], dtype=torch.float32, device=x.device)
     device, here = _device_of(x, "x")
     with here:
         n, stride = _rows(x, "x")
@@ -846,7 +858,7 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor | None, residual: torch.Tenso
             _dtype_code(x), x.data_ptr(), stride, _place(residual, "residual", device), r_stride,
             _whole(weight, "weight", device), DPB_F32 if weight is None else _dtype_code(weight), n, dim, eps,
             _whole(out, "out", device), _whole(total, "total", device), _whole(rstd, "rstd", device), _stream(x)))
-    if any(t is not None for t in given):
+    if given is not None:
         _written(given)
     return out, x if residual is None else total, rstd
 

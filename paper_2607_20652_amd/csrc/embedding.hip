@@ -3,9 +3,9 @@
 // The gradient is a sum over the tokens that name a row.  Tokens are sorted by row, each row's
 // in their own order, so that the same inputs give the same bits:
 //   1. bin: a workgroup puts 1,024 tokens in order of bucket (2^shift rows of the table, at
-//      most 1,024 buckets), with the start of each bucket;
-//   2. order: a workgroup gathers a bucket from all of those, in their order, counts its rows
-//      and places each token behind those before it;
+//      most 1,024 buckets), with the start of each bucket (not of up to 16,384 tokens);
+//   2. order: a workgroup gathers a bucket from all of those, or from the tokens themselves, in their
+//      order, counts its rows and places each token behind those before it;
 //   3. sum: a wave adds up a row of up to 64 tokens, zeros if there are none; 64 places of the sorted
 //      order that hold a longer row, padding or a frequent word, leave that row's part of them;
 //   4. join: the parts of a long row are added up in order.
@@ -20,7 +20,10 @@ namespace {
 
 constexpr int kBin = 1024;          // tokens a workgroup bins
 constexpr int kBuckets = 1024;      // most
-constexpr int kRowsAtOnce = 2048;   // rows of a bucket that are ordered together
+constexpr int kScan = 16384;        // tokens, at most, that every workgroup reads for itself
+constexpr int kScanBuckets = 512;   // most then
+constexpr int kRowsAtOnce = 1024;   // rows of a bucket that are ordered together
+constexpr int kOrderWaves = 8;      // of the workgroup that does
 constexpr int kLong = 64;           // tokens of a row that a wave adds up
 
 __device__ __forceinline__ int64_t token_at(const EmbedArgs& a, int64_t t)
@@ -75,10 +78,11 @@ __device__ __forceinline__ uint64_t same_key(uint32_t key, int bits, bool live)
     return m;
 }
 
-// Exclusive prefix sum over the workgroup's 256 threads; the total in all.
-__device__ __forceinline__ uint32_t prefix256(uint32_t v, uint32_t& total)
+// Exclusive prefix sum over the workgroup's threads; the total in all.
+template <int WAVES>
+__device__ __forceinline__ uint32_t prefix(uint32_t v, uint32_t& total)
 {
-    __shared__ uint32_t lds[4];
+    __shared__ uint32_t lds[WAVES];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint32_t s = v;
 #pragma unroll
@@ -92,7 +96,7 @@ __device__ __forceinline__ uint32_t prefix256(uint32_t v, uint32_t& total)
     uint32_t before = 0;
     total = 0;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
         if (w < wave) before += lds[w];
         total += lds[w];
     }
@@ -131,7 +135,7 @@ __global__ __launch_bounds__(256) void embed_bin_kernel(EmbedArgs a, Sorted s)
         for (int w = 0; w < 4; ++w) n[i] += count[w][threadIdx.x * 4 + i];
         sum += n[i];
     }
-    uint32_t at = prefix256(sum, total);
+    uint32_t at = prefix<4>(sum, total);
     uint32_t* const starts = s.starts + (int64_t)blockIdx.x * (s.buckets + 1);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -155,7 +159,7 @@ __global__ __launch_bounds__(256) void embed_bin_kernel(EmbedArgs a, Sorted s)
 }
 
 // Calls f(entry, valid) for a bucket's entries in bins [from, to), 64 at a time in order, all lanes
-// of the wave together.
+// of the wave together; the next 64 are under way meanwhile.
 template <typename F>
 __device__ __forceinline__ void each_entry(const Sorted& s, int bucket, int64_t from, int64_t to, F&& f)
 {
@@ -173,62 +177,117 @@ __device__ __forceinline__ void each_entry(const Sorted& s, int bucket, int64_t 
             const uint32_t o = __shfl_up(end, off, 64);
             if (lane >= off) end += o;
         }
-        const uint32_t total = __shfl(end, 63, 64);
-        for (uint32_t i = 0; i < total; i += 64) {
-            // the lane whose bin holds entry i + lane: the first whose end is behind it
-            const uint32_t want = i + lane;
+        const uint32_t total = __builtin_amdgcn_readlane(end, 63);
+        const int bins = (int)min(to - j, (int64_t)64);
+        if (total >= 32u * bins) {
+            // many in each bin: one bin after the other, without the search
+            for (int b = 0; b < bins; ++b) {
+                const uint32_t here = __builtin_amdgcn_readlane(n, b);
+                const uint2* const p = s.binned + (j + b) * kBin + __builtin_amdgcn_readlane(first, b);
+                uint2 next = (uint32_t)lane < here ? p[lane] : make_uint2(0, 0);
+                for (uint32_t i = 0; i < here; i += 64) {
+                    const uint2 x = next;
+                    if (i + 64 + lane < here) next = p[i + 64 + lane];
+                    f(x, i + lane < here);
+                }
+            }
+            continue;
+        }
+        auto fetch = [&](uint32_t want) {
+            // the lane whose bin holds the entry: the first whose end is behind it
             int at = 0;
 #pragma unroll
             for (int step = 32; step > 0; step >>= 1)
                 if (__shfl(end, at + step - 1, 64) <= want) at += step;
             at = min(at, 63);
             const uint32_t e = __shfl(end, at, 64), c = __shfl(n, at, 64), o = __shfl(first, at, 64);
-            const bool valid = want < total;
-            uint2 x = make_uint2(0, 0);
-            if (valid) x = s.binned[(j + at) * kBin + o + (want - (e - c))];
-            f(x, valid);
+            return want < total ? s.binned[(j + at) * kBin + o + (want - (e - c))] : make_uint2(0, 0);
+        };
+        uint2 next = fetch(lane);
+        for (uint32_t i = 0; i < total; i += 64) {
+            const uint2 x = next;
+            if (i + 64 < total) next = fetch(i + 64 + lane);
+            f(x, i + lane < total);
         }
     }
 }
 
-__global__ __launch_bounds__(256) void embed_order_kernel(EmbedArgs a, Sorted s)
+// A bucket's tokens by row: counted, then placed.  Out of its bins, or (SCAN) out of all tokens, which eight waves of
+// every workgroup read and keep in registers; they bound the count of tokens that this is done for.
+// Bound by latency: 16,384 tokens, as frequent as words are, over 50,304 rows take 6.2 us to bin and 17.4 to order
+// (a third is one bucket's; 39 with four waves that search their bins entry by entry), by scanning 20.6 in one launch;
+// evenly over 1,024 rows the two and the sum take 28.6 us, by scanning 24.2.
+template <bool SCAN>
+__global__ __launch_bounds__(64 * kOrderWaves) void embed_order_kernel(EmbedArgs a, Sorted s)
 {
-    __shared__ uint32_t count[4][kRowsAtOnce];
+    constexpr int kThreads = 64 * kOrderWaves, kEach = kRowsAtOnce / kThreads;   // rows a thread
+    __shared__ uint32_t count[kOrderWaves][kRowsAtOnce];
     const int bucket = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint64_t below = (1ull << lane) - 1;
-    // places before the bucket: what each bin has before it
-    uint32_t before = 0, mine = 0;
-    for (int64_t j = threadIdx.x; j < s.bins; j += 256) {
-        const uint32_t* p = s.starts + j * (s.buckets + 1) + bucket;
-        before += p[0];
-        mine += p[1] - p[0];
-    }
-    uint32_t base, size;
-    (void)prefix256(before, base);
-    (void)prefix256(mine, size);
-    const int64_t from = s.bins * wave / 4, to = s.bins * (wave + 1) / 4;
     const int64_t row0 = (int64_t)bucket << s.shift, rows = min((int64_t)1 << s.shift, a.vocab - row0);
-    const int bits = min(s.shift, 11);
+    // this wave's bins, or tokens (whole rounds of them)
+    const int64_t all = SCAN ? (a.count + 63) / 64 : s.bins, unit = SCAN ? 64 : 1;
+    const int64_t from = all * wave / kOrderWaves * unit, to = all * (wave + 1) / kOrderWaves * unit;
+    // (tokens: all of a lane's are read at once, and kept)
+    constexpr int kHeld = SCAN ? kScan / kThreads : 1;
+    uint32_t held[kHeld];
+    if constexpr (SCAN) {
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) {
+            const int64_t t = from + 64 * k + lane;
+            const int64_t v = t < min(to, a.count) ? token_at(a, t) : -1;
+            held[k] = v >= 0 && v < a.vocab ? (uint32_t)v : ~0u;
+        }
+    }
+    auto each = [&](auto&& f) {
+        if constexpr (SCAN) {
+#pragma unroll
+            for (int k = 0; k < kHeld; ++k) f(make_uint2(held[k], (uint32_t)(from + 64 * k + lane)), held[k] != ~0u);
+        } else {
+            each_entry(s, bucket, from, to, f);
+        }
+    };
+    uint32_t base = 0, size = 1;
+    if constexpr (!SCAN) {
+        // places before the bucket: what each bin has before it
+        uint32_t before = 0, mine = 0;
+        for (int64_t j = threadIdx.x; j < s.bins; j += kThreads) {
+            const uint32_t* p = s.starts + j * (s.buckets + 1) + bucket;
+            before += p[0];
+            mine += p[1] - p[0];
+        }
+        (void)prefix<kOrderWaves>(before, base);
+        (void)prefix<kOrderWaves>(mine, size);
+    }
     for (int64_t r0 = 0; r0 < rows; r0 += kRowsAtOnce) {
         const int here = (int)min((int64_t)kRowsAtOnce, rows - r0);
         const uint32_t low = (uint32_t)(row0 + r0);
+        if (size == 0) {   // a bucket that no token names
+            for (int i = threadIdx.x; i < here; i += kThreads) s.first[low + i] = base;
+            continue;
+        }
         __syncthreads();
-        for (int i = threadIdx.x; i < here * 4; i += 256) count[i / here][i % here] = 0;
+        for (int i = threadIdx.x; i < here; i += kThreads)
+#pragma unroll
+            for (int w = 0; w < kOrderWaves; ++w) count[w][i] = 0;
         __syncthreads();
-        if (size)
-            each_entry(s, bucket, from, to, [&](uint2 x, bool valid) {
-                if (valid && x.x - low < (uint32_t)here) atomicAdd(&count[wave][x.x - low], 1u);
-            });
+        uint32_t before = 0;   // a lane's tokens of earlier rows
+        each([&](uint2 x, bool valid) {
+            if (SCAN && valid && x.x < low) ++before;
+            if (valid && x.x - low < (uint32_t)here) atomicAdd(&count[wave][x.x - low], 1u);
+        });
+        if constexpr (SCAN) (void)prefix<kOrderWaves>(before, base);
         __syncthreads();
-        // eight rows a thread
-        const int first = threadIdx.x * (kRowsAtOnce / 256);
+        const int first = threadIdx.x * kEach;
         uint32_t sum = 0, total;
-        for (int i = first; i < min(first + kRowsAtOnce / 256, here); ++i)
-            for (int w = 0; w < 4; ++w) sum += count[w][i];
-        uint32_t at = base + prefix256(sum, total);
-        for (int i = first; i < min(first + kRowsAtOnce / 256, here); ++i) {
+        for (int i = first; i < min(first + kEach, here); ++i)
+#pragma unroll
+            for (int w = 0; w < kOrderWaves; ++w) sum += count[w][i];
+        uint32_t at = base + prefix<kOrderWaves>(sum, total);
+        for (int i = first; i < min(first + kEach, here); ++i) {
             s.first[low + i] = at;
-            for (int w = 0; w < 4; ++w) {
+#pragma unroll
+            for (int w = 0; w < kOrderWaves; ++w) {
                 const uint32_t c = count[w][i];
                 count[w][i] = at;
                 at += c;
@@ -236,20 +295,21 @@ __global__ __launch_bounds__(256) void embed_order_kernel(EmbedArgs a, Sorted s)
         }
         base += total;
         __syncthreads();
-        if (total)
-            each_entry(s, bucket, from, to, [&](uint2 x, bool valid) {
-                const bool live = valid && x.x - low < (uint32_t)here;
-                const uint32_t r = live ? x.x - low : 0;
-                const uint64_t m = same_key(r, bits, live);
-                const uint32_t place = count[wave][r] + __popcll(m & below);
-                wave_sync();
-                if (live) {
-                    if ((m & below) == 0) count[wave][r] = place + __popcll(m);
-                    s.order[place] = x.y;
-                    s.rows[place] = x.x;
-                }
-                wave_sync();
-            });
+        if (total == 0) continue;
+        each([&](uint2 x, bool valid) {
+            const bool live = valid && x.x - low < (uint32_t)here;
+            if (!__any(live)) return;
+            const uint32_t r = live ? x.x - low : 0;
+            const uint64_t m = same_key(r, min(s.shift, 10), live);
+            const uint32_t place = count[wave][r] + __popcll(m & below);
+            wave_sync();
+            if (live) {
+                if ((m & below) == 0) count[wave][r] = place + __popcll(m);
+                s.order[place] = x.y;
+                s.rows[place] = x.x;
+            }
+            wave_sync();
+        });
     }
     if (bucket == s.buckets - 1 && threadIdx.x == 0) s.first[a.vocab] = base;
 }
@@ -376,10 +436,11 @@ size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 // The layout of the workspace; its size is returned.
 size_t lay_out(int64_t vocab, int dim, int64_t count, char* ws, Sorted* s)
 {
+    const bool scan = count <= kScan;
     s->shift = 0;
-    while ((vocab - 1) >> s->shift >= kBuckets) ++s->shift;
+    while ((vocab - 1) >> s->shift >= (scan ? kScanBuckets : kBuckets)) ++s->shift;
     s->buckets = (int)((vocab - 1) >> s->shift) + 1;
-    s->bins = (count + kBin - 1) / kBin;
+    s->bins = scan ? 0 : (count + kBin - 1) / kBin;
     s->chunks = (count + 63) / 64;
     s->width = (dim + 3) / 4 * 4;
     size_t at = 0;
@@ -423,7 +484,8 @@ hipError_t embed_bwd(const EmbedArgs& a, hipStream_t stream)
     Sorted s;
     lay_out(a.vocab, a.dim, a.count, a.ws, &s);
     if (s.bins) embed_bin_kernel<<<dim3((unsigned)s.bins), 256, 0, stream>>>(a, s);
-    embed_order_kernel<<<dim3((unsigned)s.buckets), 256, 0, stream>>>(a, s);
+    if (s.bins) embed_order_kernel<false><<<dim3((unsigned)s.buckets), 64 * kOrderWaves, 0, stream>>>(a, s);
+    else embed_order_kernel<true><<<dim3((unsigned)s.buckets), 64 * kOrderWaves, 0, stream>>>(a, s);
     if (a.dim % E == 0 && a.stride % 16 == 0 && on16(a.table) && on16(a.out)) embed_sum<T, E>(a, s, stream);
     else embed_sum<T, 1>(a, s, stream);
     const int blocks = (a.dim + 63) / 64;

@@ -38,6 +38,9 @@ CASES = [  # tokens, vocab, dim, kind
     (1, 1, 1, "one"), (5, 3, 7, "all"), (64, 10, 64, "one"), (65, 10, 64, "one"), (816, 9, 40, "edges"), (1023, 50, 72, "all"),
     (1025, 1024, 100, "cycle"), (3000, 50304, 128, "text"), (5000, 777, 1000, "text"), (4097, 2000, 33, "one"),
     (300, 1025, 8, "none"), (2049, 70000, 16, "text"), (20000, 24, 520, "all"), (1000, 3_000_000, 4, "all"),
+    # more than are ordered out of the tokens themselves: binned
+    (16385, 50304, 64, "text"), (17000, 9, 16, "one"), (40000, 2000, 24, "cycle"), (33000, 3_000_000, 4, "text"), (70001, 1025, 8, "all"),
+    (16384, 700, 40, "text"), (20000, 1025, 8, "none"),
 ]
 
 
