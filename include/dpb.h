@@ -533,8 +533,10 @@ dpb_status dpb_adamw_step(const dpb_adamw* settings, int count, void* const* par
  * call (DPB_F32 or DPB_BF16); sums and statistics are fp32.  Everything is
  * deterministic: no atomics on results.  index_bits: 32 or 64, the width of the
  * integers in `tokens` and `targets` (device, contiguous, aligned to their width).
- * Strides are in ELEMENTS between rows, the elements of a row contiguous; dim is any
- * size from 1 on.  An output may not overlap anything else of its call, unless it says so. */
+ * Strides are in ELEMENTS between rows, the elements of a row contiguous (they may be 0, or
+ * rows overlap, in inputs); dim is any size from 1 on (the norm's up to 2^22; what a launch cannot
+ * count is DPB_EUNSUPPORTED).  An output may not overlap anything else of its call, unless it
+ * says so. */
 
 /* EMBEDDING: out[t] = scale * table[tokens[t]] (out contiguous [count, dim]).  A token outside
  * [0, vocab) gives a row of zeros.  Rows of the table start on 16 bytes and are that
@@ -545,7 +547,7 @@ dpb_status dpb_embedding(dpb_dtype dtype, const void* table, int64_t table_strid
 /* EMBEDDING BACKWARD: grad_table[v] = scale * sum of grad_out[t] over the t with tokens[t] = v,
  * all of the contiguous [vocab, dim] written (zeros for rows that no token names).
  * The tokens are sorted by their rows, keeping their order, and each row's
- * gradients are added up in it.  count < 2^31 and vocab < 2^31 - 2^16. */
+ * gradients are added up in it.  count and vocab < 2^31 - 2^16. */
 size_t dpb_embedding_bwd_workspace_bytes(int64_t vocab, int dim, int64_t count);
 dpb_status dpb_embedding_bwd(dpb_dtype dtype, const void* grad_out, int64_t grad_stride, const void* tokens, int index_bits,
                              int64_t count, int64_t vocab, int dim, float scale, void* grad_table, void* workspace,
@@ -579,8 +581,9 @@ dpb_status dpb_rms_norm_bwd(dpb_dtype dtype, const void* grad_out, int64_t grad_
 
 /* Hidden rows and the vocabulary's matrix whose products are the logits
  *   logits = scale * hidden [rows, dim] * weight [vocab, dim]^T,   scale > 0.
- * Both start on 16 bytes; strides of their rows are any (under 8 MiB): rows that do not
- * start on 16 bytes are copied into the workspace first. */
+ * Both start on 16 bytes; strides of their rows are any (under 8 MiB, and so is a row): rows that
+ * do not start on 16 bytes are copied into the workspace first.  rows * vocab < 2^35 or so: 2^24
+ * tiles of 64 x 64. */
 typedef struct {
     const void *hidden, *weight;
     int64_t hidden_stride, weight_stride;
@@ -605,7 +608,7 @@ dpb_status dpb_cross_entropy(const dpb_logits* a, dpb_dtype dtype, const void* t
  *   grad_hidden = scale D weight,   grad_weight = scale D^T hidden
  * grad_hidden [rows, dim], grad_weight [vocab, dim]: contiguous, 16-byte aligned, either may
  * be NULL.  The logits are computed once more, over pieces of the vocabulary such that a piece's
- * D takes 1 GiB of the workspace or less (or 1,024 entries).  With bf16 D is rounded to bf16 as
+ * D takes 1 GiB of the workspace or less, and 8 MiB for a token (or 1,024 entries).  With bf16 D is rounded to bf16 as
  * operand of the products.  What is not finite in a row of hidden reaches all of
  * grad_weight, in one of weight all of grad_hidden (0 times it is no 0). */
 size_t dpb_cross_entropy_bwd_workspace_bytes(const dpb_logits* a, dpb_dtype dtype);

@@ -364,14 +364,14 @@ class ParityTransformer(torch.nn.Module):
         return torch.nn.functional.linear(self.hidden(tokens, caches, start)[0], self.embed.weight)
 
     def loss(self, tokens: torch.Tensor, targets: torch.Tensor):
-        """(mean loss over the targets that are in the vocabulary, the blocks' variance loss)."""
+        """(mean loss over the targets that are in the vocabulary, 0 if none is; the blocks' variance loss)."""
         z, loss_var = self.hidden(tokens)
         weight = self.embed.weight
         if torch.is_autocast_enabled("cuda") and torch.get_autocast_dtype("cuda") == torch.bfloat16:
             z, weight = z.bfloat16(), weight.bfloat16()
         loss, _ = CrossEntropyLayer.apply(z, weight, targets)
         counted = ((targets >= 0) & (targets < weight.shape[0])).sum()
-        return loss.sum() / counted, loss_var
+        return loss.sum() / counted.clamp(min=1), loss_var
 
     def caches(self, batch: int, length: int) -> list[KeyValueCache]:
         return [b.attention.cache(batch, length) for b in self.blocks]

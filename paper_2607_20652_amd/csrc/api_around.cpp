@@ -13,6 +13,8 @@ namespace {
 
 constexpr int64_t kMaxRows = ((int64_t)1 << 31) - 65536;   // rows are counted in 32 bits
 constexpr int64_t kMaxStride = (int64_t)1 << 23;           // bytes: 255 rows of a tile stay within a 31-bit offset
+constexpr int kMaxDim = 0x7FFF0000;                       // columns are counted in ints, chunks of lanes past the last too
+constexpr int kMaxNormDim = 1 << 22;                       // 512 workgroups' parts of a weight's gradient fit a launch
 constexpr double kMaxGroups = 16777216.;                   // workgroups of 256 threads: a launch has under 2^32
 
 bool dtype_ok(dpb_dtype t) { return t == DPB_F32 || t == DPB_BF16; }
@@ -37,7 +39,7 @@ Span span(const void* p, int64_t bytes) { return p && bytes > 0 ? Span{(uintptr_
 Span rows_span(const void* p, int64_t rows, int64_t stride, int64_t row) { return span(p, rows > 0 ? (rows - 1) * stride + row : 0); }
 bool meet(const Span& a, const Span& b) { return a.set() && b.set() && a.begin < b.end && b.begin < a.end; }
 
-// A stride of rows in elements: not negative, and its bytes do not pass 2^48 over all rows.
+// A stride of rows in elements: not negative, and its bytes do not pass 2^48 over all rows, which no address does.
 bool stride_ok(int64_t stride, int64_t rows) { return stride >= 0 && (double)stride * (double)std::max<int64_t>(rows, 1) < 7e13; }
 
 bool index_ok(const void* p, int bits, int64_t n) { return (bits == 32 || bits == 64) && (n == 0 || (p && aligned(p, bits / 8))); }
@@ -52,6 +54,7 @@ dpb_status dpb_embedding(dpb_dtype dtype, const void* table, int64_t table_strid
     if (!dtype_ok(dtype) || vocab < 0 || dim < 1 || count < 0 || !std::isfinite(scale) || !index_ok(tokens, index_bits, count) ||
         !stride_ok(table_stride, vocab))
         return DPB_EINVAL;
+    if (dim > kMaxDim || !stride_ok(dim, count)) return DPB_EUNSUPPORTED;
     if (count == 0) return DPB_OK;
     const int64_t b = bytes_of(dtype);
     if ((vocab > 0 && !table) || !out || !aligned(table, b) || !aligned(out, 16)) return DPB_EINVAL;
@@ -77,7 +80,7 @@ static bool embed_bwd_sizes(int64_t vocab, int dim, int64_t count)
 }
 static bool embed_bwd_fits(int64_t vocab, int dim, int64_t count)
 {
-    if (vocab >= kMaxRows || count >= kMaxRows) return false;
+    if (vocab >= kMaxRows || count >= kMaxRows || dim > kMaxDim) return false;
     // a wave for each row of the table and each 64 tokens, and 64 elements (a workgroup where they are joined)
     const double blocks = std::ceil(dim / 64.), chunks = std::ceil(count / 64.);
     return (chunks + (double)vocab) * blocks / 4 + 1 < kMaxGroups && chunks * blocks < kMaxGroups;
@@ -126,6 +129,7 @@ dpb_status dpb_rms_norm(dpb_dtype dtype, const void* x, int64_t x_stride, const 
     if (!dtype_ok(dtype) || !dtype_ok(weight_dtype) || rows < 0 || dim < 1 || !(eps >= 0.f) || !std::isfinite(eps) ||
         !stride_ok(x_stride, rows) || (residual && !stride_ok(residual_stride, rows)))
         return DPB_EINVAL;
+    if (dim > kMaxNormDim || !stride_ok(dim, rows)) return DPB_EUNSUPPORTED;
     if (rows == 0) return DPB_OK;
     const int64_t b = bytes_of(dtype);
     if (!x || !out || (residual && !total) || !aligned(x, b) || !aligned(residual, b) || !aligned(out, b) ||
@@ -159,7 +163,7 @@ dpb_status dpb_rms_norm(dpb_dtype dtype, const void* x, int64_t x_stride, const 
 
 size_t dpb_rms_norm_bwd_workspace_bytes(int64_t rows, int dim)
 {
-    return rows <= 0 || dim < 1 ? 0 : dpb::norm_bwd_ws_bytes(rows, dim);
+    return rows <= 0 || dim < 1 || dim > kMaxNormDim ? 0 : dpb::norm_bwd_ws_bytes(rows, dim);
 }
 
 dpb_status dpb_rms_norm_bwd(dpb_dtype dtype, const void* grad_out, int64_t grad_stride, const void* grad_total,
@@ -170,6 +174,7 @@ dpb_status dpb_rms_norm_bwd(dpb_dtype dtype, const void* grad_out, int64_t grad_
     if (!dtype_ok(dtype) || !dtype_ok(weight_dtype) || rows < 0 || dim < 1 || !stride_ok(grad_stride, rows) ||
         !stride_ok(total_stride, rows) || (grad_total && !stride_ok(grad_total_stride, rows)))
         return DPB_EINVAL;
+    if (dim > kMaxNormDim || !stride_ok(dim, rows)) return DPB_EUNSUPPORTED;
     if (!grad_x && !grad_weight) return DPB_OK;
     const int64_t b = bytes_of(dtype), wb = bytes_of(weight_dtype);
     if (!aligned(grad_weight, wb)) return DPB_EINVAL;
@@ -239,13 +244,11 @@ static size_t laid_bytes(const dpb_logits* a, dpb_dtype t)
 
 static bool none(const dpb_logits* a) { return a->rows == 0 || a->vocab == 0; }
 
-static dpb_status logits_args(const dpb_logits* a, dpb_dtype dtype, const void* targets, int index_bits, void* workspace,
-                              size_t ws_bytes, size_t need)
+static dpb_status logits_args(const dpb_logits* a, const void* targets, int index_bits, void* workspace, size_t ws_bytes, size_t need)
 {
     if (!index_ok(targets, index_bits, a->rows)) return DPB_EINVAL;
     if (!a->hidden || !a->weight || !aligned(a->hidden, 16) || !aligned(a->weight, 16)) return DPB_EINVAL;
     if (!workspace || !aligned(workspace, 16) || ws_bytes < need) return DPB_EINVAL;
-    (void)dtype;
     return DPB_OK;
 }
 
@@ -305,7 +308,7 @@ dpb_status dpb_cross_entropy(const dpb_logits* a, dpb_dtype dtype, const void* t
     if (a->rows == 0) return DPB_OK;
     if (a->vocab == 0) return DPB_EINVAL;   // no distribution over nothing
     const size_t need = dpb_cross_entropy_workspace_bytes(a, dtype);
-    if ((s = logits_args(a, dtype, targets, index_bits, workspace, ws_bytes, need))) return s;
+    if ((s = logits_args(a, targets, index_bits, workspace, ws_bytes, need))) return s;
     if (!loss || !lse || !aligned(loss, 4) || !aligned(lse, 4)) return DPB_EINVAL;
     const int64_t b = bytes_of(dtype);
     const Span in[3] = {rows_span(a->hidden, a->rows, a->hidden_stride * b, a->dim * b),
@@ -333,7 +336,7 @@ dpb_status dpb_cross_entropy_bwd(const dpb_logits* a, dpb_dtype dtype, const voi
     if ((!grad_hidden && !grad_weight) || (a->rows == 0 && a->vocab == 0)) return DPB_OK;
     if (none(a)) return DPB_EINVAL;   // (of no rows the weight's gradient is zeros: the caller's to write)
     const size_t need = dpb_cross_entropy_bwd_workspace_bytes(a, dtype);
-    if ((s = logits_args(a, dtype, targets, index_bits, workspace, ws_bytes, need))) return s;
+    if ((s = logits_args(a, targets, index_bits, workspace, ws_bytes, need))) return s;
     if (!lse || !aligned(lse, 4) || !aligned(grad_loss, 4) || !aligned(grad_lse, 4) || !aligned(grad_hidden, 16) ||
         !aligned(grad_weight, 16))
         return DPB_EINVAL;

@@ -100,6 +100,21 @@ def test_norms_of_nothing():
     assert lib.dpb_rms_norm_bwd_workspace_bytes(3, 100) >= 400
 
 
+def test_rows_past_what_is_counted():
+    top, most = (1 << 31) - 1, (1 << 31) - 65536
+    lib = dpb.load()
+    assert embed(dim=top, count=0) == embed(dim=most + 1, stride=0) == EUNSUPPORTED and embed(dim=most, count=0) == OK
+    assert embed(count=1 << 60) == EUNSUPPORTED and embed_bwd(dim=top, vocab=1) == EUNSUPPORTED
+    assert lib.dpb_embedding_bwd_workspace_bytes(1, top, 1) == 0
+    for big in (dict(dim=(1 << 22) + 1), dict(dim=top), dict(rows=1 << 60, dim=1)):
+        if "rows" in big:
+            assert norm(**big, xs=0, rs=0) == EUNSUPPORTED and norm_bwd(**big, gs=0, hs=0, zs=0) == EUNSUPPORTED
+        else:
+            assert norm(**big) == EUNSUPPORTED and norm_bwd(**big) == EUNSUPPORTED
+            assert lib.dpb_rms_norm_bwd_workspace_bytes(10, big["dim"]) == 0
+    assert norm(rows=0, dim=1 << 22) == OK and lib.dpb_rms_norm_bwd_workspace_bytes(10, 1 << 22) >= 1 << 24
+
+
 def logits(hidden=GB, weight=2 * GB, hs=64, ws=64, rows=10, vocab=100, dim=64, scale=1.0):
     return dpb._LOGITS.pack(hidden, weight, hs, ws, rows, vocab, dim, scale)
 

@@ -176,3 +176,12 @@ def test_layers_give_the_calls_results():
     assert torch.equal(loss, want[0]) and torch.equal(lse, want[1])
     assert torch.equal(leaves["res"].grad, want[4]) and torch.equal(leaves["w"].grad, want[5])
     assert torch.allclose(leaves["table"].grad, want[3] + want[6], rtol=1e-6, atol=1e-6)
+
+
+def test_a_batch_of_padding_alone():
+    model = model_of()
+    tokens = torch.full((2, 16), -1, device=DEV)
+    loss, _ = model.loss(tokens, tokens)
+    loss.backward()
+    assert float(loss.detach()) == 0.0 and not model.embed.weight.grad.any()
+    assert all(torch.isfinite(p.grad).all() for p in model.parameters() if p.grad is not None)
