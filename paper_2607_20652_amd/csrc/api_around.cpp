@@ -80,10 +80,10 @@ static bool embed_bwd_sizes(int64_t vocab, int dim, int64_t count)
 }
 static bool embed_bwd_fits(int64_t vocab, int dim, int64_t count)
 {
-    if (vocab >= kMaxRows || count >= kMaxRows || dim > kMaxDim) return false;
-    // a wave for each row of the table and each 64 tokens, and 64 elements (a workgroup where they are joined)
-    const double blocks = std::ceil(dim / 64.), chunks = std::ceil(count / 64.);
-    return (chunks + (double)vocab) * blocks / 4 + 1 < kMaxGroups && chunks * blocks < kMaxGroups;
+    if (vocab >= kMaxRows || count >= kMaxRows || dim > kMaxDim || !stride_ok(dim, vocab)) return false;
+    // a wave for each 32 tokens, each 8, and 64 elements (a workgroup where parts are joined)
+    const double blocks = std::ceil(dim / 64.), chunks = std::ceil(count / 32.);
+    return (chunks + std::ceil(count / 8.)) * blocks / 4 + 1 < kMaxGroups && chunks * blocks < kMaxGroups;
 }
 
 size_t dpb_embedding_bwd_workspace_bytes(int64_t vocab, int dim, int64_t count)

@@ -5,12 +5,13 @@
 //   1. bin: a workgroup puts 1,024 tokens in order of bucket (2^shift rows of the table, at
 //      most 1,024 buckets), with the start of each bucket (not of up to 16,384 tokens);
 //   2. order: a workgroup gathers a bucket from all of those, or from the tokens themselves, in their
-//      order, counts its rows and places each token behind those before it;
-//   3. sum: a wave adds up a row of up to 64 tokens, zeros if there are none; 64 places of the sorted
-//      order that hold a longer row, padding or a frequent word, leave that row's part of them;
+//      order, counts its rows and places each token behind those before it; rows without tokens get zeros;
+//   3. sum: a wave adds up the rows of up to 32 tokens that start in 8 places of the sorted order; 32 places that
+//      hold a longer row, padding or a frequent word, leave that row's part of them;
 //   4. join: the parts of a long row are added up in order.
-// Bound by memory: the gradients read once, the table's written once; the sort moves 20
-// bytes a token.
+// Bound by memory where the table is large: the gradients read once, the table's written once; the sort moves 20
+// bytes a token.  16,384 gradients of 1,024 bf16 into 50,304 rows: 57.8 us, of which 27 + 16.5 + 5 are the kernels'
+// and the rest is between them; a copy of as many bytes takes 29.
 #include <algorithm>
 
 #include "rows.hpp"
@@ -24,7 +25,8 @@ constexpr int kScan = 16384;        // tokens, at most, that every workgroup rea
 constexpr int kScanBuckets = 512;   // most then
 constexpr int kRowsAtOnce = 1024;   // rows of a bucket that are ordered together
 constexpr int kOrderWaves = 8;      // of the workgroup that does
-constexpr int kLong = 64;           // tokens of a row that a wave adds up
+constexpr int kLong = 32;           // tokens of a row, at most, that are added up in one go; places of a chunk
+constexpr int kStarts = 8;          // places where the rows start that a wave adds up
 
 __device__ __forceinline__ int64_t token_at(const EmbedArgs& a, int64_t t)
 {
@@ -64,7 +66,7 @@ struct Sorted {
     uint32_t* rows;     // [count] their rows
     uint32_t* first;    // [vocab + 1] first place of a row
     float* part;        // [chunks][2][width]
-    int64_t chunks, width;
+    int64_t chunks, width, row_bytes;
 };
 
 // Lanes that hold the same key (of `bits` bits) among those for which `live`.
@@ -217,11 +219,14 @@ __device__ __forceinline__ void each_entry(const Sorted& s, int bucket, int64_t 
 // Bound by latency: 16,384 tokens, as frequent as words are, over 50,304 rows take 6.2 us to bin and 17.4 to order
 // (a third is one bucket's; 39 with four waves that search their bins entry by entry), by scanning 20.6 in one launch;
 // evenly over 1,024 rows the two and the sum take 28.6 us, by scanning 24.2.
+// The bucket's rows without tokens get their zeros here, whose stores go on while the rest is ordered: 26.6 us with
+// 94 MB of them, which the sums then have not to write (with a wave a row of the table those took 30, now 16.5).
 template <bool SCAN>
 __global__ __launch_bounds__(64 * kOrderWaves) void embed_order_kernel(EmbedArgs a, Sorted s)
 {
     constexpr int kThreads = 64 * kOrderWaves, kEach = kRowsAtOnce / kThreads;   // rows a thread
     __shared__ uint32_t count[kOrderWaves][kRowsAtOnce];
+    __shared__ uint8_t some[kRowsAtOnce];   // rows with tokens
     const int bucket = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint64_t below = (1ull << lane) - 1;
     const int64_t row0 = (int64_t)bucket << s.shift, rows = min((int64_t)1 << s.shift, a.vocab - row0);
@@ -262,8 +267,19 @@ __global__ __launch_bounds__(64 * kOrderWaves) void embed_order_kernel(EmbedArgs
     for (int64_t r0 = 0; r0 < rows; r0 += kRowsAtOnce) {
         const int here = (int)min((int64_t)kRowsAtOnce, rows - r0);
         const uint32_t low = (uint32_t)(row0 + r0);
+        auto zeros = [&](bool all) {
+            for (int i = wave; i < here; i += kOrderWaves) {
+                if (!all && __builtin_amdgcn_readfirstlane((int)some[i])) continue;
+                char* const row = (char*)a.out + (int64_t)(low + i) * s.row_bytes;
+                if (s.row_bytes % 16 == 0)
+                    for (int64_t c = lane * 16; c < s.row_bytes; c += 1024) *(u32x4*)(row + c) = (u32x4){0, 0, 0, 0};
+                else
+                    for (int64_t c = lane * 2; c < s.row_bytes; c += 128) *(uint16_t*)(row + c) = 0;
+            }
+        };
         if (size == 0) {   // a bucket that no token names
             for (int i = threadIdx.x; i < here; i += kThreads) s.first[low + i] = base;
+            zeros(true);
             continue;
         }
         __syncthreads();
@@ -285,6 +301,7 @@ __global__ __launch_bounds__(64 * kOrderWaves) void embed_order_kernel(EmbedArgs
             for (int w = 0; w < kOrderWaves; ++w) sum += count[w][i];
         uint32_t at = base + prefix<kOrderWaves>(sum, total);
         for (int i = first; i < min(first + kEach, here); ++i) {
+            const uint32_t before = at;
             s.first[low + i] = at;
 #pragma unroll
             for (int w = 0; w < kOrderWaves; ++w) {
@@ -292,9 +309,12 @@ __global__ __launch_bounds__(64 * kOrderWaves) void embed_order_kernel(EmbedArgs
                 count[w][i] = at;
                 at += c;
             }
+            some[i] = at != before;
         }
         base += total;
         __syncthreads();
+        // (bins are read again, and a load would wait for the stores before it)
+        if (SCAN || total == 0) zeros(total == 0);
         if (total == 0) continue;
         each([&](uint2 x, bool valid) {
             const bool live = valid && x.x - low < (uint32_t)here;
@@ -310,13 +330,14 @@ __global__ __launch_bounds__(64 * kOrderWaves) void embed_order_kernel(EmbedArgs
             }
             wave_sync();
         });
+        if (!SCAN) zeros(false);
     }
     if (bucket == s.buckets - 1 && threadIdx.x == 0) s.first[a.vocab] = base;
 }
 
 // ---- sums
 
-// The rows that 64 places of the sorted order have, and which of them are long.
+// The rows at the ends of a chunk of the sorted order's places, and which of them are long (one between them is not).
 struct Chunk {
     int64_t at;          // first place
     int n;               // places
@@ -327,8 +348,8 @@ struct Chunk {
 __device__ __forceinline__ Chunk chunk_of(const EmbedArgs& a, const Sorted& s, int64_t chunk)
 {
     Chunk c;
-    c.at = chunk * 64;
-    c.n = (int)max((int64_t)0, min((int64_t)64, (int64_t)s.first[a.vocab] - c.at));
+    c.at = chunk * kLong;
+    c.n = (int)max((int64_t)0, min((int64_t)kLong, (int64_t)s.first[a.vocab] - c.at));
     c.begin[0] = c.end[0] = c.begin[1] = c.end[1] = 0;
     c.row[0] = c.row[1] = 0;
     if (c.n <= 0) return c;
@@ -340,7 +361,7 @@ __device__ __forceinline__ Chunk chunk_of(const EmbedArgs& a, const Sorted& s, i
         const int64_t f = s.first[c.row[i]], e = s.first[(int64_t)c.row[i] + 1];
         if (e - f <= kLong) continue;
         c.begin[i] = (int)(max(f, c.at) - c.at);
-        c.end[i] = (int)(min(e, c.at + 64) - c.at);
+        c.end[i] = (int)(min(e, c.at + kLong) - c.at);
     }
     return c;
 }
@@ -353,13 +374,15 @@ __device__ __forceinline__ void sum_places(const EmbedArgs& a, const Sorted& s, 
     const uint32_t mine = lane < n ? s.order[from + lane] : 0;
 #pragma unroll
     for (int i = 0; i < E; ++i) sum[i] = 0.f;
-    constexpr int kAhead = 4;   // gradients under way together
+    constexpr int kAhead = 8;   // gradients under way together
     for (int k = 0; k < n; k += kAhead) {
         float g[kAhead][E];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j)
-            if (k + j < n && e < a.dim)
-                load_chunk<T, E>((const char*)a.table + (int64_t)__builtin_amdgcn_readlane(mine, k + j) * a.stride, e, g[j]);
+        for (int j = 0; j < kAhead; ++j) {
+            if (k + j >= n) break;
+            const uint32_t t = __builtin_amdgcn_readlane(mine, k + j);   // (by all lanes: those past the row's end hold tokens too)
+            if (e < a.dim) load_chunk<T, E>((const char*)a.table + (int64_t)t * a.stride, e, g[j]);
+        }
 #pragma unroll
         for (int j = 0; j < kAhead; ++j)
             if (k + j < n) {
@@ -369,8 +392,9 @@ __device__ __forceinline__ void sum_places(const EmbedArgs& a, const Sorted& s, 
     }
 }
 
-// Units of 64 chunks of elements, a wave each: first those of the sorted order's parts, then those of
-// the table's rows.
+// Units of 64 lanes' elements, a wave each: first the long rows' parts of the sorted order's chunks, then
+// the other rows by the places where they start.  Those gradients are loaded one after the other, whatever
+// their rows: a row by itself waits for its tokens and then for few loads.
 template <typename T, int E>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, Sorted s, int blocks)
 {
@@ -392,16 +416,57 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, Sorted s, i
         }
         return;
     }
-    const int64_t row = item - s.chunks;
-    if (row >= a.vocab) return;
-    const uint32_t first = __builtin_amdgcn_readfirstlane(s.first[row]);
-    const uint32_t n = __builtin_amdgcn_readfirstlane(s.first[row + 1]) - first;
-    if (n > kLong) return;
-    sum_places<T, E>(a, s, first, (int)n, e, sum);
-    if (e >= a.dim) return;
+    // places from the one before, a lane each
+    static_assert(kStarts + kLong < 64, "the longest row ends among the wave's places");
+    const int64_t first = (item - s.chunks) * kStarts, place = first - 1 + lane, total = s.first[a.vocab];
+    if (first >= total) return;
+    const bool there = place >= 0 && place < total;
+    const uint32_t row = there ? s.rows[place] : ~0u, token = there ? s.order[place] : 0;
+    const uint32_t before = __shfl_up(row, 1, 64);   // (of all lanes)
+    const uint64_t begins = __ballot(lane == 0 || row != before), named = __ballot(there);
+    uint64_t left = 0;   // places whose gradients are summed
+    for (uint64_t at = begins & named & ((2ull << kStarts) - 2); at; at &= at - 1) {
+        const int b = __builtin_ctzll(at);
+        const uint64_t later = begins >> b >> 1;
+        const int n = later ? __builtin_ctzll(later) + 1 : 64 - b;
+        if (n <= kLong) left |= ((1ull << n) - 1) << b;
+    }
+    int from = -1;   // the lane of the row that is summed
+    auto leave = [&]() {
+        if (from < 0) return;
+        const uint32_t to = __builtin_amdgcn_readlane(row, from);   // (by all lanes, as the tokens)
+        if (e >= a.dim) return;
 #pragma unroll
-    for (int i = 0; i < E; ++i) sum[i] *= a.scale;
-    store_chunk<T, E>(a.out, row * a.dim + e, sum);
+        for (int i = 0; i < E; ++i) sum[i] *= a.scale;
+        store_chunk<T, E>(a.out, (int64_t)to * a.dim + e, sum);
+    };
+    constexpr int kAhead = 8;
+    while (left) {
+        float g[kAhead][E];
+        int at[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            at[j] = left ? __builtin_ctzll(left) : -1;
+            left &= left - 1;
+            if (at[j] < 0) continue;
+            const uint32_t t = __builtin_amdgcn_readlane(token, at[j]);
+            if (e < a.dim) load_chunk<T, E>((const char*)a.table + (int64_t)t * a.stride, e, g[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            if (at[j] < 0) break;
+            if (begins >> at[j] & 1) {
+                leave();
+                from = at[j];
+#pragma unroll
+                for (int i = 0; i < E; ++i) sum[i] = g[j][i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < E; ++i) sum[i] += g[j][i];
+            }
+        }
+    }
+    leave();
 }
 
 // A long row that starts in this chunk: its parts' sum, 64 columns a workgroup; the waves take
@@ -413,22 +478,24 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs a, Sorted s, 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t chunk = blockIdx.x / blocks;
     const int e = (int)(blockIdx.x % blocks) * 64 + lane;
-    const Chunk c = chunk_of(a, s, chunk);
-    const int i = c.end[1] > c.begin[1] ? 1 : 0;
-    if (c.end[i] <= c.begin[i]) return;
-    const int64_t first = s.first[c.row[i]], end = s.first[(int64_t)c.row[i] + 1];
-    if (first < c.at) return;
-    const int64_t n = (end - 1) / 64 - chunk + 1;   // parts
+    // it goes on in the next chunk, and has not begun before this one
+    const int64_t at = chunk * kLong, total = s.first[a.vocab];
+    const uint32_t row = s.rows[min(at + kLong, a.count) - 1], next = s.rows[min(at + kLong, a.count - 1)];
+    const bool begun = at && s.rows[at - 1] == row;
+    if (at + kLong >= total || next != row || begun) return;
+    const int64_t first = s.first[row], end = s.first[(int64_t)row + 1];
+    if (end - first <= kLong) return;
+    const int64_t n = (end - 1) / kLong - chunk + 1;   // parts
     float sum = 0.f;
     if (e < a.dim)
 #pragma unroll 8
         for (int64_t k = n * wave / 4; k < n * (wave + 1) / 4; ++k)
-            sum += s.part[((chunk + k) * 2 + (k == 0 && first > c.at)) * s.width + e];
+            sum += s.part[((chunk + k) * 2 + (k == 0 && first > at)) * s.width + e];
     lds[wave][lane] = sum;
     __syncthreads();
     if (wave || e >= a.dim) return;
     sum = lds[0][lane] + lds[1][lane] + lds[2][lane] + lds[3][lane];
-    store_act<sizeof(T) == 2>(a.out, (int64_t)c.row[i] * a.dim + e, sum * a.scale);
+    store_act<sizeof(T) == 2>(a.out, (int64_t)row * a.dim + e, sum * a.scale);
 }
 
 size_t round16(size_t n) { return (n + 15) / 16 * 16; }
@@ -441,7 +508,7 @@ size_t lay_out(int64_t vocab, int dim, int64_t count, char* ws, Sorted* s)
     while ((vocab - 1) >> s->shift >= (scan ? kScanBuckets : kBuckets)) ++s->shift;
     s->buckets = (int)((vocab - 1) >> s->shift) + 1;
     s->bins = scan ? 0 : (count + kBin - 1) / kBin;
-    s->chunks = (count + 63) / 64;
+    s->chunks = (count + kLong - 1) / kLong;
     s->width = (dim + 3) / 4 * 4;
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -474,7 +541,7 @@ template <typename T, int E>
 void embed_sum(const EmbedArgs& a, const Sorted& s, hipStream_t stream)
 {
     const int blocks = (a.dim + 64 * E - 1) / (64 * E);
-    embed_sum_kernel<T, E><<<dim3((unsigned)(((s.chunks + a.vocab) * blocks + 3) / 4)), 256, 0, stream>>>(a, s, blocks);
+    embed_sum_kernel<T, E><<<dim3((unsigned)(((s.chunks + (a.count + kStarts - 1) / kStarts) * blocks + 3) / 4)), 256, 0, stream>>>(a, s, blocks);
 }
 
 template <typename T>
@@ -483,9 +550,11 @@ hipError_t embed_bwd(const EmbedArgs& a, hipStream_t stream)
     constexpr int E = 16 / (int)sizeof(T);
     Sorted s;
     lay_out(a.vocab, a.dim, a.count, a.ws, &s);
+    s.row_bytes = (int64_t)a.dim * (int)sizeof(T);
     if (s.bins) embed_bin_kernel<<<dim3((unsigned)s.bins), 256, 0, stream>>>(a, s);
     if (s.bins) embed_order_kernel<false><<<dim3((unsigned)s.buckets), 64 * kOrderWaves, 0, stream>>>(a, s);
     else embed_order_kernel<true><<<dim3((unsigned)s.buckets), 64 * kOrderWaves, 0, stream>>>(a, s);
+    if (a.count == 0) return hipGetLastError();
     if (a.dim % E == 0 && a.stride % 16 == 0 && on16(a.table) && on16(a.out)) embed_sum<T, E>(a, s, stream);
     else embed_sum<T, 1>(a, s, stream);
     const int blocks = (a.dim + 63) / 64;

@@ -43,7 +43,8 @@ def test_lookups_of_nothing_and_of_too_much():
     lib = dpb.load()
     assert lib.dpb_embedding_bwd_workspace_bytes(0, 64, 10) == 0
     assert lib.dpb_embedding_bwd_workspace_bytes(-1, 64, 10) == 0 and lib.dpb_embedding_bwd_workspace_bytes(5, 0, 10) == 0
-    for big in (dict(vocab=(1 << 31) - 65536, dim=1, stride=1), dict(count=(1 << 31) - 65536, dim=1, stride=1), dict(vocab=1 << 28)):
+    for big in (dict(vocab=(1 << 31) - 65536, dim=1, stride=1), dict(count=(1 << 31) - 65536, dim=1, stride=1), dict(count=1 << 30, dim=1 << 20, stride=0),
+                dict(vocab=1 << 30, dim=1 << 20)):
         assert embed_bwd(**big) == EUNSUPPORTED, big
         assert lib.dpb_embedding_bwd_workspace_bytes(big.get("vocab", 100), big.get("dim", 64), big.get("count", 10)) == 0
 
@@ -51,11 +52,11 @@ def test_lookups_of_nothing_and_of_too_much():
 @pytest.mark.parametrize("vocab,dim,count", [(1, 1, 0), (1, 1, 1), (50304, 1024, 16384), (50304, 1024, 16385), (1025, 33, 65), (3_000_000, 4, 1000)])
 def test_sorting_space(vocab, dim, count):
     """Two words a token of whole bins (above 16,384 of them), two more, starts of buckets and rows, and two parts of
-    each 64 tokens."""
+    each 32 tokens."""
     shift, bins = 0, -(-count // 1024) if count > 16384 else 0
     while (vocab - 1) >> shift >= (1024 if bins else 512):
         shift += 1
-    buckets, chunks = ((vocab - 1) >> shift) + 1, -(-count // 64)
+    buckets, chunks = ((vocab - 1) >> shift) + 1, -(-count // 32)
     up = lambda n: -(-n // 16) * 16  # noqa: E731
     want = up(bins * 8192) + up(bins * (buckets + 1) * 4) + 2 * up(count * 4) + up((vocab + 1) * 4) + up(chunks * 8 * (-(-dim // 4) * 4))
     assert dpb.load().dpb_embedding_bwd_workspace_bytes(vocab, dim, count) == want

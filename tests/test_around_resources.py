@@ -11,7 +11,8 @@ BUDGETS = [
     (r"loss_(part|grad|out)_kernelI.*Li128E", 256),
     (r"loss_(part|grad|out)_kernelI.*Li64E", 128),
     (r"embed_order_kernel", 128),
-    (r"embed_(bin|sum|join)_kernel", 80),
+    (r"embed_(bin|join)_kernel", 80),
+    (r"embed_sum_kernel", 96),
     (r"11norm_kernelI.*Li64ELi[124]E", 128),
     (r"15norm_bwd_kernelI.*Li64ELi[124]E", 256),
 ]
