@@ -9,7 +9,8 @@
 // What bounds a tile of 256 x 256: the matrix cores.  32 contraction values are 32 MFMAs a
 // wave (1,024 cycles) beside 16 reads of LDS and 8 loads.  A wave of 128 x 128 reads half an
 // operand an MFMA; with waves of 128 x 64 LDS would deliver three quarters of one and
-// take the loads besides, its whole bandwidth.
+// take the loads besides, its whole bandwidth.  (16,384 x 1,024 x 25,344 from blocks: 617 to 700 us, 1.22 to
+// 1.38 PFLOP/s.)
 #pragma once
 
 #include "attention.hpp"

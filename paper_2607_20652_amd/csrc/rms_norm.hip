@@ -6,6 +6,7 @@
 // 32 KB) between its sum and its outputs, so everything is read and written once;
 // longer rows are read twice.  The weight's gradient is summed in registers over the rows that
 // a workgroup takes in turn, and a second kernel adds up the workgroups' parts in order.
+// (16,384 rows of 1,024 bf16: 28 us forward, 32 backward; a copy of as many bytes takes 28.)
 #include <algorithm>
 
 #include "rows.hpp"
@@ -274,19 +275,25 @@ __global__ __launch_bounds__(1024) void norm_sum_kernel(NormBwdArgs a, int parts
     else store_act<false>(a.dweight, e, v);
 }
 
-// Workgroups that take rows in turn, at most: two a compute unit in the backward, whose parts
-// the second kernel reads; eight in the forward.
+// Workgroups that take rows in turn, at most so many a compute unit.
 int norm_groups(int64_t rows, int each, int per_cu)
 {
     return (int)std::min<int64_t>((rows + each - 1) / each, (int64_t)device_cus() * per_cu);
 }
 
+// The backward: their parts are what the second kernel reads (16,384 rows of 1,024 bf16: 32.5 us with one, 26.8
+// with two, 29.6 with four; a workgroup a row 36.5).
 constexpr int kBwdGroups = 2;
 
+// The forward: enough to have some 64 KB a compute unit under way, and so few that a row's weights are read for
+// several rows and the last round is full.  16,384 bf16 rows, us with 4, 6 and 8 of them: 1,024 wide 28.0, 29.1, 31.2;
+// 2,048: 55.7, 68.4, 65.5; 4,096: 103.7, 100.8, 126; 8,192: 204, 242, 216; of one chunk a lane (65,536 of 512): 49.3, 44.8, 46.0;
+// rows that are read by elements, 500: 33.5, 26.1, 21.0, and 1,001: 82.5, 63.1, 81.9 (their registers let six be resident).
 template <typename T, int E, int LANES, int C>
 hipError_t norm(const NormArgs& a, hipStream_t s)
 {
-    norm_kernel<T, E, LANES, C><<<dim3(norm_groups(a.rows, 256 / LANES, 8)), 256, 0, s>>>(a);
+    constexpr int kGroups = E == 1 ? (C > 8 ? 6 : 8) : C == 1 ? 8 : 4;
+    norm_kernel<T, E, LANES, C><<<dim3(norm_groups(a.rows, 256 / LANES, kGroups)), 256, 0, s>>>(a);
     return hipGetLastError();
 }
 
