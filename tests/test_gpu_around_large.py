@@ -1,5 +1,7 @@
 """Embedding, norm and vocabulary loss at sizes where tiles are largest, products are split, the vocabulary goes in
 pieces or offsets pass 32 bits; and the layers' backward in a captured graph."""
+import threading
+
 import pytest
 import torch
 
@@ -101,6 +103,54 @@ def test_hidden_rows_far_apart():
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     got, want = (dpb.cross_entropy_bwd(ga, x, y, t, want[1]) for x, y in ((far_h, far_w), (h, w)))
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_one_workspace_for_calls_of_all_sizes():
+    """Whatever an earlier call has left in it; and one that is too small is refused."""
+    space = torch.full((1 << 24,), float("nan"), device=DEV)
+    for rows, dim, vocab in ((700, 129, 2000), (40, 64, 40000), (3000, 256, 300)):
+        h, w, t, ga, _ = draw(rows, dim, vocab, torch.bfloat16)
+        loss, lse = dpb.cross_entropy(h, w, t)
+        got = dpb.cross_entropy(h, w, t, workspace=space)
+        assert torch.equal(got[0], loss) and torch.equal(got[1], lse)
+        for a, b in zip(dpb.cross_entropy_bwd(ga, h, w, t, lse, workspace=space), dpb.cross_entropy_bwd(ga, h, w, t, lse)):
+            assert torch.equal(a, b)
+        assert torch.equal(dpb.embedding_bwd(h, t, vocab, workspace=space), dpb.embedding_bwd(h, t, vocab))
+        weight = w[0].contiguous()
+        _, total, rstd = dpb.rms_norm(h, weight)
+        for a, b in zip(dpb.rms_norm_bwd(h, total, weight, rstd, workspace=space), dpb.rms_norm_bwd(h, total, weight, rstd)):
+            assert torch.equal(a, b)
+        for call in (lambda: dpb.cross_entropy(h, w, t, workspace=space[:4]), lambda: dpb.cross_entropy_bwd(ga, h, w, t, lse, workspace=space[:4]),
+                     lambda: dpb.embedding_bwd(h, t, vocab, workspace=space[:4]), lambda: dpb.rms_norm_bwd(h, total, weight, rstd, workspace=space[:4])):
+            with pytest.raises(RuntimeError):
+                call()
+
+
+def test_calls_of_two_threads():
+    """Each on a stream of its own, at once."""
+    def work(seed, out):
+        torch.cuda.set_device(0)
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(10):
+                h, w, t, ga, lse = inputs[seed]
+                out.append((*dpb.cross_entropy(h, w, t), *dpb.cross_entropy_bwd(ga, h, w, t, lse), dpb.embedding_bwd(h, t, len(w))))
+            torch.cuda.current_stream().synchronize()
+
+    inputs, want = [], []
+    for size in ((600, 96, 1500), (50, 128, 9000)):
+        h, w, t, ga, _ = draw(*size, torch.bfloat16)
+        loss, lse = dpb.cross_entropy(h, w, t)
+        inputs.append((h, w, t, ga, lse))
+        want.append((loss, lse, *dpb.cross_entropy_bwd(ga, h, w, t, lse), dpb.embedding_bwd(h, t, len(w))))
+    torch.cuda.synchronize()
+    got = [[], []]
+    threads = [threading.Thread(target=work, args=(i, got[i])) for i in range(2)]
+    for thread in threads:
+        thread.start()
+    for thread in threads:
+        thread.join()
+    for outs, one in zip(got, want):
+        assert len(outs) == 10 and all(torch.equal(a, b) for out in outs for a, b in zip(out, one))
 
 
 def test_a_captured_backward_of_the_layers():
