@@ -21,17 +21,14 @@ __device__ __forceinline__ void wave_sync()
 
 __device__ __forceinline__ float bf16_bits_to_f32(uint32_t b) { return __uint_as_float(b << 16); }
 
-// float -> bf16 bits, round to nearest even.
-__device__ __forceinline__ uint32_t f32_to_bf16_rne(float f)
-{
-    uint32_t u = __float_as_uint(f);
-    u += 0x7FFFu + ((u >> 16) & 1u);
-    return u >> 16;
-}
+// float -> bf16 bits, round to nearest even: the hardware's conversion, which
+// keeps a NaN of any payload a NaN.  (The sum of the bits and half a step, which is
+// the same for all other numbers, carries a NaN of all bits set over to 0.)
+__device__ __forceinline__ uint32_t f32_to_bf16_rne(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
 
 // Two fp32 values rounded to nearest even as one word of bf16 (lo in bits
 // 0-15): a single hardware conversion on gfx950, equal to f32_to_bf16_rne of
-// each half for every non-NaN input.
+// each half.
 typedef float dpb_f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 dpb_bf16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi)
