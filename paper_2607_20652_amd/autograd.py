@@ -239,6 +239,14 @@ def _even(t: torch.Tensor) -> torch.Tensor:
     return t.clone(memory_format=torch.contiguous_format) if t.data_ptr() % 16 else t
 
 
+def _near(t: torch.Tensor) -> torch.Tensor:
+    """t, or a copy whose rows are as the loss takes them: even, and closer than it reads them from (the last token of
+    each long sequence, say)."""
+    t = _even(t)
+    far = not t.is_contiguous() and B._rows(t, "rows")[1] * t.element_size() >= B.LOGITS_STRIDE
+    return t.contiguous() if far else t
+
+
 class EmbeddingLayer(torch.autograd.Function):
     """scale * table[tokens]; tokens outside the table give zeros and no gradient."""
 
@@ -294,7 +302,7 @@ class CrossEntropyLayer(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, scale: float = 1.0):
-        hidden, weight, targets = _even(hidden), _even(weight), targets.contiguous()
+        hidden, weight, targets = _near(hidden), _near(weight), targets.contiguous()
         loss, lse = B.cross_entropy(hidden, weight, targets, scale)
         ctx.save_for_backward(hidden, weight, targets, lse)
         ctx.scale = scale

@@ -715,6 +715,7 @@ def _adamw(params, grads, m, v, scales, master, step, lr, betas, eps, weight_dec
 # ---- operators around the blocks: embedding, norm, loss over the vocabulary
 
 _LOGITS = struct.Struct("=QQqqqqif")
+LOGITS_STRIDE = 1 << 23     # bytes: rows of hidden states and vocabularies are closer than this
 
 
 def _place(t: torch.Tensor | None, name: str, device: int) -> int | None:
@@ -918,7 +919,8 @@ def cross_entropy(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Ten
     """(loss, lse), fp32 of the targets' shape: lse = log sum_v exp(scale <hidden, weight_v>),
     loss = lse - scale <hidden, weight_target>, 0 for a target outside [0, vocab).
 
-    hidden [..., dim] and weight [vocab, dim] of one type, rows evenly apart; the logits are never in memory."""
+    hidden [..., dim] and weight [vocab, dim] of one type, rows evenly apart and under 8 MiB from one to the
+    next (rows further apart are the caller's to copy); the logits are never in memory."""
     a, n = _logits(hidden, weight, targets, scale)
     given = [loss, lse]
     if loss is None:

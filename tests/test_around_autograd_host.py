@@ -135,3 +135,29 @@ def test_model_refuses_places_that_it_has_not(plain):
     assert torch.allclose(loss, want)
     loss.backward()
     assert all(p.grad is not None for p in model.parameters())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("far", ["hidden", "weight", "both"])
+def test_rows_far_apart_reach_the_loss_within_its_strides(plain, monkeypatch, dtype, far):
+    """The last token of each sequence of a long batch: rows of 8 MiB and more apart, which the library does not read
+    where they are, are copied; what it then gets has a workspace (a description that it refuses has none)."""
+    lib, seen = B.load(), []
+    for name in ("cross_entropy", "cross_entropy_bwd"):
+        def note(*args, _name=name, _f=getattr(B, name), **kw):
+            hidden, weight, targets = args[1:4] if _name.endswith("bwd") else args[:3]
+            a, _ = B._logits(hidden, weight, targets, 0.5)
+            seen.append(getattr(lib, f"dpb_{_name}_workspace_bytes")(a, B._dtype_code(hidden)))
+            return _f(*args, **kw)
+        monkeypatch.setattr(B, name, note)
+    step = (1 << 23) // torch.empty((), dtype=dtype).element_size()
+    wide = lambda n: torch.zeros(n * step, dtype=dtype).as_strided((n, 8), (step, 1))  # noqa: E731
+    near = lambda n: torch.zeros(n, 8, dtype=dtype)  # noqa: E731
+    h, w = (wide if far != "weight" else near)(4), (wide if far != "hidden" else near)(3)
+    h.copy_(torch.randn(4, 8, generator=torch.Generator().manual_seed(0)))
+    w.copy_(torch.randn(3, 8, generator=torch.Generator().manual_seed(1)))
+    h, w, t = h.requires_grad_(), w.requires_grad_(), torch.tensor([0, 2, 1, 0])
+    loss, lse = A.cross_entropy_layer(h, w, t, 0.5)
+    (loss.sum() + lse.sum()).backward()
+    assert len(seen) == 2 and all(seen)
+    assert torch.equal(loss, cross_entropy(h, w, t, 0.5)[0]) and h.grad.shape == h.shape and w.grad.shape == w.shape

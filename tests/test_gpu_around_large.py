@@ -186,3 +186,21 @@ def test_a_captured_backward_of_the_layers():
         torch.cuda.synchronize()
         others = [x.detach().clone().requires_grad_() for x in leaves]   # (leaves of their own)
         assert all(torch.equal(a, b) for a, b in zip(got, step(others)))
+
+
+@pytest.mark.parametrize("dtype,length", [(torch.bfloat16, 4096), (torch.bfloat16, 5000), (torch.float32, 2048)])
+def test_the_last_token_of_each_long_sequence(dtype, length):
+    """Hidden rows 8 MiB and more apart, through the layer: what their copy gives."""
+    h, w, t, ga, _ = draw(4, 1024, 600, dtype)
+    stream = torch.zeros(4, length, 1024, dtype=dtype, device=DEV)
+    stream[:, -1] = h
+    stream.requires_grad_()
+    far, near, table = stream[:, -1], h.clone().requires_grad_(), w.clone().requires_grad_()
+    for x in (far, near):
+        loss, lse = A.cross_entropy_layer(x, table, t)
+        if x is far:
+            first = loss, lse, *torch.autograd.grad((loss * ga).sum() + lse.sum(), (stream, table))
+        else:
+            second = loss, lse, *torch.autograd.grad((loss * ga).sum() + lse.sum(), (near, table))
+    assert all(torch.equal(first[i], second[i]) for i in (0, 1, 3))
+    assert torch.equal(first[2][:, -1], second[2]) and not first[2][:, :-1].any()
