@@ -105,9 +105,33 @@ def dpb_layer(x: torch.Tensor, plan: B.Plan, normalized: bool = True, n_min: int
     return DPBLayer.apply(x, plan, normalized, n_min, std)
 
 
+class RMSNorm(torch.nn.RMSNorm):
+    """torch.nn.RMSNorm over the last dimension; with a residual, norm(x, residual) is (norm of their sum, the sum) by
+    RMSNormLayer, in the residual's type."""
+
+    def forward(self, x: torch.Tensor, residual: torch.Tensor | None = None):
+        if residual is None:
+            return super().forward(x)
+        # (torch.nn.RMSNorm's own default, in bf16 too)
+        eps = torch.finfo(torch.float32).eps if self.eps is None else self.eps
+        # (under autocast a sublayer's output has not the stream's type)
+        return RMSNormLayer.apply(x.to(residual.dtype), self.weight, residual, eps)
+
+
+def _add_norm(norm: torch.nn.Module, x: torch.Tensor, residual: torch.Tensor):
+    """(norm of the sum, the sum), in one call where the norm offers that: another may stand in its place."""
+    if isinstance(norm, RMSNorm):
+        return norm(x, residual)
+    total = x.to(residual.dtype) + residual
+    return norm(total), total
+
+
 class DPBMLP(torch.nn.Module):
     """h + W2 gelu(W1 DPB(rmsnorm(h))): a transformer MLP sublayer with the
-    parity bottleneck at its input.  forward returns (output, loss_var)."""
+    parity bottleneck at its input.  forward returns (output, loss_var).
+
+    With a residual, h is h + residual, and the output the two terms (W2 ..., h + residual) of
+    the sum: the next norm adds them."""
 
     def __init__(self, plan: B.Plan, d_ff: int, normalized: bool = True, n_min: int | None = None,
                  standardize: bool = False, momentum: float = 0.01, dtype: torch.dtype = torch.float32, device=None):
@@ -118,14 +142,18 @@ class DPBMLP(torch.nn.Module):
         if self.std is not None:
             self.register_buffer("std_stats", self.std.stats)
             self.register_buffer("std_m2", self.std.m2)
-        self.norm = torch.nn.RMSNorm(d, dtype=dtype, device=device)
+        self.norm = RMSNorm(d, dtype=dtype, device=device)
         self.fc1 = torch.nn.Linear(d, d_ff, dtype=dtype, device=device)
         self.fc2 = torch.nn.Linear(d_ff, d, dtype=dtype, device=device)
 
-    def forward(self, h: torch.Tensor):
-        shape = h.shape
-        out, loss_var = self.feed(self.norm(h).reshape(-1, shape[-1]))
-        return h + out.reshape(shape), loss_var
+    def forward(self, h: torch.Tensor, residual: torch.Tensor | None = None):
+        if residual is None:
+            z = self.norm(h)
+        else:
+            z, h = _add_norm(self.norm, h, residual)
+        out, loss_var = self.feed(z.reshape(-1, z.shape[-1]))
+        out = out.reshape(h.shape)
+        return (h + out if residual is None else (out, h)), loss_var
 
     def feed(self, z: torch.Tensor):
         """The sublayer without its norm and residual, for rows z [T, d]: (W2 gelu(W1 DPB(z)), loss_var)."""
@@ -187,19 +215,23 @@ class KeyValueCache:
 class CausalAttention(torch.nn.Module):
     """h + W_o attention(rmsnorm(h)), queries, keys and values from one projection; `kv_heads`
     key heads are shared by `heads` query heads.  With a cache, h holds the tokens behind
-    those in it."""
+    those in it.  With a residual, h is h + residual, and (W_o ..., h + residual) comes back: the
+    two terms of the output, which the next norm adds."""
 
     def __init__(self, d: int, heads: int, kv_heads: int | None = None, dtype: torch.dtype = torch.float32, device=None):
         super().__init__()
         self.heads, self.kv_heads, self.head_dim = heads, kv_heads or heads, d // heads
         if self.head_dim * heads != d:
             raise ValueError(f"{heads} heads do not divide a width of {d}")
-        self.norm = torch.nn.RMSNorm(d, dtype=dtype, device=device)
+        self.norm = RMSNorm(d, dtype=dtype, device=device)
         self.qkv = torch.nn.Linear(d, (heads + 2 * self.kv_heads) * self.head_dim, bias=False, dtype=dtype, device=device)
         self.out = torch.nn.Linear(d, d, bias=False, dtype=dtype, device=device)
 
-    def forward(self, h: torch.Tensor, cache: KeyValueCache | None = None):
-        return h + self.mix(self.norm(h), cache)
+    def forward(self, h: torch.Tensor, cache: KeyValueCache | None = None, residual: torch.Tensor | None = None):
+        if residual is None:
+            return h + self.mix(self.norm(h), cache)
+        z, h = _add_norm(self.norm, h, residual)
+        return self.mix(z, cache), h
 
     def mix(self, z: torch.Tensor, cache: KeyValueCache | None = None):
         """The sublayer without its norm and residual: W_o attention(z)."""
@@ -218,7 +250,8 @@ class CausalAttention(torch.nn.Module):
 
 class ParityBlock(torch.nn.Module):
     """One block of a Parity Transformer: causal attention, then DPBMLP (§3.1).  forward
-    returns (output, loss_var)."""
+    returns (output, loss_var); with a residual, as the sublayers do, the input is
+    h + residual and the output its last two terms."""
 
     def __init__(self, plan: B.Plan, heads: int, d_ff: int, kv_heads: int | None = None,
                  dtype: torch.dtype = torch.float32, device=None, **mlp):
@@ -226,8 +259,10 @@ class ParityBlock(torch.nn.Module):
         self.attention = CausalAttention(plan.d, heads, kv_heads, dtype, device)
         self.mlp = DPBMLP(plan, d_ff, dtype=dtype, device=device, **mlp)
 
-    def forward(self, h: torch.Tensor, cache: KeyValueCache | None = None):
-        return self.mlp(self.attention(h, cache))
+    def forward(self, h: torch.Tensor, cache: KeyValueCache | None = None, residual: torch.Tensor | None = None):
+        if residual is None:
+            return self.mlp(self.attention(h, cache))
+        return self.mlp(*self.attention(h, cache, residual))
 
 
 def _even(t: torch.Tensor) -> torch.Tensor:
@@ -267,6 +302,16 @@ class EmbeddingLayer(torch.autograd.Function):
 def embedding_layer(tokens: torch.Tensor, table: torch.Tensor, scale: float = 1.0):
     """Functional form of EmbeddingLayer."""
     return EmbeddingLayer.apply(tokens, table, scale)
+
+
+class Embedding(torch.nn.Embedding):
+    """torch.nn.Embedding by EmbeddingLayer: rows of the weight for tokens, zeros for those outside it."""
+
+    def __init__(self, vocab: int, dim: int, dtype: torch.dtype = torch.float32, device=None):
+        super().__init__(vocab, dim, dtype=dtype, device=device)
+
+    def forward(self, tokens: torch.Tensor):
+        return EmbeddingLayer.apply(tokens, self.weight)
 
 
 class RMSNormLayer(torch.autograd.Function):
@@ -329,28 +374,22 @@ def cross_entropy_layer(hidden: torch.Tensor, weight: torch.Tensor, targets: tor
 class ParityTransformer(torch.nn.Module):
     """Tied token embeddings, learned positions and RMSNorm around ParityBlocks (§3.1).
 
-    The residual stream is carried as its two last terms, so that each addition is
-    part of the next norm; the blocks' own modules and parameters are used as they
-    are.  forward gives logits; loss the mean loss of the tokens that count, without
-    logits in memory."""
+    The residual stream is carried from module to module as its two last terms, so that
+    each addition is part of the next norm: block(x, cache, h) gives the next ((x, h), loss_var),
+    which is what hooks and wrappers meet.  Every module is called as one; a norm
+    of another kind in a norm's place follows an addition of its own.  forward gives
+    logits; loss the mean loss of the tokens that count, without logits in memory."""
 
     def __init__(self, plan: B.Plan, vocab: int, length: int, layers: int, heads: int, d_ff: int, kv_heads: int | None = None,
                  dtype: torch.dtype = torch.float32, device=None, std: float = 0.02, **mlp):
         super().__init__()
-        self.embed = torch.nn.Embedding(vocab, plan.d, dtype=dtype, device=device)
-        self.position = torch.nn.Embedding(length, plan.d, dtype=dtype, device=device)
+        self.embed = Embedding(vocab, plan.d, dtype=dtype, device=device)
+        self.position = Embedding(length, plan.d, dtype=dtype, device=device)
         torch.nn.init.normal_(self.embed.weight, std=std)
         torch.nn.init.normal_(self.position.weight, std=std)
         self.blocks = torch.nn.ModuleList(
             ParityBlock(plan, heads, d_ff, kv_heads, dtype=dtype, device=device, **mlp) for _ in range(layers))
-        self.norm = torch.nn.RMSNorm(plan.d, dtype=dtype, device=device)
-
-    @staticmethod
-    def _norm(norm: torch.nn.RMSNorm, x: torch.Tensor, residual: torch.Tensor):
-        # (torch.nn.RMSNorm's own default, in bf16 too)
-        eps = torch.finfo(torch.float32).eps if norm.eps is None else norm.eps
-        # (under autocast a sublayer's output has not the stream's type)
-        return RMSNormLayer.apply(x.to(residual.dtype), norm.weight, residual, eps)
+        self.norm = RMSNorm(plan.d, dtype=dtype, device=device)
 
     def hidden(self, tokens: torch.Tensor, caches=None, start: int = 0):
         """(rows behind the last norm, the blocks' summed variance loss); with caches, tokens are
@@ -358,15 +397,12 @@ class ParityTransformer(torch.nn.Module):
         if start < 0 or start + tokens.shape[1] > self.position.num_embeddings:
             raise ValueError(f"tokens {start} to {start + tokens.shape[1]}: the model has {self.position.num_embeddings} places")
         at = torch.arange(start, start + tokens.shape[1], device=tokens.device).expand_as(tokens)
-        x, h = EmbeddingLayer.apply(tokens, self.embed.weight), EmbeddingLayer.apply(at, self.position.weight)
+        x, h = self.embed(tokens), self.position(at)
         loss_var = 0.0
         for i, block in enumerate(self.blocks):
-            z, h = self._norm(block.attention.norm, x, h)
-            x = block.attention.mix(z, None if caches is None else caches[i])
-            z, h = self._norm(block.mlp.norm, x, h)
-            x, loss = block.mlp.feed(z.flatten(0, 1))
-            x, loss_var = x.view(z.shape), loss_var + loss
-        return self._norm(self.norm, x, h)[0], loss_var
+            (x, h), loss = block(x, None if caches is None else caches[i], h)
+            loss_var = loss_var + loss
+        return _add_norm(self.norm, x, h)[0], loss_var
 
     def forward(self, tokens: torch.Tensor, caches=None, start: int = 0):
         return torch.nn.functional.linear(self.hidden(tokens, caches, start)[0], self.embed.weight)

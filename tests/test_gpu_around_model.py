@@ -185,3 +185,29 @@ def test_a_batch_of_padding_alone():
     loss.backward()
     assert float(loss.detach()) == 0.0 and not model.embed.weight.grad.any()
     assert all(torch.isfinite(p.grad).all() for p in model.parameters() if p.grad is not None)
+
+
+def test_a_model_of_checkpointed_blocks():
+    """Blocks behind a wrapper that runs their forward once more in the backward: the same loss and gradients."""
+    class Wrapper(torch.nn.Module):
+        def __init__(self, block):
+            super().__init__()
+            self.block = block
+
+        def forward(self, *args):
+            return torch.utils.checkpoint.checkpoint(self.block, *args, use_reentrant=False)
+
+    model = model_of()
+    tokens = torch.randint(501, (3, 37), device=DEV)
+    want, _ = model.loss(tokens, tokens)
+    want.backward()
+    wanted = [p.grad.clone() for p in model.parameters()]
+    model.zero_grad()
+    for i in range(len(model.blocks)):
+        model.blocks[i] = Wrapper(model.blocks[i])
+    loss, _ = model.loss(tokens, tokens)
+    loss.backward()
+    assert torch.equal(loss, want)
+    for p, g in zip(model.parameters(), wanted):
+        # (products of the library may add up in another order)
+        assert (p.grad - g).abs().max() <= 1e-5 * g.abs().max()
