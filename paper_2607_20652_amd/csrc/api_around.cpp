@@ -220,6 +220,8 @@ static dpb_status logits_ok(const dpb_logits* a, dpb_dtype dtype, bool backward)
     if (!a || !dtype_ok(dtype) || a->rows < 0 || a->vocab < 0 || a->dim < 1 || !(a->scale > 0.f) || !std::isfinite(a->scale) ||
         a->hidden_stride < 0 || a->weight_stride < 0)
         return DPB_EINVAL;
+    // (the kernels form logits as exponents of 2)
+    if (!std::isfinite(a->scale * 1.4426950408889634f)) return DPB_EUNSUPPORTED;
     const int64_t b = bytes_of(dtype);
     if (a->rows >= kMaxRows || a->vocab >= kMaxRows || round_up(a->dim * b, 16) >= kMaxStride || a->hidden_stride >= kMaxStride / b ||
         a->weight_stride >= kMaxStride / b || !dpb::loss_launchable(a->rows, a->vocab, a->dim, backward))

@@ -210,3 +210,14 @@ def test_rows_in_memory():
     for bad in (x[:, :3], x.transpose(0, 1), x[..., ::2], x.transpose(1, 2)):
         with pytest.raises(ValueError):
             dpb._rows(bad, "x")
+
+
+def test_a_scale_whose_exponents_overflow_is_refused():
+    """exp(l) is 2^(l log2(e)): scale log2(e) has to be an fp32 number as well."""
+    lib, most = dpb.load(), 3.4028234e38 / 1.4426952
+    for scale in (2.4e38, 3e38, 3.4028234e38):
+        assert loss(scale=scale) == EUNSUPPORTED and loss_bwd(scale=scale) == EUNSUPPORTED
+        assert lib.dpb_cross_entropy_workspace_bytes(logits(scale=scale), 1) == 0
+        assert lib.dpb_cross_entropy_bwd_workspace_bytes(logits(scale=scale), 1) == 0
+    for scale in (0.9999 * most, 1e-30):
+        assert lib.dpb_cross_entropy_workspace_bytes(logits(scale=scale), 1) == lib.dpb_cross_entropy_workspace_bytes(logits(), 1) > 0
