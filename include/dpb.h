@@ -596,8 +596,9 @@ typedef struct {
 /* CROSS ENTROPY, the logits never in memory:
  *   lse[t]  = log sum_v exp logits[t, v]
  *   loss[t] = lse[t] - logits[t, targets[t]],  0 for a target outside [0, vocab)
- * loss, lse: device fp32 [rows].  A row whose logits are not all finite gets values that are
- * not; it does not reach other rows' results.  The workspace sizes go by sizes and strides
+ * loss, lse: device fp32 [rows].  A logit of -inf has the probability 0 (and as a target's the loss
+ * inf); NaN and +inf, which logits past 2.35e38 count as, make their row's lse NaN or inf, and its loss NaN or inf where
+ * it has one.  No row reaches other rows' results.  The workspace sizes go by sizes and strides
  * alone (0 for a description that the call refuses). */
 size_t dpb_cross_entropy_workspace_bytes(const dpb_logits* a, dpb_dtype dtype);
 dpb_status dpb_cross_entropy(const dpb_logits* a, dpb_dtype dtype, const void* targets, int index_bits, float* loss,

@@ -201,3 +201,27 @@ def test_nothing_to_do_and_given_outputs():
     grads = [torch.empty_like(h), torch.empty_like(w)]
     got = dpb.cross_entropy_bwd(want[0], h, w, t, want[1], dhidden=grads[0], dweight=grads[1])
     assert got[0] is grads[0] and all(torch.equal(a, b) for a, b in zip(got, dpb.cross_entropy_bwd(want[0], h, w, t, want[1])))
+
+
+@TYPES
+def test_a_logit_of_minus_infinity_is_no_entry(dtype):
+    """Loss and log-sum-exp are those of the vocabulary without it, and what is one token's stays with it."""
+    h, w, t, _, _ = draw(200, 72, 700, dtype)
+    h, t = h.abs() + 0.5, t.clamp(0, 699)
+    t[t == 400] = 0
+    w = w.clone()
+    w[400] = 1.0
+    w[400, 7] = float("-inf")
+    rest = torch.cat([w[:400], w[401:]])
+    (want, off), (want_lse, lse_off), _ = R.cross_entropy(h, rest, t - (t > 400).long(), 0.3)
+    loss, lse = dpb.cross_entropy(h, w, t, 0.3)
+    R.check("loss", loss, want, off)
+    R.check("lse", lse, want_lse, lse_off)
+    t[3], h[5, 7], h[6, 0] = 400, -1.0, float("nan")      # the target's logit is -inf; +inf; NaN
+    loss, lse = dpb.cross_entropy(h, w, t, 0.3)
+    assert loss[3] == float("inf") and torch.isfinite(lse[3])
+    assert not torch.isfinite(loss[5:7]).any() and not torch.isfinite(lse[5:7]).any()
+    fine = torch.ones(200, dtype=torch.bool, device=DEV)
+    fine[[3, 5, 6]] = False
+    R.check("loss", loss[fine], want[fine], off[fine])
+    R.check("lse", lse[fine], want_lse[fine], lse_off[fine])
