@@ -204,3 +204,21 @@ def test_the_last_token_of_each_long_sequence(dtype, length):
             second = loss, lse, *torch.autograd.grad((loss * ga).sum() + lse.sum(), (near, table))
     assert all(torch.equal(first[i], second[i]) for i in (0, 1, 3))
     assert torch.equal(first[2][:, -1], second[2]) and not first[2][:, :-1].any()
+
+
+@TYPES
+@pytest.mark.parametrize("rows,dim,vocab", [
+    (8192, 200, 20000),     # scores in tiles of 256 with seven steps: four and three
+    (4096, 320, 16384),     # ten: twice four and two
+    (4096, 570, 16384),     # eighteen, the last of which is not full
+])
+def test_steps_that_are_no_multiple_of_the_stages(rows, dim, vocab, dtype):
+    h, w, t, ga, ge = draw(rows, dim, vocab, dtype)
+    loss, lse = dpb.cross_entropy(h, w, t, 0.7)
+    want_loss, want_lse, _ = R.cross_entropy(h, w, t, 0.7)
+    R.check("loss", loss, *want_loss)
+    R.check("lse", lse, *want_lse)
+    got = dpb.cross_entropy_bwd(ga, h, w, t, lse, 0.7, grad_lse=ge)
+    for name, x, want in zip(("dhidden", "dweight"), got, R.cross_entropy_bwd(ga, h, w, t, lse, 0.7, ge)):
+        R.check(name, x, *want)
+    assert all(torch.equal(a, b) for a, b in zip(got, dpb.cross_entropy_bwd(ga, h, w, t, lse, 0.7, grad_lse=ge)))
