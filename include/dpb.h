@@ -583,7 +583,7 @@ dpb_status dpb_rms_norm_bwd(dpb_dtype dtype, const void* grad_out, int64_t grad_
  *   logits = scale * hidden [rows, dim] * weight [vocab, dim]^T,   0 < scale < 2.35e38
  * (the largest fp32 number over log2(e): logits are formed as exponents of 2).
  * Both start on 16 bytes; strides of their rows are any (under 8 MiB, and so is a row): rows that
- * do not start on 16 bytes are copied into the workspace first.  rows * vocab < 2^35 or so: 2^24
+ * do not start on 16 bytes are copied into the workspace first.  rows * vocab < 2^36 or so: 2^24
  * tiles of 64 x 64. */
 typedef struct {
     const void *hidden, *weight;

@@ -580,8 +580,8 @@ Cut cut(int64_t m, int64_t n, int64_t k, bool bf16, bool split)
     return best;
 }
 
-// The backward's pieces of the vocabulary: at most 1 GiB of D, and rows of 8 MiB (those of a tile stay
-// within a 31-bit offset).
+// The backward's pieces of the vocabulary: at most 1 GiB of D, or 1,024 entries' (more than 1 GiB from 524,288 bf16
+// or 262,144 fp32 tokens on), and rows of 8 MiB (those of a tile stay within a 31-bit offset).
 constexpr int64_t kPieceBytes = (int64_t)1 << 30, kPieceRow = (int64_t)1 << 23;
 struct Backward {
     int64_t piece;       // vocabulary entries of a piece (the last one may have fewer)

@@ -195,12 +195,12 @@ struct Job {
 // E x E tiles, one behind the other: a tile's first loads are sent while the one before is being stored;
 // run() adds up its products.
 //
-// Large bf16 tiles take 32 contraction values a step through five stages of 32 KB: a step of 1,024
-// MFMA cycles is shorter than memory's latency, four of them are not.  Smaller ones share a compute unit
-// and take twice that through two stages; fp32 steps last 4,096 cycles.
+// Large bf16 tiles take 32 contraction values a step through four stages of 32 KB: a step of 1,024
+// MFMA cycles is shorter than memory's latency, the three that a load is ahead are not (a fifth stage gained
+// nothing).  Smaller ones share a compute unit and take twice that through two stages; fp32 steps last 4,096 cycles.
 template <typename T, bool TA, bool TB, Lies LB, int E>
 struct Product {
-        static constexpr int kK = E == 256 ? 32 : 128 / (int)sizeof(T), kStages = E == 256 ? 4 : 2;
+    static constexpr int kK = E == 256 ? 32 : 128 / (int)sizeof(T), kStages = E == 256 ? 4 : 2;
     typedef Panel<T, TA, Lies::rows, E, kK> PA;
     typedef Panel<T, TB, LB, E, kK> PB;
     typedef typename Operand<T>::type Op;
