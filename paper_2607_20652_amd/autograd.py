@@ -29,8 +29,9 @@ and `ParityBlock` the two sublayers of one transformer block.
 
 `EmbeddingLayer`, `RMSNormLayer` and `CrossEntropyLayer` are what stands around the
 blocks as differentiable functions: the lookup of a table's rows, the residual's
-addition with the norm of the sum, and the loss over a vocabulary; `ParityTransformer`
-is the whole model from them (§3.1).
+addition with the norm of the sum, and the loss over a vocabulary; `Embedding` and
+`RMSNorm` are torch's modules by the first two, and `ParityTransformer` is the whole model
+from them (§3.1).
 """
 from __future__ import annotations
 
